@@ -415,6 +415,163 @@ int32_t dip_tiered_mlp_forward(const dip_tiered_mlp* mlp, const float* x, int32_
                                float* y_out, const dip_debug* dbg, void* ws, size_t ws_bytes,
                                void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Around the MLP: one (speculative) decode step over a paged key/value cache
+ *
+ * A step takes `n_batch` sequences and, of each, a few new rows: the next token alone, a piece
+ * of a prompt, or a tree of drafted tokens whose node 0 is the last token the sequence has
+ * (at most DIP_MAX_TREE nodes).  dip_kv_reserve makes room for the rows, dip_kv_append writes
+ * a layer's keys and values of them, dip_window_attention / dip_tree_attention attend,
+ * dip_verify_tree says which drafts stand, dip_kv_compact keeps those and commits.
+ * ------------------------------------------------------------------------------------------ */
+
+/* A paged key/value cache, owned by the caller.  Element (layer l, page p, head h, slot s, dim d)
+ * of k and of v lies l * layer_stride + p * page_stride + h * head_stride + s * slot_stride + d
+ * elements from its start, so that heads may come before slots or behind them; all starts and
+ * strides are multiples of 16 bytes.  Position i of sequence q is slot i % page_size of page
+ * page_table[q * max_pages + i / page_size].
+ * A table entry or sequence number outside its range is never followed out of bounds: rows that
+ * would be written there are dropped, and what is read there is taken from page 0. */
+typedef struct dip_kv_cache {
+    void* k;              /* device                                                          */
+    void* v;              /* device; the same type and strides                               */
+    int32_t* page_table;  /* device; n_seqs * max_pages entries, -1: no page                 */
+    int32_t* seq_len;     /* device; n_seqs: committed tokens of each sequence               */
+    int32_t* page_refs;   /* device; n_pages: table entries that name the page, 0: free      */
+    int32_t dtype;        /* DIP_F32 or DIP_BF16                                             */
+    int32_t n_layers;
+    int32_t n_pages;
+    int32_t page_size;    /* slots of a page, a power of two in [1, 4096]                    */
+    int32_t n_kv_heads;
+    int32_t head_dim;     /* a multiple of 16 bytes; the attention calls: 64, 96 or 128      */
+    int32_t n_seqs;
+    int32_t max_pages;    /* of one sequence; max_pages * page_size < 2^31                   */
+    int64_t layer_stride; /* in elements                                                     */
+    int64_t page_stride;
+    int64_t head_stride;
+    int64_t slot_stride;
+} dip_kv_cache;
+
+/* The rows of one step.  Entry b is sequence seqs[b] with rows row_start[b] .. row_start[b+1] - 1
+ * of every row-indexed array; its row t stands at position seq_len + t (in a tree: node t).  The
+ * host fields size the launches: rows of an entry beyond max_rows, and rows from n_rows on, are
+ * not looked at, and a sequence longer than max_len (its new rows included) is read up to max_len
+ * positions only. */
+typedef struct dip_batch {
+    const int32_t* seqs;      /* device; n_batch distinct sequences (dip_verify_tree: may be NULL)  */
+    const int32_t* row_start; /* device; n_batch + 1 entries, ascending from 0 to n_rows            */
+    int32_t n_batch;          /* 1 .. DIP_MAX_BATCH                                                 */
+    int32_t n_rows;           /* rows of all entries, >= 1                                          */
+    int32_t max_rows;         /* most rows of one entry, >= 1                                       */
+    int32_t max_len;          /* most tokens of one sequence after this step (0: what fits the table) */
+} dip_batch;
+
+#define DIP_MAX_BATCH 1024
+#define DIP_MAX_TREE 64
+
+/* Every page free, every sequence empty (page_refs, page_table and seq_len are written; k and v are not). */
+int32_t dip_kv_init(const dip_kv_cache* cache, void* stream);
+
+/* Give up all pages of the n listed sequences (device array; a page is free when nobody holds it) and
+ * make them empty.  Entries outside [0, n_seqs) are skipped, repeated ones count once. */
+int32_t dip_kv_free(const dip_kv_cache* cache, const int32_t* seqs, int32_t n, void* stream);
+
+/* Sequence dst[i] becomes a copy of sequence src[i] that shares its pages (up to seq_len tokens),
+ * i < n (device arrays).  The destinations are empty and distinct, and none is a source; several may
+ * have one source. */
+int32_t dip_kv_fork(const dip_kv_cache* cache, const int32_t* src, const int32_t* dst, int32_t n, void* stream);
+
+/* Copy whole pages, all layers, k and v: page src[i] to page dst[i], i < n (device arrays; the
+ * destinations are distinct and none is a source; pairs out of range are skipped).  Tables and
+ * counts stay as they are. */
+int32_t dip_kv_copy_pages(const dip_kv_cache* cache, const int32_t* src, const int32_t* dst, int32_t n, void* stream);
+
+/*
+ * Make room for the rows of a step: every entry gets pages of its own for positions seq_len ..
+ * seq_len + rows - 1.  A table entry without a page takes a free one; a page that other sequences
+ * hold too when the call starts is exchanged for a free one, and what the entry has of it is copied
+ * (copy on write; all layers).  The lowest free pages are given out, to the entries in order and to
+ * each in order of position.  An entry whose pages, with all that earlier entries asked for, exceed the
+ * free ones (or whose rows do not fit the table) gets none: granted[b] = 0 and its table stays;
+ * otherwise granted[b] = 1.  Calling it again for the same rows changes nothing.
+ *   granted  n_batch words or NULL      ws  *_workspace_bytes() bytes, 256-aligned
+ */
+size_t dip_kv_reserve_workspace_bytes(const dip_kv_cache* cache, const dip_batch* batch);
+int32_t dip_kv_reserve(const dip_kv_cache* cache, const dip_batch* batch, int32_t* granted, void* ws,
+                       size_t ws_bytes, void* stream);
+
+/*
+ * Write keys and values of the step's rows into layers layer .. layer + n_layers - 1.  Row r of
+ * layer l: n_kv_heads * head_dim elements at l * new_layer_stride + r * row_stride of k_new and
+ * v_new (elements; multiples of 16 bytes; l counts from 0).  seq_len stays (dip_kv_compact commits).
+ */
+int32_t dip_kv_append(const dip_kv_cache* cache, int32_t layer, int32_t n_layers, const dip_batch* batch,
+                      const void* k_new, const void* v_new, int64_t row_stride, int64_t new_layer_stride,
+                      void* stream);
+
+/*
+ * Keep keep[b] rows of every entry (device; values are clamped to its rows; NULL: all of them) and
+ * commit: row path[row_start[b] + j] of the entry moves to row j, j < keep[b], in every layer (path:
+ * device, n_rows entries, ascending within an entry, path[j] >= j; NULL: the first keep[b] rows
+ * stay where they are), seq_len += keep[b], and pages beyond the new length are given up.  Rows
+ * that have no page (an entry that dip_kv_reserve granted nothing) are not committed.
+ */
+int32_t dip_kv_compact(const dip_kv_cache* cache, const dip_batch* batch, const int32_t* path, const int32_t* keep,
+                       void* stream);
+
+/*
+ * Attention of a step's rows over the cache, their own keys and values already in it.  Query head h
+ * attends with key/value head h / (n_q_heads / n_kv_heads):
+ *     out[r, h] = sum_j p_j v_j,   p = softmax over the visible j of scale * q[r, h] . k_j
+ * dip_window_attention: row t of an entry stands at pos = seq_len + t and sees
+ *     j <= pos  and  (j > pos - window  or  j < sinks).
+ * dip_tree_attention: parents[r] is the entry's node that drafted node t (-1: none, any other value
+ * outside [0, t): the node is absent, as are the nodes below an absent one); node t stands at pos =
+ * seq_len + its depth, sees the ancestors that are nodes of the tree and itself, and of the committed
+ * positions j < seq_len those with  j > pos - window  or  j < sinks.
+ * window 0 means no bound (sinks then change nothing).  A row that sees nothing, and an absent node,
+ * gets zeros.  Positions that a row does not see do not matter to it, whatever they hold.
+ *   q, out   n_rows rows of n_q_heads * head_dim elements of the cache's type, q_stride / out_stride
+ *            elements apart (multiples of 16 bytes); out may not overlap q
+ *   scale > 0      n_q_heads a multiple of n_kv_heads      ws  *_workspace_bytes() bytes, 256-aligned
+ * Scores, softmax statistics and sums are fp32; with a DIP_BF16 cache the weights p enter their product
+ * with v as bf16.  The order of the sums is fixed by shapes, lengths and max_len (bit-repeatable).
+ */
+size_t dip_attention_workspace_bytes(const dip_kv_cache* cache, const dip_batch* batch, int32_t n_q_heads,
+                                     int32_t window, int32_t sinks);
+int32_t dip_window_attention(const dip_kv_cache* cache, int32_t layer, const dip_batch* batch, const void* q,
+                             int64_t q_stride, int32_t n_q_heads, float scale, int32_t window, int32_t sinks,
+                             void* out, int64_t out_stride, void* ws, size_t ws_bytes, void* stream);
+int32_t dip_tree_attention(const dip_kv_cache* cache, int32_t layer, const dip_batch* batch, const int32_t* parents,
+                           const void* q, int64_t q_stride, int32_t n_q_heads, float scale, int32_t window,
+                           int32_t sinks, void* out, int64_t out_stride, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Verification of drafted trees (entries and parents as in dip_tree_attention, at most DIP_MAX_TREE
+ * nodes).  Node t carries tokens[r]; p[r] is the target's distribution behind node t and q[r] the one
+ * its children were drawn from, independently.  From node 0 on, the children of a node are tried in
+ * order, child j (from 0) with its number u[r] in [0, 1):
+ *     taken iff  u q(x) G_j < (p(x) - lam_j q(x))+ ,   lam_0 = 0, G_0 = 1,
+ *     lam_{j+1} = lam_j + G_j,   G_j = sum_x (p(x) - lam_j q(x))+  for j >= 1,
+ * which is the rule  r <- norm((r - q)+) after each refused child: the j-th r is (p - lam_j q)+ / G_j.
+ * A child that is taken is the next node; where none is (m children), the next token is the first x with
+ *     sum_{y <= x} w(y) > u_sample[b] * sum w,   w = (p - lam_m q)+  (p itself where that is all zero).
+ *   p, q       n_rows rows of n_vocab probabilities (both DIP_F32 or DIP_BF16), p_stride / q_stride
+ *              elements apart
+ *   max_kids   1 .. DIP_MAX_TREE - 1: children of a node beyond that many are passed over
+ *   keep       n_batch: nodes that stand, node 0 among them (0: the entry has no rows, or its node 0
+ *              is no root)
+ *   path       n_rows: the nodes that stand, then -1            token   n_batch: -1 where keep is 0 or
+ *              p has no positive entry
+ * Sums and comparisons are in 64 bits.  A token outside [0, n_vocab) is never taken.
+ *   ws  *_workspace_bytes() bytes, 256-aligned
+ */
+size_t dip_verify_tree_workspace_bytes(const dip_batch* batch, int32_t n_vocab, int32_t max_kids);
+int32_t dip_verify_tree(const dip_batch* batch, const int32_t* tokens, const int32_t* parents, const void* p,
+                        int64_t p_stride, const void* q, int64_t q_stride, int32_t dtype, int32_t n_vocab,
+                        const float* u, const float* u_sample, int32_t max_kids, int32_t* keep, int32_t* path,
+                        int32_t* token, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,4 +22,7 @@ from .libdip import (  # noqa: F401
     dip_partial_pruning_forward_workspace_bytes,
     dip_swiglu_mlp_forward_batched, dip_swiglu_mlp_forward_batched_workspace_bytes,
     dip_swiglu_mlp_forward_batched_stack, dip_swiglu_mlp_forward_batched_stack_workspace_bytes, dip_profile_read, dip_profile_disable,
+    DIP_MAX_BATCH, DIP_MAX_TREE, Batch, KvCache, dip_kv_init, dip_kv_free, dip_kv_fork, dip_kv_copy_pages,
+    dip_kv_reserve, dip_kv_reserve_workspace_bytes, dip_kv_append, dip_kv_compact, dip_attention_workspace_bytes,
+    dip_window_attention, dip_tree_attention, dip_verify_tree, dip_verify_tree_workspace_bytes,
 )

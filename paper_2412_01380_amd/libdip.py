@@ -69,6 +69,19 @@ class _TieredMlp(C.Structure):
     _fields_ = [("w_ug", _TieredWeight), ("w_d", _TieredWeight)]
 
 
+class _KvCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_table", C.c_void_p), ("seq_len", C.c_void_p),
+                ("page_refs", C.c_void_p), ("dtype", C.c_int32), ("n_layers", C.c_int32), ("n_pages", C.c_int32),
+                ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("n_seqs", C.c_int32),
+                ("max_pages", C.c_int32), ("layer_stride", C.c_int64), ("page_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("slot_stride", C.c_int64)]
+
+
+class _Batch(C.Structure):
+    _fields_ = [("seqs", C.c_void_p), ("row_start", C.c_void_p), ("n_batch", C.c_int32), ("n_rows", C.c_int32),
+                ("max_rows", C.c_int32), ("max_len", C.c_int32)]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(lib_path):
         raise ImportError(
@@ -146,6 +159,22 @@ def _load() -> C.CDLL:
     L.dip_tiered_mlp_forward.restype = i32
     L.dip_tiered_mlp_forward.argtypes = [C.POINTER(_TieredMlp), vp, i32, i32, C.POINTER(_Cache),
                                          C.POINTER(_Cache), f32, vp, C.POINTER(_Debug), vp, sz, vp]
+    kv, bt = C.POINTER(_KvCache), C.POINTER(_Batch)
+    for name, args in {
+            "dip_kv_init": [kv, vp], "dip_kv_free": [kv, vp, i32, vp], "dip_kv_fork": [kv, vp, vp, i32, vp],
+            "dip_kv_copy_pages": [kv, vp, vp, i32, vp], "dip_kv_reserve": [kv, bt, vp, vp, sz, vp],
+            "dip_kv_append": [kv, i32, i32, bt, vp, vp, i64, i64, vp], "dip_kv_compact": [kv, bt, vp, vp, vp],
+            "dip_window_attention": [kv, i32, bt, vp, i64, i32, f32, i32, i32, vp, i64, vp, sz, vp],
+            "dip_tree_attention": [kv, i32, bt, vp, vp, i64, i32, f32, i32, i32, vp, i64, vp, sz, vp],
+            "dip_verify_tree": [bt, vp, vp, vp, i64, vp, i64, i32, i32, vp, vp, i32, vp, vp, vp, vp, sz, vp]}.items():
+        getattr(L, name).restype = i32
+        getattr(L, name).argtypes = args
+    L.dip_kv_reserve_workspace_bytes.restype = sz
+    L.dip_kv_reserve_workspace_bytes.argtypes = [kv, bt]
+    L.dip_attention_workspace_bytes.restype = sz
+    L.dip_attention_workspace_bytes.argtypes = [kv, bt, i32, i32, i32]
+    L.dip_verify_tree_workspace_bytes.restype = sz
+    L.dip_verify_tree_workspace_bytes.argtypes = [bt, i32, i32]
     L.dip_tune_gemv.restype = i32
     L.dip_tune_gemv.argtypes = [i32, i32, i32, i32]
     L.dip_gemv_launch_shape.restype = i32
@@ -177,7 +206,10 @@ EXPORTS = ["dip_version", "dip_last_error", "dip_ca_scores", "dip_prune_topk", "
            "dip_swiglu_mlp_forward_batched_stack", "dip_glu_pruning_forward_workspace_bytes",
            "dip_glu_pruning_forward", "dip_gathered_rowdot",
            "dip_partial_pruning_forward_workspace_bytes", "dip_partial_pruning_forward", "dip_tier_init_workspace_bytes",
-           "dip_tier_init", "dip_tiered_mlp_forward_workspace_bytes", "dip_tiered_mlp_forward", "dip_tune_gemv", "dip_gemv_launch_shape", "dip_set_fusion", "dip_fused_launch_shape", "dip_stream_read", "dip_profile_enable", "dip_profile_read",
+           "dip_tier_init", "dip_tiered_mlp_forward_workspace_bytes", "dip_tiered_mlp_forward",
+           "dip_kv_init", "dip_kv_free", "dip_kv_fork", "dip_kv_copy_pages", "dip_kv_reserve_workspace_bytes", "dip_kv_reserve",
+           "dip_kv_append", "dip_kv_compact", "dip_attention_workspace_bytes", "dip_window_attention", "dip_tree_attention",
+           "dip_verify_tree_workspace_bytes", "dip_verify_tree", "dip_tune_gemv", "dip_gemv_launch_shape", "dip_set_fusion", "dip_fused_launch_shape", "dip_stream_read", "dip_profile_enable", "dip_profile_read",
            "dip_profile_disable"]
 
 
@@ -572,6 +604,164 @@ def dip_tiered_mlp_forward(mlp: TieredMlp, x, k_in: int, k_mid: int, cache_in: C
         C.byref(mlp.c), _ptr(x, torch.float32), k_in, k_mid, C.byref(cache_in.c), C.byref(cache_mid.c),
         gamma, _ptr(y_out, torch.float32), C.byref(dbg.c) if dbg is not None else None,
         _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+DIP_MAX_BATCH, DIP_MAX_TREE = 1024, 64
+
+
+class KvCache:
+    """A paged key/value cache over caller-owned device tensors: k and v [n_layers][n_pages][n_kv_heads]
+    [page_size][head_dim] (float32 or bfloat16; views with any strides of whole 16-byte pieces and a
+    contiguous head, so the storage may put slots before heads), page_table [n_seqs][max_pages],
+    seq_len [n_seqs] and page_refs [n_pages] int32."""
+
+    def __init__(self, k, v, page_table, seq_len, page_refs):
+        import torch
+        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+            raise TypeError("k and v must be 5-D tensors of one shape, layout and dtype")
+        if not k.is_cuda or not v.is_cuda or k.stride(4) != 1:
+            raise TypeError("k and v must be device tensors with unit inner stride")
+        if k.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"unsupported cache dtype {k.dtype}")
+        n_layers, n_pages, n_heads, page, dim = k.shape
+        if page_table.dim() != 2 or page_refs.numel() != n_pages or seq_len.numel() != page_table.shape[0]:
+            raise TypeError("page_table is [n_seqs][max_pages], seq_len [n_seqs], page_refs [n_pages]")
+        self.k, self.v, self.page_table, self.seq_len, self.page_refs = k, v, page_table, seq_len, page_refs
+        i32 = torch.int32
+        self.c = _KvCache(k.data_ptr(), v.data_ptr(), _ptr(page_table, i32), _ptr(seq_len, i32), _ptr(page_refs, i32),
+                          DIP_F32 if k.dtype == torch.float32 else DIP_BF16, n_layers, n_pages, page, n_heads, dim,
+                          page_table.shape[0], page_table.shape[1], k.stride(0), k.stride(1), k.stride(2), k.stride(3))
+        self.ref = C.byref(self.c)
+
+
+class Batch:
+    """The rows of one step: entry b is sequence seqs[b] with rows row_start[b] .. row_start[b+1] - 1
+    (int32 device tensors); n_rows in all, at most max_rows of one entry, and no sequence longer than
+    max_len with them (0: no bound but the page table)."""
+
+    def __init__(self, row_start, n_rows: int, max_rows: int, seqs=None, max_len: int = 0):
+        import torch
+        if row_start.numel() < 2 or (seqs is not None and seqs.numel() != row_start.numel() - 1):
+            raise TypeError("row_start has one entry more than seqs")
+        self.row_start, self.seqs, self.n_batch, self.n_rows = row_start, seqs, row_start.numel() - 1, n_rows
+        self.c = _Batch(_ptr(seqs, torch.int32), _ptr(row_start, torch.int32), self.n_batch, n_rows, max_rows, max_len)
+        self.ref = C.byref(self.c)
+
+
+def _rows(t, dtype, n_rows: int, what: str):
+    """(pointer, row stride in elements) of row-indexed data; everything behind the row index is contiguous."""
+    if not t.is_cuda or t.dtype != dtype:
+        raise TypeError(f"{what} must be a device tensor of {dtype}")
+    if t.shape[0] < n_rows:
+        raise TypeError(f"{what} has {t.shape[0]} rows of {n_rows}")
+    if t.shape[0] > 0 and not t[0].is_contiguous():
+        raise TypeError(f"a row of {what} must be contiguous")
+    return t.data_ptr(), t.stride(0)
+
+
+def _ints(t, n: int, what: str):
+    import torch
+    p = _ptr(t, torch.int32)
+    if t is not None and t.numel() < n:
+        raise TypeError(f"{what} has {t.numel()} entries of {n}")
+    return p
+
+
+def dip_kv_init(cache: KvCache, stream=None) -> None:
+    _check(lib.dip_kv_init(cache.ref, _stream(stream)))
+
+
+def dip_kv_free(cache: KvCache, seqs, stream=None) -> None:
+    _check(lib.dip_kv_free(cache.ref, _ints(seqs, 1, "seqs"), seqs.numel(), _stream(stream)))
+
+
+def dip_kv_fork(cache: KvCache, src, dst, stream=None) -> None:
+    n = src.numel()
+    _check(lib.dip_kv_fork(cache.ref, _ints(src, 1, "src"), _ints(dst, n, "dst"), n, _stream(stream)))
+
+
+def dip_kv_copy_pages(cache: KvCache, src, dst, stream=None) -> None:
+    n = src.numel()
+    _check(lib.dip_kv_copy_pages(cache.ref, _ints(src, 1, "src"), _ints(dst, n, "dst"), n, _stream(stream)))
+
+
+def dip_kv_reserve_workspace_bytes(cache: KvCache, batch: Batch) -> int:
+    return lib.dip_kv_reserve_workspace_bytes(cache.ref, batch.ref)
+
+
+def dip_kv_reserve(cache: KvCache, batch: Batch, granted, ws, stream=None) -> None:
+    _check(lib.dip_kv_reserve(cache.ref, batch.ref, _ints(granted, batch.n_batch, "granted"), _ptr(ws),
+                              ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def dip_kv_append(cache: KvCache, layer: int, batch: Batch, k_new, v_new, stream=None) -> None:
+    """k_new, v_new: [n_rows][n_kv_heads][head_dim] for one layer, or [n_layers][n_rows][n_kv_heads][head_dim]
+    for layers layer .. layer + n_layers - 1; rows may be strided (a slice of a fused projection)."""
+    if k_new.dim() not in (3, 4) or k_new.shape != v_new.shape or k_new.stride() != v_new.stride():
+        raise TypeError("k_new and v_new must have one shape and layout, rows x heads x dims")
+    if tuple(k_new.shape[-2:]) != (cache.k.shape[2], cache.k.shape[4]):
+        raise TypeError("k_new rows must be [n_kv_heads][head_dim]")
+    many = k_new.dim() == 4
+    k0, v0 = (k_new[0], v_new[0]) if many else (k_new, v_new)
+    kp, stride = _rows(k0, cache.k.dtype, batch.n_rows, "k_new")
+    vp, _ = _rows(v0, cache.k.dtype, batch.n_rows, "v_new")
+    _check(lib.dip_kv_append(cache.ref, layer, k_new.shape[0] if many else 1, batch.ref, kp, vp, stride,
+                             k_new.stride(0) if many else 0, _stream(stream)))
+
+
+def dip_kv_compact(cache: KvCache, batch: Batch, path, keep, stream=None) -> None:
+    _check(lib.dip_kv_compact(cache.ref, batch.ref, _ints(path, batch.n_rows, "path"),
+                              _ints(keep, batch.n_batch, "keep"), _stream(stream)))
+
+
+def dip_attention_workspace_bytes(cache: KvCache, batch: Batch, n_q_heads: int, window: int = 0, sinks: int = 0) -> int:
+    return lib.dip_attention_workspace_bytes(cache.ref, batch.ref, n_q_heads, window, sinks)
+
+
+def _attention_rows(cache: KvCache, batch: Batch, q, out):
+    if q.dim() != 3 or out.dim() != 3 or q.shape[1:] != out.shape[1:] or q.shape[2] != cache.k.shape[4]:
+        raise TypeError("q and out are [n_rows][n_q_heads][head_dim]")
+    return _rows(q, cache.k.dtype, batch.n_rows, "q") + _rows(out, cache.k.dtype, batch.n_rows, "out")
+
+
+def dip_window_attention(cache: KvCache, layer: int, batch: Batch, q, scale: float, window: int, sinks: int, out, ws,
+                         stream=None) -> None:
+    """q, out: [n_rows][n_q_heads][head_dim] of the cache's dtype; rows may be strided."""
+    qp, qs, op, os_ = _attention_rows(cache, batch, q, out)
+    _check(lib.dip_window_attention(cache.ref, layer, batch.ref, qp, qs, q.shape[1], scale, window, sinks, op, os_,
+                                    _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def dip_tree_attention(cache: KvCache, layer: int, batch: Batch, parents, q, scale: float, window: int, sinks: int, out,
+                       ws, stream=None) -> None:
+    """As dip_window_attention, for rows that are the nodes of drafted trees (parents: n_rows int32)."""
+    qp, qs, op, os_ = _attention_rows(cache, batch, q, out)
+    _check(lib.dip_tree_attention(cache.ref, layer, batch.ref, _ints(parents, batch.n_rows, "parents"), qp, qs, q.shape[1],
+                                  scale, window, sinks, op, os_, _ptr(ws), ws.numel() * ws.element_size(),
+                                  _stream(stream)))
+
+
+def dip_verify_tree_workspace_bytes(batch: Batch, n_vocab: int, max_kids: int) -> int:
+    return lib.dip_verify_tree_workspace_bytes(batch.ref, n_vocab, max_kids)
+
+
+def dip_verify_tree(batch: Batch, tokens, parents, p, q, u, u_sample, max_kids: int, keep, path, token, ws,
+                    stream=None) -> None:
+    """p, q: [n_rows][n_vocab] float32 or bfloat16, rows may be strided; u [n_rows], u_sample [n_batch] float32;
+    keep [n_batch], path [n_rows], token [n_batch] int32 outputs."""
+    import torch
+    n = batch.n_rows
+    if p.dtype not in (torch.float32, torch.bfloat16) or p.dim() != 2 or p.shape[1] != q.shape[1]:
+        raise TypeError("p and q are [n_rows][n_vocab], float32 or bfloat16")
+    if u.numel() < n or u_sample.numel() < batch.n_batch:
+        raise TypeError("u has n_rows entries, u_sample n_batch")
+    pp, ps = _rows(p, p.dtype, n, "p")
+    qp, qs = _rows(q, p.dtype, n, "q")
+    _check(lib.dip_verify_tree(batch.ref, _ints(tokens, n, "tokens"), _ints(parents, n, "parents"), pp, ps, qp, qs,
+                               DIP_F32 if p.dtype == torch.float32 else DIP_BF16, p.shape[1], _ptr(u, torch.float32),
+                               _ptr(u_sample, torch.float32), max_kids, _ints(keep, batch.n_batch, "keep"),
+                               _ints(path, n, "path"), _ints(token, batch.n_batch, "token"), _ptr(ws),
+                               ws.numel() * ws.element_size(), _stream(stream)))
 
 
 def dip_tune_gemv(lanes_per_row: int = 0, waves: int = 0, ksplit: int = 0, unroll: int = 0) -> None:
