@@ -1,0 +1,393 @@
+// What the attention kernels share: which keys a block of rows sees, key/value tiles in LDS, the two
+// matrix-core products of a tile and the running softmax between them.
+//
+// For a block of rows r (n = r % 16 the column of a product) and the keys m of a tile
+//     S^T = K Q^T          [keys x rows]     16x16 products, K from LDS, Q^T in registers
+//     P^T = exp2(c S^T - max)                in the registers that S^T came out in
+//     O^T = O^T + V^T P^T  [dims x rows]     V^T from LDS
+// A lane (column n = lane % 16, g = lane / 16) gets S^T of keys 4 g + i, i < 4, of each 16 keys, and that is
+// what the second product takes from it if V's keys come in the same order: P never leaves its lane.  A row's
+// maximum is one value per column, so rescaling O^T is a product with a lane's own number.
+#ifndef DIP_ATTN_DEVICE_H_
+#define DIP_ATTN_DEVICE_H_
+
+#include "dip_decode_internal.h"
+
+namespace dip {
+namespace attn {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+struct AttnParams {
+    KvView c;                 // k and v already at the layer
+    BatchView b;
+    const int32_t* parents;   // null: window attention
+    const char* q;
+    char* out;
+    int64_t q_stride;         // bytes
+    int64_t out_stride;
+    int n_q_heads;
+    int group;                // query heads of a key/value head
+    float scale_log2;         // scale * log2(e)
+    int window;               // 0: no bound
+    int sinks;
+    int max_len;
+    int splits;               // shares that a row block's keys are cut into
+    int tiles_per_split;
+    int row_blocks;           // of an entry and key/value head
+    float* part_o;            // [row block][split][rows of a block][D], not normalised
+    float2* part_ml;          // [row block][split][rows of a block]: maximum (times scale_log2), sum
+};
+
+// ---- which keys a block of rows sees -----------------------------------------------------------
+struct Range {
+    int tiles;                // tiles of KEYS positions that some row sees: the sinks' first ...
+    int sink_tiles;
+    int first;                // ... then those from here on
+    int end;                  // no row sees position `end` or anything behind it
+    int sure;                 // every row sees all positions below `sure` ...
+    int from;                 // ... from `from` on, and the sinks
+};
+template <int KEYS>
+__device__ __forceinline__ Range key_range(const AttnParams& p, int len, int rows, int t0, int t1) {
+    Range r;
+    int lo;                   // first position behind the sinks that some row sees
+    if (p.parents) {          // rows stand at len + depth, 0 <= depth < rows
+        r.end = len + rows;
+        r.sure = len;
+        lo = p.window ? max(0, len - p.window + 1) : 0;
+        r.from = p.window ? max(0, len + rows - p.window) : 0;
+    } else {
+        r.end = len + t1 + 1;
+        r.sure = len + t0 + 1;
+        lo = p.window ? max(0, len + t0 - p.window + 1) : 0;
+        r.from = p.window ? max(0, len + t1 - p.window + 1) : 0;
+    }
+    r.end = min(r.end, p.max_len);
+    r.sure = min(r.sure, p.max_len);
+    const int last = (r.end + KEYS - 1) / KEYS;
+    if (p.sinks >= lo) {
+        r.sink_tiles = 0;
+        r.first = 0;
+    } else {
+        r.sink_tiles = (min(p.sinks, r.end) + KEYS - 1) / KEYS;
+        r.first = max(lo / KEYS, r.sink_tiles);
+    }
+    r.tiles = r.sink_tiles + max(0, last - r.first);
+    return r;
+}
+__device__ __forceinline__ int tile_at(const Range& r, int vt) { return vt < r.sink_tiles ? vt : r.first + vt - r.sink_tiles; }
+
+// what one row sees
+struct RowSees {
+    int lo, hi;               // positions [lo, hi) and sinks below hi ...
+    uint64_t tree;            // ... and nodes of its tree
+};
+__device__ __forceinline__ bool sees(const RowSees& r, int j, int sinks, int len) {
+    const bool past = j < r.hi && (j >= r.lo || j < sinks);
+    const unsigned node = (unsigned)(j - len);
+    return past || (node < 64u && ((r.tree >> node) & 1));
+}
+
+// The ancestors of every node of an entry's tree, itself among them (0: the node is absent), into LDS by
+// one wavefront: pointers jump 1, 2, 4 .. steps up.
+__device__ __forceinline__ void tree_masks(const int32_t* parents, int rows, uint64_t* out) {
+    const int lane = threadIdx.x & 63;
+    int up = lane < rows ? parents[lane] : -2;
+    if (up < -1 || up >= lane) up = -2;
+    uint64_t mask = 1ull << lane;
+#pragma unroll
+    for (int i = 0; i < 6; ++i) {
+        const int at = up < 0 ? lane : up;
+        const uint32_t lo = __shfl((uint32_t)mask, at), hi = __shfl((uint32_t)(mask >> 32), at);
+        const int next = __shfl(up, at);
+        if (up >= 0) {
+            mask |= ((uint64_t)hi << 32) | lo;
+            up = next;
+        }
+    }
+    out[lane] = up == -1 ? mask : 0;
+}
+
+__device__ __forceinline__ RowSees row_sees(const AttnParams& p, int len, int t, const uint64_t* masks) {
+    RowSees r;
+    int pos = len + t;
+    r.tree = 0;
+    if (p.parents) {
+        r.tree = masks[t];
+        pos = len + __popcll(r.tree) - 1;
+        r.hi = r.tree ? len : 0;
+    } else {
+        r.hi = pos + 1;
+    }
+    r.lo = p.window ? max(0, pos - p.window + 1) : 0;
+    return r;
+}
+
+// ---- tiles in LDS --------------------------------------------------------------------------------
+// KEYS rows of D elements, 16-byte pieces swizzled so that 16 rows' pieces of one dim (a K operand) and
+// the 16 pieces of a row (a V operand) both fall on different banks.  Filled by loads that go to LDS
+// directly, each lane fetching the piece that belongs at its place.
+template <typename E, int D>
+struct Geo {
+    static constexpr int ES = sizeof(E);
+    static constexpr int ROWB = D * ES;
+    static constexpr int CPR = ROWB / 16;                  // pieces of a row
+    static constexpr int KEYS = ES == 2 ? 32 : 16;         // of one step of the products
+    __device__ static __forceinline__ int slot(int row, int c) {
+        if constexpr (CPR == 16 || CPR == 32) return c ^ (row & 15);
+        else if constexpr (CPR == 8) return c ^ ((row >> 1) & 7);
+        else if constexpr (CPR == 12) { const int s = c + ((row >> 2) & 3); return s >= 12 ? s - 12 : s; }
+        else { static_assert(CPR == 24, "row length"); const int s = c + ((row >> 1) & 7); return s >= 24 ? s - 24 : s; }
+    }
+    __device__ static __forceinline__ int piece(int row, int s) {   // the inverse
+        if constexpr (CPR == 16 || CPR == 32) return s ^ (row & 15);
+        else if constexpr (CPR == 8) return s ^ ((row >> 1) & 7);
+        else if constexpr (CPR == 12) { const int c = s - ((row >> 2) & 3); return c < 0 ? c + 12 : c; }
+        else { const int c = s - ((row >> 1) & 7); return c < 0 ? c + 24 : c; }
+    }
+};
+
+__device__ __forceinline__ uint32_t lds_offset(const void* p) { return (uint32_t)(size_t)(const lds_char*)p; }
+
+// 64 x 16 bytes from the lanes' addresses to LDS at `to` + 16 * lane.  Written in assembly because the
+// compiler would make every later LDS read wait for all of them; nothing but the counter says that they are
+// there, so readers wait with wait_loads().  (The load writes no register; m0 is put back.)
+__device__ __forceinline__ void load_to_lds(const char* from, uint32_t to) {
+    uint32_t m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "v"(from), "s"(to) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// ---- the two products ----------------------------------------------------------------------------
+__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+// maximum / sum over the four lanes of a column (lane ^ 16, lane ^ 32)
+__device__ __forceinline__ float column_max(float x) {
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float column_sum(float x) {
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// NB blocks of 16 rows of one wavefront.
+template <typename E, int D, int NB>
+struct Core;
+
+template <int D, int NB>
+struct Core<uint16_t, D, NB> {
+    typedef Geo<uint16_t, D> G;
+    static constexpr int KEYS = 32, MT = 2, OB = D / 16, QS = D / 32;
+    bf16x8 q[NB][QS];
+    f32x4 o[NB][OB];
+
+    __device__ __forceinline__ void load_q(int nb, const char* row) {      // row: the lane's column, or null
+#pragma unroll
+        for (int s = 0; s < QS; ++s) {
+            u32x4 x = {0, 0, 0, 0};
+            if (row) x = *(const u32x4*)(row + (4 * s + ((threadIdx.x & 63) >> 4)) * 16);
+            q[nb][s] = __builtin_bit_cast(bf16x8, x);
+        }
+    }
+    __device__ __forceinline__ void scores(const lds_char* k, f32x4 (&s)[NB][MT]) const {
+        const int m = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) s[nb][mt] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int st = 0; st < QS; ++st) {
+                const bf16x8 a = *(const __attribute__((address_space(3))) bf16x8*)(k + (16 * mt + m) * G::ROWB + G::slot(16 * mt + m, 4 * st + g) * 16);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) s[nb][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[nb][st], s[nb][mt], 0, 0, 0);
+            }
+        }
+    }
+    // p: the weights in place of the scores.  As one bf16 term each they are off by up to 2^-8, which over many
+    // keys averages out but shows where a few of them carry a row; with TWO the remainder is a second term.
+    template <bool TWO>
+    __device__ __forceinline__ void add_values(const lds_char* v, const f32x4 (&p)[NB][MT]) {
+        const int i = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+        bf16x8 w[NB], rest[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = p[nb][e >> 2][e & 3];
+                w[nb][e] = (__bf16)x;
+                if constexpr (TWO) rest[nb][e] = (__bf16)(x - (float)w[nb][e]);
+            }
+#pragma unroll
+        for (int db = 0; db < OB; ++db) {
+            // four keys at this lane's dim each: the transposing read hands lane i column i of 4 rows x 16 dims
+            bf16x8 a;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int key = 16 * half + 4 * g + (i >> 2), c = 2 * db + ((i & 3) >> 1);
+                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) s16x4*)(v + key * G::ROWB + G::slot(key, c) * 16 + (i & 1) * 8));
+                const bf16x4 y = __builtin_bit_cast(bf16x4, x);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) a[4 * half + e] = y[e];
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[nb], o[nb][db], 0, 0, 0);
+            if constexpr (TWO) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, rest[nb], o[nb][db], 0, 0, 0);
+            }
+        }
+    }
+    // first dim of the four that o[nb][x] .. hold: quad y of them, y < OB
+    __device__ __forceinline__ static int quad_dim(int y) { return 16 * y + 4 * ((threadIdx.x & 63) >> 4); }
+    __device__ __forceinline__ f32x4 quad(int nb, int y) const { return o[nb][y]; }
+};
+
+template <int D, int NB>
+struct Core<float, D, NB> {
+    typedef Geo<float, D> G;
+    static constexpr int KEYS = 16, MT = 1, OB = D / 16, QS = D / 16;
+    static constexpr int VE = D % 64 == 0 ? 4 : 2;         // dims of a lane's V read
+    f32x4 q[NB][QS];
+    f32x4 o[NB][OB];
+
+    __device__ __forceinline__ void load_q(int nb, const char* row) {
+#pragma unroll
+        for (int s = 0; s < QS; ++s) {
+            q[nb][s] = f32x4{0, 0, 0, 0};
+            if (row) q[nb][s] = *(const f32x4*)(row + (4 * s + ((threadIdx.x & 63) >> 4)) * 16);
+        }
+    }
+    __device__ __forceinline__ void scores(const lds_char* k, f32x4 (&s)[NB][MT]) const {
+        const int m = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) s[nb][0] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int st = 0; st < QS; ++st) {
+            const f32x4 a = *(const __attribute__((address_space(3))) f32x4*)(k + m * G::ROWB + G::slot(m, 4 * st + g) * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) s[nb][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], q[nb][st][e], s[nb][0], 0, 0, 0);
+        }
+    }
+    template <bool>
+    __device__ __forceinline__ void add_values(const lds_char* v, const f32x4 (&p)[NB][MT]) {
+        const int m = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+        for (int b = 0; b < OB / VE; ++b) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int key = 4 * g + i;
+                float a[VE];
+                if constexpr (VE == 4) {
+                    const f32x4 x = *(const __attribute__((address_space(3))) f32x4*)(v + key * G::ROWB + G::slot(key, 16 * b + m) * 16);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) a[e] = x[e];
+                } else {
+                    const f32x2 x = *(const __attribute__((address_space(3))) f32x2*)(v + key * G::ROWB + G::slot(key, 8 * b + (m >> 1)) * 16 + (m & 1) * 8);
+                    a[0] = x[0];
+                    a[1] = x[1];
+                }
+#pragma unroll
+                for (int e = 0; e < VE; ++e)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+                        o[nb][b * VE + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], p[nb][0][i], o[nb][b * VE + e], 0, 0, 0);
+            }
+        }
+    }
+    // o[nb][b * VE + e][i] is dim 16 VE b + VE (4 g + i) + e: four neighbours are e = 0 .. 3 of one i, or
+    // e = 0, 1 of two
+    __device__ __forceinline__ static int quad_dim(int y) {
+        const int b = y / VE, x = y % VE, g = (threadIdx.x & 63) >> 4;
+        return VE == 4 ? 64 * b + 4 * (4 * g + x) : 32 * b + 2 * (4 * g + 2 * x);
+    }
+    __device__ __forceinline__ f32x4 quad(int nb, int y) const {
+        const int b = y / VE, x = y % VE;
+        if constexpr (VE == 4) return f32x4{o[nb][4 * b][x], o[nb][4 * b + 1][x], o[nb][4 * b + 2][x], o[nb][4 * b + 3][x]};
+        else return f32x4{o[nb][2 * b][2 * x], o[nb][2 * b + 1][2 * x], o[nb][2 * b][2 * x + 1], o[nb][2 * b + 1][2 * x + 1]};
+    }
+};
+
+// The running softmax of a wavefront's columns: m the maximum of c S so far, l this lane's share of the sum.
+template <typename E, int D, int NB>
+struct Softmax {
+    typedef Core<E, D, NB> C;
+    float m[NB], l[NB];
+    __device__ __forceinline__ void start(C& core) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            m[nb] = -INFINITY;
+            l[nb] = 0.f;
+#pragma unroll
+            for (int b = 0; b < C::OB; ++b) core.o[nb][b] = f32x4{0, 0, 0, 0};
+        }
+    }
+    // scores -> weights, everything before them rescaled to the new maximum
+    __device__ __forceinline__ void step(C& core, f32x4 (&s)[NB][C::MT], float c) {
+        float top[NB];
+        bool more = false;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            float x = s[nb][0][0];
+#pragma unroll
+            for (int e = 1; e < 4 * C::MT; ++e) x = fmaxf(x, s[nb][e >> 2][e & 3]);
+            top[nb] = fmaxf(m[nb], column_max(x) * c);
+            more |= top[nb] > m[nb];
+        }
+        if (__any(more)) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const float old = top[nb] > m[nb] ? fast_exp2(m[nb] - top[nb]) : 1.f;
+                m[nb] = top[nb];
+                l[nb] *= old;
+#pragma unroll
+                for (int b = 0; b < C::OB; ++b) core.o[nb][b] *= old;
+            }
+        }
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const float base = m[nb] == -INFINITY ? 0.f : m[nb];
+#pragma unroll
+            for (int e = 0; e < 4 * C::MT; ++e) {
+                const float w = fast_exp2(fmaf(s[nb][e >> 2][e & 3], c, -base));
+                s[nb][e >> 2][e & 3] = w;
+                l[nb] += w;
+            }
+        }
+    }
+};
+
+template <typename E>
+__device__ __forceinline__ void store_quad(char* row, int dim, f32x4 x) {
+    if constexpr (sizeof(E) == 4) {
+        *(f32x4*)(row + dim * 4) = x;
+    } else {
+        bf16x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = (__bf16)x[e];
+        *(bf16x4*)(row + dim * 2) = y;
+    }
+}
+
+}  // namespace attn
+}  // namespace dip
+
+#endif  // DIP_ATTN_DEVICE_H_
