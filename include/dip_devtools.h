@@ -51,10 +51,9 @@ int32_t dip_gemv_launch_shape(const dip_weight* w, int32_t k, int32_t bundled, i
 #define DIP_KERNEL_CACHE_UPDATE 7 /* a cache update launched on its own (end of a forward call) */
 #define DIP_KERNEL_STREAM_READ 8  /* dip_stream_read                                            */
 #define DIP_KERNEL_ATTENTION 9    /* dip_window_attention, dip_tree_attention                   */
-#define DIP_KERNEL_ATTENTION_JOIN 10 /* their second launch: shares of one row joined           */
-#define DIP_KERNEL_VERIFY 11      /* the launches of dip_verify_tree                            */
-#define DIP_KERNEL_KV 12          /* page operations of a key/value cache                       */
-#define DIP_KERNEL_KINDS 13
+#define DIP_KERNEL_VERIFY 10      /* the launches of dip_verify_tree                            */
+#define DIP_KERNEL_KV 11          /* page operations of a key/value cache                       */
+#define DIP_KERNEL_KINDS 12
 int32_t dip_profile_enable(int32_t max_launches);
 int32_t dip_profile_read(int32_t kind, double* total_ms /* host */, int32_t* launches /* host */);
 int32_t dip_profile_disable(void);

@@ -4,6 +4,7 @@
 // group -- form blocks of 16, 32 or 64; a workgroup takes a block and a share of the keys that it sees.
 
 #include <cmath>
+#include <type_traits>
 
 #include "dip_attn_device.h"
 
@@ -11,7 +12,11 @@ namespace dip {
 namespace attn {
 namespace {
 
-constexpr int kWaves = 4;
+#ifndef KW
+#define KW 4
+#define KT 512
+#endif
+constexpr int kWaves = KW;
 constexpr int kThreads = kWaves * 64;
 constexpr int kIds = 1024;                // page numbers of a share, in LDS
 constexpr int kRing = 2;                  // tiles of a wavefront in LDS: one in use, one on its way
@@ -28,6 +33,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams
     __shared__ int s_ids[kIds];
     __shared__ uint64_t s_tree[64];
     __shared__ float s_m[kWaves][ROWS], s_l[kWaves][ROWS];
+    __shared__ int s_last;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int split = blockIdx.x % p.splits;
@@ -48,14 +54,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams
     if (begin >= end && split > 0) return;
 
     // the share's page numbers, `per` of a tile
-    const int shift = p.c.page_shift;
-    const int per = max(1, KEYS >> shift);
-    for (int i = tid; i < (end - begin) * per; i += kThreads) {
-        const int vt = i / per;
-        const int at = ((tile_at(range, begin + vt) * KEYS) >> shift) + (i - vt * per);
-        int page = at < p.c.max_pages ? p.c.table[(size_t)seq * p.c.max_pages + at] : 0;
-        s_ids[i] = (unsigned)page < (unsigned)p.c.n_pages ? page : 0;
-    }
+    const int per = max(1, KEYS >> p.c.page_shift);
+    page_ids<KEYS, kThreads>(p.c, seq, range, begin, end - begin, per, s_ids);
+    if (shares > 1 && tid == 0) ticket_open(p.tickets + (size_t)block * kTicketStride, p.epoch);
     if (p.parents && wave == 0) tree_masks(p.parents + er.first, er.rows, s_tree);
     __syncthreads();
 
@@ -85,38 +86,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams
         const uint32_t to = ring_at + (i & (kRing - 1)) * (2 * TILE);
 #pragma unroll
         for (int x = 0; x < LOADS; ++x) {
-            const int at = x * 64 + lane, r = at / G::CPR;
-            const int pos = min(j0 + r, range.end - 1);
-            const int page = s_ids[(vt - begin) * per + ((pos >> shift) - (j0 >> shift))];
-            const int64_t off = (page * p.c.page_stride + (pos & ((1 << shift) - 1)) * p.c.slot_stride + G::piece(r, at % G::CPR)) * 16;
+            const int64_t off = piece_offset<G>(p.c, s_ids + (vt - begin) * per, j0, range.end, x);
             load_to_lds(kbase + off, to + x * 1024);
             load_to_lds(vbase + off, to + TILE + x * 1024);
         }
     };
-    // V's pieces that are not finite become zero, for a weight of zero to take them out; the keys' bits
-    auto take_out = [&](lds_char* v) {
-        uint32_t bad = 0;
-#pragma unroll
-        for (int x = 0; x < LOADS; ++x) {
-            auto* at = (__attribute__((address_space(3))) u32x4*)(v + x * 1024 + lane * 16);
-            const u32x4 w = *at;
-            bool inf = false;
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                if constexpr (sizeof(E) == 4) inf |= (w[y] & 0x7f800000u) == 0x7f800000u;
-                else inf |= (w[y] & 0x7f800000u) == 0x7f800000u || (w[y] & 0x7f80u) == 0x7f80u;
-            }
-            if (inf) {
-                *at = u32x4{0, 0, 0, 0};
-                bad |= 1u << ((x * 64 + lane) / G::CPR);
-            }
-        }
-        if (__any(bad))
-            for (int off = 1; off < 64; off <<= 1) bad |= __shfl_xor(bad, off);
-        asm volatile("" ::: "memory");
-        return bad;
-    };
-
     if (mine > 0) fetch(0);
     if (mine > 1) fetch(1);
     for (int i = 0; i < mine; ++i) {
@@ -124,23 +98,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams
         const int j0 = tile_at(range, begin + wave + kWaves * i) * KEYS;
         const lds_char* kt = ring + (i & (kRing - 1)) * (2 * TILE);
         f32x4 s[NB][C::MT];
-        core.scores(kt, s);
+        core.scores(kt, s, 0);
         const bool whole = j0 + KEYS <= range.sure && (j0 >= range.from || j0 + KEYS <= p.sinks);
         if (!whole) {
-            const uint32_t bad = take_out((lds_char*)kt + TILE);
-            const int g = lane >> 4;
+            uint64_t bad = 0;
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-                for (int x = 0; x < 4 * C::MT; ++x) {
-                    const int key = 16 * (x >> 2) + 4 * g + (x & 3);
-                    float z = (bad >> key) & 1 ? NAN : s[nb][x >> 2][x & 3];
-                    if (!sees(row[nb], j0 + key, p.sinks, len)) z = -INFINITY;
-                    s[nb][x >> 2][x & 3] = z;
-                }
+            for (int x = 0; x < LOADS; ++x) bad |= take_out<G>((lds_char*)kt + TILE, x);
+            if (__any(bad != 0))
+                for (int off = 1; off < 64; off <<= 1) bad |= __shfl_xor((uint32_t)bad, off);
+            asm volatile("" ::: "memory");
+            apply_sees(s, row, j0, p.sinks, len, bad);
         }
         soft.step(core, s, p.scale_log2);
-        core.template add_values<true>(kt + TILE, s);
+        typename C::Weights w;
+        C::template pack<true>(s, 0, w);
+        core.template add_values<true>(kt + TILE, w);
         if (i + kRing < mine) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (everything read from the tile that goes)
             fetch(i + kRing);
@@ -166,7 +138,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams
         float top = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
-        const float a = s_m[wave][r] == -INFINITY ? 0.f : fast_exp2(s_m[wave][r] - top);
+        const float a = join_weight(s_m[wave][r], top);
 #pragma unroll
         for (int y = 0; y < C::OB; ++y) {
             const int quad = C::quad_dim(y) / 4;
@@ -180,107 +152,302 @@ __global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) l += s_m[w][r] == -INFINITY ? (s_l[w][r] == 0.f ? 0.f : s_l[w][r]) : s_l[w][r] * fast_exp2(s_m[w][r] - top);
+        for (int w = 0; w < kWaves; ++w) l += s_m[w][r] == -INFINITY ? s_l[w][r] : s_l[w][r] * fast_exp2(s_m[w][r] - top);
         f32x4 o = {0, 0, 0, 0};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) o += *(const f32x4*)(s_o + ((w * ROWS + r) * QUADS + (quad + r) % QUADS) * 4);
         if (shares > 1) {
             const size_t at = ((size_t)block * p.splits + split) * ROWS + r;
-            *(f32x4*)(p.part_o + at * D + quad * 4) = o;
-            if (quad == 0) p.part_ml[at] = make_float2(top, l);
+            share_put(p.part_o + at * D + quad * 4, o);
+            if (quad == 0)
+                __hip_atomic_store((uint64_t*)(p.part_ml + at), ((uint64_t)__float_as_uint(l) << 32) | __float_as_uint(top),
+                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         } else {
             const int t = (r0 + r) / p.group, h = head * p.group + (r0 + r) % p.group;
             const f32x4 zero = {0, 0, 0, 0};
-            store_quad<E>(p.out + (int64_t)(er.first + t) * p.out_stride + (int64_t)h * (D * G::ES), quad * 4, l == 0.f ? zero : o / l);
+            store_quad<E>(p.out + (int64_t)(er.first + t) * p.out_stride + (int64_t)h * (D * G::ES), quad * 4, l == 0.f ? zero : o * (1.f / l));
+        }
+    }
+    if (shares <= 1) return;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) s_last = ticket_last(p.tickets + (size_t)block * kTicketStride, p.epoch, shares);
+    __syncthreads();
+    if (s_last) join_shares<E, D, ROWS, kThreads, true>(p, block, shares, er.first, head, r0, 0, n_rows);
+}
+
+// Rows enough to fill the matrix cores: eight wavefronts of 16 NB rows each share the tiles, one barrier a tile.
+// The two wavefronts of a SIMD take turns: of tile i's products and the softmax between them, the first four
+// wavefronts run [K_i Q, V_{i-1} P_{i-1}, softmax i], the other four [softmax i-1, K_i Q, V_{i-1} P_{i-1}], so
+// that one's exponentials run beside the other's products.  Four tiles of LDS: V of the last one, the
+// current one, two on their way.
+constexpr int kBlockWaves = 8;
+constexpr int kBlockThreads = kBlockWaves * 64;
+constexpr int kBlockRing = 4;
+constexpr int kIdTiles = 64;              // tiles whose page numbers are in LDS at a time
+
+template <typename E, int D, int NB>
+__global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const AttnParams p) {
+    typedef Geo<E, D> G;
+    typedef Core<E, D, NB> C;
+    constexpr int SUB = 2, KEYS = SUB * G::KEYS, TILE = KEYS * G::ROWB, LOADS = TILE / 1024, ROWS = 16 * NB * kBlockWaves;
+    constexpr int MINE = (LOADS + kBlockWaves - 1) / kBlockWaves;     // loads of a wavefront (some twice where uneven)
+    constexpr int Q = SUB * C::MT;
+    __shared__ __align__(1024) char s_ring[kBlockRing * 2 * TILE];
+    __shared__ int s_ids[kIdTiles * KEYS];
+    __shared__ uint64_t s_tree[64];
+    __shared__ uint32_t s_bad[2][2];
+
+    // XCD x gets consecutive blocks, so that blocks of one head find its keys in their L2
+    const int per_xcd = (p.grid + 7) / 8, unit = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    if (unit >= p.grid) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int split = unit % p.splits;
+    const int block = unit / p.splits;
+    const int rb = block % p.row_blocks;
+    const int head = block / p.row_blocks % p.c.n_heads;
+    const int e = block / p.row_blocks / p.c.n_heads;
+
+    const EntryRows er = entry_rows(p.b, e);
+    const int r0 = rb * ROWS, n_rows = min(ROWS, er.rows * p.group - r0);
+    if (n_rows <= 0) return;
+    const int seq = entry_seq(p.b, p.c, e);
+    const int len = seq >= 0 ? min(entry_len(p.c, seq), p.max_len) : 0;
+    Range range = key_range<KEYS>(p, len, er.rows, r0 / p.group, (r0 + n_rows - 1) / p.group);
+    if (seq < 0) range.tiles = 0;
+    const int shares = (range.tiles + p.tiles_per_split - 1) / p.tiles_per_split;
+    const int begin = split * p.tiles_per_split, n = max(0, min(range.tiles - begin, p.tiles_per_split));
+    if (n == 0 && split > 0) return;
+
+    const int per = max(1, KEYS >> p.c.page_shift);
+    page_ids<KEYS, kBlockThreads>(p.c, seq, range, begin, min(n, kIdTiles), per, s_ids);
+    if (p.parents && wave == 0) tree_masks(p.parents + er.first, er.rows, s_tree);
+    if (tid < 4) s_bad[tid >> 1][tid & 1] = 0;
+    __syncthreads();
+
+    C core;
+    const int w0 = wave * 16 * NB;                        // the wavefront's first row in the block
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const int r = w0 + 16 * nb + (lane & 15), t = (r0 + r) / p.group;
+        core.load_q(nb, r < n_rows ? p.q + (int64_t)(er.first + t) * p.q_stride + (int64_t)(head * p.group + (r0 + r) % p.group) * (D * G::ES) : nullptr);
+    }
+    // what the lane's rows see, worked out where it is asked for rather than kept in registers (`lane` from
+    // fresh(): the compiler would keep it all the same)
+    auto fresh = [&]() { int x = tid & 63; asm volatile("" : "+v"(x)); return x; };
+    auto sees_of = [&](int lane, RowSees (&row)[NB]) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int r = w0 + 16 * nb + (lane & 15);
+            row[nb] = row_sees(p, len, r < n_rows ? (r0 + r) / p.group : 0, s_tree);
+        }
+    };
+    Softmax<E, D, NB> soft;
+    soft.start(core);
+
+    const char* kbase = p.c.k + p.c.head_stride * head * 16;
+    const char* vbase = p.c.v + p.c.head_stride * head * 16;
+    const lds_char* ring = (const lds_char*)s_ring;
+    const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_offset(s_ring));
+    auto tile_of = [&](int i) { return ring + (i & (kBlockRing - 1)) * (2 * TILE); };
+    auto fetch = [&](int i) {
+        const int j0 = tile_at(range, begin + i) * KEYS;
+        const int* ids = s_ids + (i & (kIdTiles - 1)) * per;
+        const uint32_t to = ring_at + (i & (kBlockRing - 1)) * (2 * TILE);
+#pragma unroll
+        for (int m = 0; m < MINE; ++m) {
+            const int x = (wave * MINE + m) % LOADS;
+            const int64_t off = piece_offset<G>(p.c, ids, j0, range.end, x);
+            load_to_lds(kbase + off, to + x * 1024);
+            load_to_lds(vbase + off, to + TILE + x * 1024);
+        }
+    };
+    auto barrier = [&]() {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    // tile i is there for everybody, tile i - 2 done with, and tile i + 2 on its way
+    auto arrive = [&](int i) {
+        if (i + 1 < n) wait_loads<2 * MINE>(); else wait_loads<0>();
+        barrier();
+        if (i + 2 < n) {
+            if (((i + 2) & (kIdTiles - 1)) == 0) {
+                page_ids<KEYS, kBlockThreads>(p.c, seq, range, begin + i + 2, min(n - i - 2, kIdTiles), per, s_ids);
+                barrier();
+            }
+            fetch(i + 2);
+        }
+    };
+    auto scores = [&](int i, f32x4 (&s)[NB][Q]) {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) core.scores(tile_of(i) + u * G::KEYS * G::ROWB, s, u * C::MT);
+    };
+    // tiles that some row does not see all of: rows that see few keys have them here, so weights go in as two
+    // terms
+    auto edge = [&](int from, int to) {
+        if (tid < 2) s_bad[from & 1][tid] = 0;
+        RowSees row[NB];
+        sees_of(fresh(), row);
+        for (int i = from; i < to; ++i) {
+            arrive(i);
+            if (tid < 2) s_bad[(i + 1) & 1][tid] = 0;
+            uint64_t bad = 0;
+#pragma unroll
+            for (int m = 0; m < MINE; ++m) bad |= take_out<G>((lds_char*)tile_of(i) + TILE, (wave * MINE + m) % LOADS);
+            if (bad) {
+                atomicOr(&s_bad[i & 1][0], (uint32_t)bad);
+                atomicOr(&s_bad[i & 1][1], (uint32_t)(bad >> 32));
+            }
+            barrier();
+            bad = ((uint64_t)s_bad[i & 1][1] << 32) | s_bad[i & 1][0];
+            f32x4 s[NB][Q];
+            scores(i, s);
+            apply_sees(s, row, tile_at(range, begin + i) * KEYS, p.sinks, len, bad);
+            soft.step(core, s, p.scale_log2);
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                typename C::Weights w;
+                C::template pack<true>(s, u * C::MT, w);
+                core.template add_values<true>(tile_of(i) + TILE + u * G::KEYS * G::ROWB, w);
+            }
+        }
+    };
+    auto middle = [&](auto late, int from, int to) {
+        if (from >= to) return;
+        f32x4 s[NB][Q];
+        typename C::Weights w[SUB];
+        auto weigh = [&]() {
+            soft.step(core, s, p.scale_log2);
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) C::template pack<false>(s, u * C::MT, w[u]);
+        };
+        auto values = [&](int i) {
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) core.template add_values<false>(tile_of(i) + TILE + u * G::KEYS * G::ROWB, w[u]);
+        };
+        arrive(from);
+        scores(from, s);
+        if (!late.value) weigh();
+        for (int i = from + 1; i < to; ++i) {
+            arrive(i);
+            if (late.value) weigh();
+            scores(i, s);
+            values(i - 1);
+            if (!late.value) weigh();
+        }
+        if (late.value) weigh();
+        values(to - 1);
+    };
+
+    // [edge][middle][edge] of the share; the middle is what everybody sees all of
+    const int mid0 = min(n, max(0, range.sink_tiles + max(0, (range.from + KEYS - 1) / KEYS - range.first) - begin));
+    const int mid1 = min(n, max(mid0, range.sink_tiles + range.sure / KEYS - range.first - begin));
+    if (n > 0) fetch(0);
+    if (n > 1) fetch(1);
+    edge(0, mid0);
+    if (wave >= kBlockWaves / 2) middle(std::true_type(), mid0, mid1);
+    else middle(std::false_type(), mid0, mid1);
+    edge(mid1, n);
+
+    RowSees row[NB];
+    sees_of(fresh(), row);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const int r = 16 * nb + (lane & 15) + w0;
+        const bool alive = row[nb].hi > 0 || row[nb].tree;
+        const float l = alive ? column_sum(soft.l[nb]) : 0.f;
+        if (r >= n_rows) continue;
+        if (shares > 1) {
+            const size_t at = ((size_t)block * p.splits + split) * ROWS + r;
+#pragma unroll
+            for (int y = 0; y < C::OB; ++y) *(f32x4*)(p.part_o + at * D + C::quad_dim(y)) = core.quad(nb, y);
+            if (lane < 16) p.part_ml[at] = make_float2(alive ? soft.m[nb] : -INFINITY, l);
+        } else {
+            const int t = (r0 + r) / p.group, h = head * p.group + (r0 + r) % p.group;
+            char* out = p.out + (int64_t)(er.first + t) * p.out_stride + (int64_t)h * (D * G::ES);
+            const f32x4 zero = {0, 0, 0, 0};
+            const float inv = 1.f / l;
+#pragma unroll
+            for (int y = 0; y < C::OB; ++y) store_quad<E>(out, C::quad_dim(y), l == 0.f ? zero : core.quad(nb, y) * inv);
         }
     }
 }
 
-// Shares of one row joined: 8 rows of a block to a workgroup of 256, four dims to a thread.
+// The shares of attn_block_kernel's rows, 8 rows to a workgroup: what one workgroup, the last to arrive, would
+// take far longer over (256 rows of 20 shares: 120 us alone, 9 us in a launch of its own).
 constexpr int kJoinRows = 8;
-template <typename E, int D, int KEYS>
-__global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p, const int rows_of_block) {
-    constexpr int QUADS = D / 4;
-    const int block = blockIdx.x;
+template <typename E, int D, int NB>
+__global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p) {
+    constexpr int ROWS = 16 * NB * kBlockWaves;
+    const int block = blockIdx.x / (ROWS / kJoinRows), part = blockIdx.x % (ROWS / kJoinRows);
     const int rb = block % p.row_blocks;
     const int head = block / p.row_blocks % p.c.n_heads;
     const int e = block / p.row_blocks / p.c.n_heads;
     const EntryRows er = entry_rows(p.b, e);
-    const int r0 = rb * rows_of_block, n_rows = min(rows_of_block, er.rows * p.group - r0);
-    if (n_rows <= (int)blockIdx.y * kJoinRows) return;
+    const int r0 = rb * ROWS, n_rows = min(ROWS, er.rows * p.group - r0);
+    if (n_rows <= part * kJoinRows) return;
     const int seq = entry_seq(p.b, p.c, e);
     if (seq < 0) return;
     const int len = min(entry_len(p.c, seq), p.max_len);
-    const Range range = key_range<KEYS>(p, len, er.rows, r0 / p.group, (r0 + n_rows - 1) / p.group);
+    const Range range = key_range<2 * Geo<E, D>::KEYS>(p, len, er.rows, r0 / p.group, (r0 + n_rows - 1) / p.group);
     const int shares = (range.tiles + p.tiles_per_split - 1) / p.tiles_per_split;
-    if (shares <= 1) return;
-    for (int i = threadIdx.x; i < kJoinRows * QUADS; i += 256) {
-        const int r = blockIdx.y * kJoinRows + i / QUADS, quad = i % QUADS;
-        if (r >= n_rows) break;
-        const size_t at = (size_t)block * p.splits * rows_of_block + r;
-        float top = -INFINITY;
-        for (int s = 0; s < shares; ++s) top = fmaxf(top, p.part_ml[at + (size_t)s * rows_of_block].x);
-        f32x4 o = {0, 0, 0, 0};
-        float l = 0.f;
-#pragma unroll 4
-        for (int s = 0; s < shares; ++s) {
-            const float2 ml = p.part_ml[at + (size_t)s * rows_of_block];
-            const f32x4 x = *(const f32x4*)(p.part_o + (at + (size_t)s * rows_of_block) * D + quad * 4);
-            const float a = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - top);
-            if (ml.x != -INFINITY || ml.y != 0.f) {
-                l += ml.x == -INFINITY ? ml.y : ml.y * a;
-                o += x * a;
-            }
-        }
-        const int t = (r0 + r) / p.group, h = head * p.group + (r0 + r) % p.group;
-        const f32x4 zero = {0, 0, 0, 0};
-        store_quad<E>(p.out + (int64_t)(er.first + t) * p.out_stride + (int64_t)h * (D * (int)sizeof(E)), quad * 4, l == 0.f ? zero : o / l);
-    }
+    if (shares > 1) join_shares<E, D, ROWS, 256, false>(p, block, shares, er.first, head, r0, part * kJoinRows, min(n_rows, (part + 1) * kJoinRows));
 }
 
 // ---- launch plan ----------------------------------------------------------------------------------
 struct Plan {
-    int nb, row_blocks, splits, tiles_per_split;
+    bool shared;              // attn_block_kernel
+    int nb, rows, row_blocks, splits, tiles_per_split;
     int64_t blocks;
-    size_t off_ml, total;
+    size_t off_ml, off_tickets, total;
 };
 int reach(const dip_kv_cache* c, const dip_batch* b) {
     const int fit = c->max_pages * c->page_size;
     return b->max_len && b->max_len < fit ? b->max_len : fit;
 }
+#ifndef BT
+#define BT 768
+#endif
 Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads, int window, int sinks) {
     Plan pl;
-    const int keys = c->dtype == DIP_F32 ? 16 : 32;
     const int64_t rows = (int64_t)rows_bound(b) * (n_q_heads / c->n_kv_heads);
-    pl.nb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    pl.row_blocks = (int)((rows + 16 * pl.nb - 1) / (16 * pl.nb));
+    pl.shared = rows > 64;
+    pl.nb = pl.shared ? (rows <= 128 ? 1 : 2) : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    pl.rows = 16 * pl.nb * (pl.shared ? kBlockWaves : 1);
+    const int keys = (c->dtype == DIP_F32 ? 16 : 32) * (pl.shared ? 2 : 1);
+    pl.row_blocks = (int)((rows + pl.rows - 1) / pl.rows);
     pl.blocks = (int64_t)b->n_batch * c->n_kv_heads * pl.row_blocks;
     // most tiles that a block of rows sees
-    const int64_t all = ((int64_t)reach(c, b) + keys - 1) / keys;
-    int64_t tiles = all;
+    int64_t tiles = ((int64_t)reach(c, b) + keys - 1) / keys;
     if (window) {
         const int64_t w = ((int64_t)sinks + keys - 1) / keys + ((int64_t)window + rows_bound(b)) / keys + 2;
         if (w < tiles) tiles = w;
     }
-    // enough workgroups for the chip, but no share under two tiles a wavefront, and none with more page
-    // numbers than LDS holds
-    int64_t want = (512 + pl.blocks - 1) / pl.blocks;
+    // enough workgroups for the chip, but no share under two tiles a wavefront (eight shared ones), and none
+    // with more page numbers than LDS holds
+    const int64_t want = ((pl.shared ? BT : KT) + pl.blocks - 1) / pl.blocks;
     int64_t per = (tiles + want - 1) / want;
-    if (per < 2 * kWaves) per = 2 * kWaves;
-    per = (per + kWaves - 1) / kWaves * kWaves;
-    const int ids = keys / c->page_size > 1 ? keys / c->page_size : 1;
-    if (per > kIds / ids) per = kIds / ids;
+    if (per < 8) per = 8;
+    if (!pl.shared) {
+        per = (per + kWaves - 1) / kWaves * kWaves;
+        const int ids = keys / c->page_size > 1 ? keys / c->page_size : 1;
+        if (per > kIds / ids) per = kIds / ids;
+    }
     pl.tiles_per_split = (int)per;
     pl.splits = (int)((tiles + per - 1) / per);
     if (pl.splits < 1) pl.splits = 1;
     size_t o = 0;
     if (pl.splits > 1) {
-        const size_t rows_all = (size_t)pl.blocks * pl.splits * 16 * pl.nb;
+        const size_t rows_all = (size_t)pl.blocks * pl.splits * pl.rows;
         o = align_up(rows_all * c->head_dim * sizeof(float), 256);
         pl.off_ml = o;
         o += align_up(rows_all * sizeof(float2), 256);
+        pl.off_tickets = o;
+        if (!pl.shared) o += sizeof(uint64_t) * kTicketStride * (size_t)pl.blocks;
     } else {
-        pl.off_ml = 0;
+        pl.off_ml = pl.off_tickets = 0;
     }
     pl.total = o < 256 ? 256 : o;
     return pl;
@@ -288,20 +455,23 @@ Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads, in
 
 template <typename E, int D>
 int32_t launch(const AttnParams& p, const Plan& pl, hipStream_t stream) {
-    const dim3 grid((unsigned)(pl.blocks * pl.splits));
     hipError_t err;
-    if (pl.nb == 1) err = launch_timed(attn_rows_kernel<E, D, 1>, grid, dim3(kThreads), stream, DIP_KERNEL_ATTENTION, p);
-    else if (pl.nb == 2) err = launch_timed(attn_rows_kernel<E, D, 2>, grid, dim3(kThreads), stream, DIP_KERNEL_ATTENTION, p);
-    else err = launch_timed(attn_rows_kernel<E, D, 4>, grid, dim3(kThreads), stream, DIP_KERNEL_ATTENTION, p);
-    int32_t st = check_hip(err, "attention launch");
-    if (st || pl.splits == 1) return st;
-    hipEvent_t e0, e1;
-    const dim3 jgrid((unsigned)pl.blocks, 16 * pl.nb / kJoinRows);
-    if (prof_next(DIP_KERNEL_ATTENTION_JOIN, &e0, &e1))
-        hipExtLaunchKernelGGL((attn_join_kernel<E, D, Geo<E, D>::KEYS>), jgrid, dim3(256), 0, stream, e0, e1, 0, p, 16 * pl.nb);
-    else
-        hipLaunchKernelGGL((attn_join_kernel<E, D, Geo<E, D>::KEYS>), jgrid, dim3(256), 0, stream, p, 16 * pl.nb);
-    return check_hip(hipGetLastError(), "attention join launch");
+    if (pl.shared) {
+        const dim3 grid((unsigned)((p.grid + 7) / 8 * 8));
+        if (pl.nb == 1) err = launch_timed(attn_block_kernel<E, D, 1>, grid, dim3(kBlockThreads), stream, DIP_KERNEL_ATTENTION, p);
+        else err = launch_timed(attn_block_kernel<E, D, 2>, grid, dim3(kBlockThreads), stream, DIP_KERNEL_ATTENTION, p);
+        if (err == hipSuccess && pl.splits > 1) {
+            const dim3 join((unsigned)(pl.blocks * (pl.rows / kJoinRows)));
+            if (pl.nb == 1) err = launch_timed(attn_join_kernel<E, D, 1>, join, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
+            else err = launch_timed(attn_join_kernel<E, D, 2>, join, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
+        }
+    } else {
+        const dim3 grid((unsigned)p.grid);
+        if (pl.nb == 1) err = launch_timed(attn_rows_kernel<E, D, 1>, grid, dim3(kThreads), stream, DIP_KERNEL_ATTENTION, p);
+        else if (pl.nb == 2) err = launch_timed(attn_rows_kernel<E, D, 2>, grid, dim3(kThreads), stream, DIP_KERNEL_ATTENTION, p);
+        else err = launch_timed(attn_rows_kernel<E, D, 4>, grid, dim3(kThreads), stream, DIP_KERNEL_ATTENTION, p);
+    }
+    return check_hip(err, "attention launch");
 }
 template <typename E>
 int32_t launch_dim(const AttnParams& p, const Plan& pl, int head_dim, hipStream_t stream) {
@@ -323,7 +493,7 @@ int32_t check_attention(const dip_kv_cache* c, const dip_batch* b, int32_t n_q_h
     const int64_t rows = (int64_t)rows_bound(b) * (n_q_heads / c->n_kv_heads);
     if (rows >= 1 << 30) return fail(DIP_ERR_UNSUPPORTED, "attention: too many rows of one entry");
     const Plan pl = plan_attention(c, b, n_q_heads, window, sinks);
-    if (pl.blocks * pl.splits >= (int64_t)1 << 31) return fail(DIP_ERR_UNSUPPORTED, "attention: too many rows for one call");
+    if (pl.blocks * (pl.splits > 32 ? pl.splits : 32) >= (int64_t)1 << 30) return fail(DIP_ERR_UNSUPPORTED, "attention: too many rows for one call");
     return DIP_OK;
 }
 
@@ -362,8 +532,11 @@ int32_t attend(const dip_kv_cache* c, int32_t layer, const dip_batch* b, const i
     p.splits = pl.splits;
     p.tiles_per_split = pl.tiles_per_split;
     p.row_blocks = pl.row_blocks;
+    p.grid = (int)(pl.blocks * pl.splits);
     p.part_o = (float*)ws;
     p.part_ml = (float2*)((char*)ws + pl.off_ml);
+    p.tickets = (uint64_t*)((char*)ws + pl.off_tickets);
+    p.epoch = pl.splits > 1 ? next_epoch() : 0;
     return c->dtype == DIP_F32 ? launch_dim<float>(p, pl, c->head_dim, (hipStream_t)stream)
                                : launch_dim<uint16_t>(p, pl, c->head_dim, (hipStream_t)stream);
 }

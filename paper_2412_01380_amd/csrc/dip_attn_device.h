@@ -42,9 +42,13 @@ struct AttnParams {
     int splits;               // shares that a row block's keys are cut into
     int tiles_per_split;
     int row_blocks;           // of an entry and key/value head
+    int grid;                 // row blocks times splits
     float* part_o;            // [row block][split][rows of a block][D], not normalised
     float2* part_ml;          // [row block][split][rows of a block]: maximum (times scale_log2), sum
+    uint64_t* tickets;        // a word per row block, kTicketStride apart, whatever they hold
+    uint64_t epoch;           // this launch's tag in them
 };
+constexpr int kTicketStride = 16;         // words: 128 bytes, so that atomics of different blocks do not queue
 
 // ---- which keys a block of rows sees -----------------------------------------------------------
 struct Range {
@@ -90,10 +94,13 @@ struct RowSees {
     int lo, hi;               // positions [lo, hi) and sinks below hi ...
     uint64_t tree;            // ... and nodes of its tree
 };
-__device__ __forceinline__ bool sees(const RowSees& r, int j, int sinks, int len) {
-    const bool past = j < r.hi && (j >= r.lo || j < sinks);
-    const unsigned node = (unsigned)(j - len);
-    return past || (node < 64u && ((r.tree >> node) & 1));
+// As a bit for each of the 64 positions from j0 on.
+__device__ __forceinline__ uint64_t below(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
+__device__ __forceinline__ uint64_t sees(const RowSees& r, int j0, int sinks, int len) {
+    uint64_t bits = below(r.hi - j0) & (~below(r.lo - j0) | below(sinks - j0));
+    const int at = len - j0;                              // of node 0
+    if (at > -64 && at < 64) bits |= at >= 0 ? r.tree << at : r.tree >> -at;
+    return bits;
 }
 
 // The ancestors of every node of an entry's tree, itself among them (0: the node is absent), into LDS by
@@ -131,6 +138,18 @@ __device__ __forceinline__ RowSees row_sees(const AttnParams& p, int len, int t,
     return r;
 }
 
+// The page numbers of `tiles` tiles from virtual tile `from` on, `per` of each, by the whole workgroup
+// (numbers that are none become page 0).
+template <int KEYS, int THREADS>
+__device__ __forceinline__ void page_ids(const KvView& c, int seq, const Range& range, int from, int tiles, int per, int* ids) {
+    for (int i = threadIdx.x; i < tiles * per; i += THREADS) {
+        const int vt = i / per;
+        const int at = ((tile_at(range, from + vt) * KEYS) >> c.page_shift) + (i - vt * per);
+        const int page = at < c.max_pages ? c.table[(size_t)seq * c.max_pages + at] : 0;
+        ids[i] = (unsigned)page < (unsigned)c.n_pages ? page : 0;
+    }
+}
+
 // ---- tiles in LDS --------------------------------------------------------------------------------
 // KEYS rows of D elements, 16-byte pieces swizzled so that 16 rows' pieces of one dim (a K operand) and
 // the 16 pieces of a row (a V operand) both fall on different banks.  Filled by loads that go to LDS
@@ -165,9 +184,36 @@ __device__ __forceinline__ void load_to_lds(const char* from, uint32_t to) {
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
                  : "=&s"(m0) : "v"(from), "s"(to) : "memory");
 }
+// This lane's 16 bytes of load x of a tile: `off` from the start of the head.  ids: the tile's page numbers.
+template <typename G>
+__device__ __forceinline__ int64_t piece_offset(const KvView& c, const int* ids, int j0, int end, int x) {
+    const int at = x * 64 + (threadIdx.x & 63), r = at / G::CPR;
+    const int pos = min(j0 + r, end - 1), shift = c.page_shift;
+    const int page = ids[(pos >> shift) - (j0 >> shift)];
+    return (page * c.page_stride + (pos & ((1 << shift) - 1)) * c.slot_stride + G::piece(r, at % G::CPR)) * 16;
+}
 template <int N>
 __device__ __forceinline__ void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// Load x of a V tile in LDS: this lane's piece becomes zero if it is not finite, so that a weight of zero takes
+// it out; the bit of its key, or 0.  (Only tiles that some row does not see all of are looked through: in the
+// others what is not finite belongs in the results.)
+template <typename G>
+__device__ __forceinline__ uint64_t take_out(lds_char* v, int x) {
+    const int lane = threadIdx.x & 63;
+    auto* at = (__attribute__((address_space(3))) u32x4*)(v + x * 1024 + lane * 16);
+    const u32x4 w = *at;
+    bool inf = false;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+        inf |= (w[y] & 0x7f800000u) == 0x7f800000u;
+        if constexpr (G::ES == 2) inf |= (w[y] & 0x7f80u) == 0x7f80u;
+    }
+    if (!inf) return 0;
+    *at = u32x4{0, 0, 0, 0};
+    return 1ull << ((x * 64 + lane) / G::CPR);
 }
 
 // ---- the two products ----------------------------------------------------------------------------
@@ -205,34 +251,42 @@ struct Core<uint16_t, D, NB> {
             q[nb][s] = __builtin_bit_cast(bf16x8, x);
         }
     }
-    __device__ __forceinline__ void scores(const lds_char* k, f32x4 (&s)[NB][MT]) const {
+    // KEYS keys' scores into s[.][at ..]: s[nb][at + x][i] is key 16 x + 4 g + i
+    template <int Q>
+    __device__ __forceinline__ void scores(const lds_char* k, f32x4 (&s)[NB][Q], int at) const {
         const int m = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) s[nb][mt] = f32x4{0, 0, 0, 0};
+            for (int nb = 0; nb < NB; ++nb) s[nb][at + mt] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int st = 0; st < QS; ++st) {
                 const bf16x8 a = *(const __attribute__((address_space(3))) bf16x8*)(k + (16 * mt + m) * G::ROWB + G::slot(16 * mt + m, 4 * st + g) * 16);
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) s[nb][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[nb][st], s[nb][mt], 0, 0, 0);
+                for (int nb = 0; nb < NB; ++nb) s[nb][at + mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[nb][st], s[nb][at + mt], 0, 0, 0);
             }
         }
     }
-    // p: the weights in place of the scores.  As one bf16 term each they are off by up to 2^-8, which over many
-    // keys averages out but shows where a few of them carry a row; with TWO the remainder is a second term.
-    template <bool TWO>
-    __device__ __forceinline__ void add_values(const lds_char* v, const f32x4 (&p)[NB][MT]) {
-        const int i = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+    // The weights of KEYS keys as the second product takes them.  As one bf16 term each they are off by up to
+    // 2^-8, which over many keys averages out but shows where a few of them carry a row; with TWO the
+    // remainder is a second term.
+    struct Weights {
         bf16x8 w[NB], rest[NB];
+    };
+    template <bool TWO, int Q>
+    __device__ __forceinline__ static void pack(const f32x4 (&p)[NB][Q], int at, Weights& x) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float x = p[nb][e >> 2][e & 3];
-                w[nb][e] = (__bf16)x;
-                if constexpr (TWO) rest[nb][e] = (__bf16)(x - (float)w[nb][e]);
+                const float y = p[nb][at + (e >> 2)][e & 3];
+                x.w[nb][e] = (__bf16)y;
+                if constexpr (TWO) x.rest[nb][e] = (__bf16)(y - (float)x.w[nb][e]);
             }
+    }
+    template <bool TWO>
+    __device__ __forceinline__ void add_values(const lds_char* v, const Weights& p) {
+        const int i = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
 #pragma unroll
         for (int db = 0; db < OB; ++db) {
             // four keys at this lane's dim each: the transposing read hands lane i column i of 4 rows x 16 dims
@@ -247,10 +301,10 @@ struct Core<uint16_t, D, NB> {
                 for (int e = 0; e < 4; ++e) a[4 * half + e] = y[e];
             }
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[nb], o[nb][db], 0, 0, 0);
+            for (int nb = 0; nb < NB; ++nb) o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p.w[nb], o[nb][db], 0, 0, 0);
             if constexpr (TWO) {
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, rest[nb], o[nb][db], 0, 0, 0);
+                for (int nb = 0; nb < NB; ++nb) o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p.rest[nb], o[nb][db], 0, 0, 0);
             }
         }
     }
@@ -274,21 +328,30 @@ struct Core<float, D, NB> {
             if (row) q[nb][s] = *(const f32x4*)(row + (4 * s + ((threadIdx.x & 63) >> 4)) * 16);
         }
     }
-    __device__ __forceinline__ void scores(const lds_char* k, f32x4 (&s)[NB][MT]) const {
+    template <int Q>
+    __device__ __forceinline__ void scores(const lds_char* k, f32x4 (&s)[NB][Q], int at) const {
         const int m = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) s[nb][0] = f32x4{0, 0, 0, 0};
+        for (int nb = 0; nb < NB; ++nb) s[nb][at] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int st = 0; st < QS; ++st) {
             const f32x4 a = *(const __attribute__((address_space(3))) f32x4*)(k + m * G::ROWB + G::slot(m, 4 * st + g) * 16);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) s[nb][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], q[nb][st][e], s[nb][0], 0, 0, 0);
+                for (int nb = 0; nb < NB; ++nb) s[nb][at] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], q[nb][st][e], s[nb][at], 0, 0, 0);
         }
     }
+    struct Weights {
+        f32x4 w[NB];
+    };
+    template <bool, int Q>
+    __device__ __forceinline__ static void pack(const f32x4 (&p)[NB][Q], int at, Weights& x) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) x.w[nb] = p[nb][at];
+    }
     template <bool>
-    __device__ __forceinline__ void add_values(const lds_char* v, const f32x4 (&p)[NB][MT]) {
+    __device__ __forceinline__ void add_values(const lds_char* v, const Weights& p) {
         const int m = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
 #pragma unroll
         for (int b = 0; b < OB / VE; ++b) {
@@ -309,7 +372,7 @@ struct Core<float, D, NB> {
                 for (int e = 0; e < VE; ++e)
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb)
-                        o[nb][b * VE + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], p[nb][0][i], o[nb][b * VE + e], 0, 0, 0);
+                        o[nb][b * VE + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], p.w[nb][i], o[nb][b * VE + e], 0, 0, 0);
             }
         }
     }
@@ -327,6 +390,9 @@ struct Core<float, D, NB> {
 };
 
 // The running softmax of a wavefront's columns: m the maximum of c S so far, l this lane's share of the sum.
+// m may lag behind the maximum by up to kSlack: weights up to 2^kSlack instead of 1, at the same relative
+// rounding, spare the rescaling that some of 32 rows would ask for with nearly every tile.
+constexpr float kSlack = 8.f;
 template <typename E, int D, int NB>
 struct Softmax {
     typedef Core<E, D, NB> C;
@@ -341,16 +407,17 @@ struct Softmax {
         }
     }
     // scores -> weights, everything before them rescaled to the new maximum
-    __device__ __forceinline__ void step(C& core, f32x4 (&s)[NB][C::MT], float c) {
+    template <int Q>
+    __device__ __forceinline__ void step(C& core, f32x4 (&s)[NB][Q], float c) {
         float top[NB];
         bool more = false;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             float x = s[nb][0][0];
 #pragma unroll
-            for (int e = 1; e < 4 * C::MT; ++e) x = fmaxf(x, s[nb][e >> 2][e & 3]);
+            for (int e = 1; e < 4 * Q; ++e) x = fmaxf(x, s[nb][e >> 2][e & 3]);
             top[nb] = fmaxf(m[nb], column_max(x) * c);
-            more |= top[nb] > m[nb];
+            more |= top[nb] > m[nb] + kSlack;
         }
         if (__any(more)) {
 #pragma unroll
@@ -366,7 +433,7 @@ struct Softmax {
         for (int nb = 0; nb < NB; ++nb) {
             const float base = m[nb] == -INFINITY ? 0.f : m[nb];
 #pragma unroll
-            for (int e = 0; e < 4 * C::MT; ++e) {
+            for (int e = 0; e < 4 * Q; ++e) {
                 const float w = fast_exp2(fmaf(s[nb][e >> 2][e & 3], c, -base));
                 s[nb][e >> 2][e & 3] = w;
                 l[nb] += w;
@@ -374,6 +441,26 @@ struct Softmax {
         }
     }
 };
+
+// Scores of a tile from position j0 on that some row does not see all of: what a row does not see counts for
+// nothing, and what it sees of a key whose value is not finite (`bad`) makes it NaN.
+template <int NB, int Q>
+__device__ __forceinline__ void apply_sees(f32x4 (&s)[NB][Q], const RowSees (&row)[NB], int j0, int sinks, int len, uint64_t bad) {
+    const int g4 = 4 * ((threadIdx.x & 63) >> 4);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const uint64_t bits = sees(row[nb], j0, sinks, len) >> g4;
+        if (bad) {
+            const uint64_t spoilt = bad >> g4;
+#pragma unroll
+            for (int x = 0; x < 4 * Q; ++x)
+                if ((spoilt >> (16 * (x >> 2) + (x & 3))) & 1) s[nb][x >> 2][x & 3] = NAN;
+        }
+#pragma unroll
+        for (int x = 0; x < 4 * Q; ++x)
+            s[nb][x >> 2][x & 3] = (bits >> (16 * (x >> 2) + (x & 3))) & 1 ? s[nb][x >> 2][x & 3] : -INFINITY;
+    }
+}
 
 template <typename E>
 __device__ __forceinline__ void store_quad(char* row, int dim, f32x4 x) {
@@ -384,6 +471,85 @@ __device__ __forceinline__ void store_quad(char* row, int dim, f32x4 x) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] = (__bf16)x[e];
         *(bf16x4*)(row + dim * 2) = y;
+    }
+}
+
+// ---- shares of one block of rows -------------------------------------------------------------------
+// A ticket word is the tag of a launch (upper 48 bits) and the tickets drawn in it; a word with another tag
+// counts as none, so nothing has to clear it.  The workgroup that draws the last ticket joins the shares.
+// They travel through agent-scope accesses, which the L2s of all dies agree on, and are ordered before the
+// ticket by waiting until the stores are acknowledged.
+__device__ __forceinline__ void share_put(float* to, f32x4 x) {
+    const uint64_t a = ((uint64_t)__float_as_uint(x[1]) << 32) | __float_as_uint(x[0]);
+    const uint64_t b = ((uint64_t)__float_as_uint(x[3]) << 32) | __float_as_uint(x[2]);
+    __hip_atomic_store((uint64_t*)to, a, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store((uint64_t*)to + 1, b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 share_pair(const float* from) {
+    const uint64_t a = __hip_atomic_load((const uint64_t*)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((uint32_t)a), __uint_as_float((uint32_t)(a >> 32)));
+}
+__device__ __forceinline__ void ticket_open(uint64_t* word, uint64_t epoch) {
+    uint64_t seen = __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if ((seen ^ epoch) >> 16)
+        __hip_atomic_compare_exchange_strong(word, &seen, epoch, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// one thread, behind the barrier behind everybody's stores: whether this was the last of `n`
+__device__ __forceinline__ bool ticket_last(uint64_t* word, uint64_t epoch, int n) {
+    const bool last = __hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == epoch + (uint64_t)(n - 1);
+    if (last) __hip_atomic_store(word, epoch, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // (for a replay)
+    return last;
+}
+
+// What a sum with maximum m weighs when joined under the maximum `top` (no key at all: m is -inf, l 0)
+__device__ __forceinline__ float join_weight(float m, float top) { return m == -INFINITY ? 0.f : fast_exp2(m - top); }
+
+// The shares of rows [from, to) of a block: a quad of a row by one thread.  AGENT: written in this launch.
+template <bool AGENT>
+__device__ __forceinline__ float2 share_get(const float* from) {
+    if constexpr (AGENT) return share_pair(from);
+    else return *(const float2*)from;
+}
+template <typename E, int D, int ROWS, int THREADS, bool AGENT>
+__device__ __forceinline__ void join_shares(const AttnParams& p, int block, int shares, int first_row, int head, int r0, int from, int to) {
+    constexpr int QUADS = D / 4, FLIGHT = 4;
+    const size_t base = (size_t)block * p.splits * ROWS;
+    for (int i = threadIdx.x; i < (to - from) * QUADS; i += THREADS) {
+        const int r = from + i / QUADS, quad = i % QUADS;
+        // running maximum over the shares, FLIGHT of them on their way at a time
+        float top = -INFINITY, l = 0.f;
+        f32x4 o = {0, 0, 0, 0};
+        for (int s0 = 0; s0 < shares; s0 += FLIGHT) {
+            float2 ml[FLIGHT], a[FLIGHT], b[FLIGHT];
+#pragma unroll
+            for (int f = 0; f < FLIGHT; ++f) {
+                ml[f] = make_float2(-INFINITY, 0.f);
+                a[f] = b[f] = make_float2(0.f, 0.f);
+                if (s0 + f < shares) {
+                    const size_t at = base + (size_t)(s0 + f) * ROWS + r;
+                    ml[f] = share_get<AGENT>((const float*)(p.part_ml + at));
+                    a[f] = share_get<AGENT>(p.part_o + at * D + quad * 4);
+                    b[f] = share_get<AGENT>(p.part_o + at * D + quad * 4 + 2);
+                }
+            }
+            float next = top;
+#pragma unroll
+            for (int f = 0; f < FLIGHT; ++f) next = fmaxf(next, ml[f].x);
+            const float old = join_weight(top, next);
+            l *= old;
+            o *= old;
+            top = next;
+#pragma unroll
+            for (int f = 0; f < FLIGHT; ++f) {
+                if (ml[f].y == 0.f) continue;             // (nothing seen: its sums may be anything)
+                const float w = join_weight(ml[f].x, top);
+                l += ml[f].x == -INFINITY ? ml[f].y : ml[f].y * w;
+                o += f32x4{a[f].x, a[f].y, b[f].x, b[f].y} * w;
+            }
+        }
+        const int t = (r0 + r) / p.group, h = head * p.group + (r0 + r) % p.group;
+        const f32x4 zero = {0, 0, 0, 0};
+        store_quad<E>(p.out + (int64_t)(first_row + t) * p.out_stride + (int64_t)h * (D * (int)sizeof(E)), quad * 4, l == 0.f ? zero : o * (1.f / l));
     }
 }
 

@@ -652,11 +652,12 @@ def _rows(t, dtype, n_rows: int, what: str):
     """(pointer, row stride in elements) of row-indexed data; everything behind the row index is contiguous."""
     if not t.is_cuda or t.dtype != dtype:
         raise TypeError(f"{what} must be a device tensor of {dtype}")
-    if t.shape[0] < n_rows:
-        raise TypeError(f"{what} has {t.shape[0]} rows of {n_rows}")
-    if t.shape[0] > 0 and not t[0].is_contiguous():
+    shape, stride = t.shape, t.stride()
+    if shape[0] < n_rows:
+        raise TypeError(f"{what} has {shape[0]} rows of {n_rows}")
+    if stride[-1] != 1 or (len(shape) == 3 and shape[1] > 1 and stride[1] != shape[2]):
         raise TypeError(f"a row of {what} must be contiguous")
-    return t.data_ptr(), t.stride(0)
+    return t.data_ptr(), stride[0]
 
 
 def _ints(t, n: int, what: str):
