@@ -4,7 +4,6 @@
 // group -- form blocks of 16, 32 or 64; a workgroup takes a block and a share of the keys that it sees.
 
 #include <cmath>
-#include <type_traits>
 
 #include "dip_attn_device.h"
 
@@ -17,6 +16,7 @@ namespace {
 #define KT 512
 #endif
 constexpr int kWaves = KW;
+constexpr int kRowsTarget = KT;
 constexpr int kThreads = kWaves * 64;
 constexpr int kIds = 1024;                // page numbers of a share, in LDS
 constexpr int kRing = 2;                  // tiles of a wavefront in LDS: one in use, one on its way
@@ -77,7 +77,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams
 
     const char* kbase = p.c.k + p.c.head_stride * head * 16;
     const char* vbase = p.c.v + p.c.head_stride * head * 16;
-    const lds_char* ring = (const lds_char*)s_ring + wave * (kRing * 2 * TILE);
     const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_offset(s_ring) + wave * (kRing * 2 * TILE));
     const int mine = max(0, (end - begin - wave + kWaves - 1) / kWaves);
 
@@ -96,14 +95,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams
     for (int i = 0; i < mine; ++i) {
         if (i + 1 < mine) wait_loads<2 * LOADS>(); else wait_loads<0>();
         const int j0 = tile_at(range, begin + wave + kWaves * i) * KEYS;
-        const lds_char* kt = ring + (i & (kRing - 1)) * (2 * TILE);
+        const uint32_t tile = ring_at + (i & (kRing - 1)) * (2 * TILE);
         f32x4 s[NB][C::MT];
-        core.scores(kt, s, 0);
+        core.scores(C::k_base(tile), s);
         const bool whole = j0 + KEYS <= range.sure && (j0 >= range.from || j0 + KEYS <= p.sinks);
         if (!whole) {
             uint64_t bad = 0;
 #pragma unroll
-            for (int x = 0; x < LOADS; ++x) bad |= take_out<G>((lds_char*)kt + TILE, x);
+            for (int x = 0; x < LOADS; ++x) bad |= take_out<G>(tile + TILE, x);
             if (__any(bad != 0))
                 for (int off = 1; off < 64; off <<= 1) bad |= __shfl_xor((uint32_t)bad, off);
             asm volatile("" ::: "memory");
@@ -112,7 +111,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams
         soft.step(core, s, p.scale_log2);
         typename C::Weights w;
         C::template pack<true>(s, 0, w);
-        core.template add_values<true>(kt + TILE, w);
+        core.template add_values<true>(C::v_base(tile + TILE), 0, w);
         if (i + kRing < mine) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (everything read from the tile that goes)
             fetch(i + kRing);
@@ -177,20 +176,19 @@ __global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams
 }
 
 // Rows enough to fill the matrix cores: eight wavefronts of 16 NB rows each share the tiles, one barrier a tile.
-// The two wavefronts of a SIMD take turns: of tile i's products and the softmax between them, the first four
-// wavefronts run [K_i Q, V_{i-1} P_{i-1}, softmax i], the other four [softmax i-1, K_i Q, V_{i-1} P_{i-1}], so
-// that one's exponentials run beside the other's products.  Four tiles of LDS: V of the last one, the
-// current one, two on their way.
+// Four tiles of LDS: V of the last one, the current one, two on their way.
 constexpr int kBlockWaves = 8;
+constexpr int kBlockSub = 2;              // key blocks of the products in a tile: 64 keys
 constexpr int kBlockThreads = kBlockWaves * 64;
 constexpr int kBlockRing = 4;
+constexpr int kFewKeys = 512;             // of a row: below that its weights go in as two terms where they are at an edge
 constexpr int kIdTiles = 64;              // tiles whose page numbers are in LDS at a time
 
 template <typename E, int D, int NB>
 __global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const AttnParams p) {
     typedef Geo<E, D> G;
     typedef Core<E, D, NB> C;
-    constexpr int SUB = 2, KEYS = SUB * G::KEYS, TILE = KEYS * G::ROWB, LOADS = TILE / 1024, ROWS = 16 * NB * kBlockWaves;
+    constexpr int SUB = kBlockSub, KEYS = SUB * G::KEYS, TILE = KEYS * G::ROWB, LOADS = TILE / 1024, ROWS = 16 * NB * kBlockWaves;
     constexpr int MINE = (LOADS + kBlockWaves - 1) / kBlockWaves;     // loads of a wavefront (some twice where uneven)
     constexpr int Q = SUB * C::MT;
     __shared__ __align__(1024) char s_ring[kBlockRing * 2 * TILE];
@@ -247,9 +245,8 @@ __global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const Attn
 
     const char* kbase = p.c.k + p.c.head_stride * head * 16;
     const char* vbase = p.c.v + p.c.head_stride * head * 16;
-    const lds_char* ring = (const lds_char*)s_ring;
     const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_offset(s_ring));
-    auto tile_of = [&](int i) { return ring + (i & (kBlockRing - 1)) * (2 * TILE); };
+    auto tile_of = [&](int i) { return ring_at + (i & (kBlockRing - 1)) * (2 * TILE); };
     auto fetch = [&](int i) {
         const int j0 = tile_at(range, begin + i) * KEYS;
         const int* ids = s_ids + (i & (kIdTiles - 1)) * per;
@@ -280,12 +277,14 @@ __global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const Attn
             fetch(i + 2);
         }
     };
-    auto scores = [&](int i, f32x4 (&s)[NB][Q]) {
-#pragma unroll
-        for (int u = 0; u < SUB; ++u) core.scores(tile_of(i) + u * G::KEYS * G::ROWB, s, u * C::MT);
-    };
-    // tiles that some row does not see all of: rows that see few keys have them here, so weights go in as two
-    // terms
+    auto scores = [&](int i, f32x4 (&s)[NB][Q]) { core.scores(C::k_base(tile_of(i)), s); };
+    // What the wavefront's rows see lies below see_hi and, but for the sinks, from see_lo on; `few`: some row sees
+    // few keys, which then lie in tiles at an edge.
+    const int wt0 = (r0 + w0) / p.group, wt1 = (r0 + min(w0 + 16 * NB, n_rows) - 1) / p.group;
+    const int see_hi = w0 >= n_rows ? 0 : p.parents ? range.end : min(range.end, len + wt1 + 1);
+    const int see_lo = !p.window ? 0 : max(0, len + (p.parents ? 0 : wt0) - p.window + 1);
+    const bool few = min(range.sure, p.window ? p.window : range.sure) < kFewKeys;
+    // tiles that some row does not see all of
     auto edge = [&](int from, int to) {
         if (tid < 2) s_bad[from & 1][tid] = 0;
         RowSees row[NB];
@@ -295,26 +294,36 @@ __global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const Attn
             if (tid < 2) s_bad[(i + 1) & 1][tid] = 0;
             uint64_t bad = 0;
 #pragma unroll
-            for (int m = 0; m < MINE; ++m) bad |= take_out<G>((lds_char*)tile_of(i) + TILE, (wave * MINE + m) % LOADS);
+            for (int m = 0; m < MINE; ++m) bad |= take_out<G>(tile_of(i) + TILE, (wave * MINE + m) % LOADS);
             if (bad) {
                 atomicOr(&s_bad[i & 1][0], (uint32_t)bad);
                 atomicOr(&s_bad[i & 1][1], (uint32_t)(bad >> 32));
             }
             barrier();
             bad = ((uint64_t)s_bad[i & 1][1] << 32) | s_bad[i & 1][0];
+            // (a wavefront that sees nothing of the tile only keeps the others' time)
+            const int j0 = tile_at(range, begin + i) * KEYS;
+            if (j0 >= see_hi || (j0 + KEYS <= see_lo && j0 >= p.sinks)) continue;
             f32x4 s[NB][Q];
             scores(i, s);
-            apply_sees(s, row, tile_at(range, begin + i) * KEYS, p.sinks, len, bad);
+            apply_sees(s, row, j0, p.sinks, len, bad);
             soft.step(core, s, p.scale_log2);
+            const uint32_t v = C::v_base(tile_of(i) + TILE);
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
                 typename C::Weights w;
-                C::template pack<true>(s, u * C::MT, w);
-                core.template add_values<true>(tile_of(i) + TILE + u * G::KEYS * G::ROWB, w);
+                if (few) {
+                    C::template pack<true>(s, u * C::MT, w);
+                    core.template add_values<true>(v, u * G::KEYS, w);
+                } else {
+                    C::template pack<false>(s, u * C::MT, w);
+                    core.template add_values<false>(v, u * G::KEYS, w);
+                }
             }
         }
     };
-    auto middle = [&](auto late, int from, int to) {
+    // the others: the second product lags one tile behind the first, so that both are at hand together
+    auto middle = [&](int from, int to) {
         if (from >= to) return;
         f32x4 s[NB][Q];
         typename C::Weights w[SUB];
@@ -324,20 +333,20 @@ __global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const Attn
             for (int u = 0; u < SUB; ++u) C::template pack<false>(s, u * C::MT, w[u]);
         };
         auto values = [&](int i) {
+            const uint32_t v = C::v_base(tile_of(i) + TILE);
 #pragma unroll
-            for (int u = 0; u < SUB; ++u) core.template add_values<false>(tile_of(i) + TILE + u * G::KEYS * G::ROWB, w[u]);
+            for (int u = 0; u < SUB; ++u) core.template add_values<false>(v, u * G::KEYS, w[u]);
         };
         arrive(from);
         scores(from, s);
-        if (!late.value) weigh();
         for (int i = from + 1; i < to; ++i) {
             arrive(i);
-            if (late.value) weigh();
+            weigh();
             scores(i, s);
             values(i - 1);
-            if (!late.value) weigh();
+            C::template schedule_products<SUB>();
         }
-        if (late.value) weigh();
+        weigh();
         values(to - 1);
     };
 
@@ -347,8 +356,7 @@ __global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const Attn
     if (n > 0) fetch(0);
     if (n > 1) fetch(1);
     edge(0, mid0);
-    if (wave >= kBlockWaves / 2) middle(std::true_type(), mid0, mid1);
-    else middle(std::false_type(), mid0, mid1);
+    middle(mid0, mid1);
     edge(mid1, n);
 
     RowSees row[NB];
@@ -391,7 +399,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p) {
     const int seq = entry_seq(p.b, p.c, e);
     if (seq < 0) return;
     const int len = min(entry_len(p.c, seq), p.max_len);
-    const Range range = key_range<2 * Geo<E, D>::KEYS>(p, len, er.rows, r0 / p.group, (r0 + n_rows - 1) / p.group);
+    const Range range = key_range<kBlockSub * Geo<E, D>::KEYS>(p, len, er.rows, r0 / p.group, (r0 + n_rows - 1) / p.group);
     const int shares = (range.tiles + p.tiles_per_split - 1) / p.tiles_per_split;
     if (shares > 1) join_shares<E, D, ROWS, 256, false>(p, block, shares, er.first, head, r0, part * kJoinRows, min(n_rows, (part + 1) * kJoinRows));
 }
@@ -407,16 +415,14 @@ int reach(const dip_kv_cache* c, const dip_batch* b) {
     const int fit = c->max_pages * c->page_size;
     return b->max_len && b->max_len < fit ? b->max_len : fit;
 }
-#ifndef BT
-#define BT 768
-#endif
 Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads, int window, int sinks) {
     Plan pl;
     const int64_t rows = (int64_t)rows_bound(b) * (n_q_heads / c->n_kv_heads);
-    pl.shared = rows > 64;
-    pl.nb = pl.shared ? (rows <= 128 ? 1 : 2) : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    // more than 64 rows share tiles; not in fp32, whose products take sixteen times as long and hide any traffic
+    pl.shared = rows > 64 && c->dtype == DIP_BF16;
+    pl.nb = pl.shared ? (rows <= 16 * kBlockWaves ? 1 : 2) : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     pl.rows = 16 * pl.nb * (pl.shared ? kBlockWaves : 1);
-    const int keys = (c->dtype == DIP_F32 ? 16 : 32) * (pl.shared ? 2 : 1);
+    const int keys = (c->dtype == DIP_F32 ? 16 : 32) * (pl.shared ? kBlockSub : 1);
     pl.row_blocks = (int)((rows + pl.rows - 1) / pl.rows);
     pl.blocks = (int64_t)b->n_batch * c->n_kv_heads * pl.row_blocks;
     // most tiles that a block of rows sees
@@ -427,7 +433,7 @@ Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads, in
     }
     // enough workgroups for the chip, but no share under two tiles a wavefront (eight shared ones), and none
     // with more page numbers than LDS holds
-    const int64_t want = ((pl.shared ? BT : KT) + pl.blocks - 1) / pl.blocks;
+    const int64_t want = ((pl.shared ? 768 : kRowsTarget) + pl.blocks - 1) / pl.blocks;
     int64_t per = (tiles + want - 1) / want;
     if (per < 8) per = 8;
     if (!pl.shared) {
@@ -456,20 +462,26 @@ Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads, in
 template <typename E, int D>
 int32_t launch(const AttnParams& p, const Plan& pl, hipStream_t stream) {
     hipError_t err;
+    const dim3 grid((unsigned)p.grid), block(kThreads);
     if (pl.shared) {
-        const dim3 grid((unsigned)((p.grid + 7) / 8 * 8));
-        if (pl.nb == 1) err = launch_timed(attn_block_kernel<E, D, 1>, grid, dim3(kBlockThreads), stream, DIP_KERNEL_ATTENTION, p);
-        else err = launch_timed(attn_block_kernel<E, D, 2>, grid, dim3(kBlockThreads), stream, DIP_KERNEL_ATTENTION, p);
-        if (err == hipSuccess && pl.splits > 1) {
-            const dim3 join((unsigned)(pl.blocks * (pl.rows / kJoinRows)));
-            if (pl.nb == 1) err = launch_timed(attn_join_kernel<E, D, 1>, join, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
-            else err = launch_timed(attn_join_kernel<E, D, 2>, join, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
+        if constexpr (sizeof(E) == 2) {
+            const dim3 bgrid((unsigned)((p.grid + 7) / 8 * 8)), bblock(kBlockThreads);
+            if (pl.nb == 1) err = launch_timed(attn_block_kernel<E, D, 1>, bgrid, bblock, stream, DIP_KERNEL_ATTENTION, p);
+            else err = launch_timed(attn_block_kernel<E, D, 2>, bgrid, bblock, stream, DIP_KERNEL_ATTENTION, p);
+            if (err == hipSuccess && pl.splits > 1) {
+                const dim3 join((unsigned)(pl.blocks * (pl.rows / kJoinRows)));
+                if (pl.nb == 1) err = launch_timed(attn_join_kernel<E, D, 1>, join, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
+                else err = launch_timed(attn_join_kernel<E, D, 2>, join, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
+            }
+        } else {
+            return fail(DIP_ERR_UNSUPPORTED, "attention: no launch for this shape");
         }
+    } else if (pl.nb == 1) {
+        err = launch_timed(attn_rows_kernel<E, D, 1>, grid, block, stream, DIP_KERNEL_ATTENTION, p);
+    } else if (pl.nb == 2) {
+        err = launch_timed(attn_rows_kernel<E, D, 2>, grid, block, stream, DIP_KERNEL_ATTENTION, p);
     } else {
-        const dim3 grid((unsigned)p.grid);
-        if (pl.nb == 1) err = launch_timed(attn_rows_kernel<E, D, 1>, grid, dim3(kThreads), stream, DIP_KERNEL_ATTENTION, p);
-        else if (pl.nb == 2) err = launch_timed(attn_rows_kernel<E, D, 2>, grid, dim3(kThreads), stream, DIP_KERNEL_ATTENTION, p);
-        else err = launch_timed(attn_rows_kernel<E, D, 4>, grid, dim3(kThreads), stream, DIP_KERNEL_ATTENTION, p);
+        err = launch_timed(attn_rows_kernel<E, D, 4>, grid, block, stream, DIP_KERNEL_ATTENTION, p);
     }
     return check_hip(err, "attention launch");
 }

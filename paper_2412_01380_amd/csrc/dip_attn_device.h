@@ -160,17 +160,17 @@ struct Geo {
     static constexpr int ROWB = D * ES;
     static constexpr int CPR = ROWB / 16;                  // pieces of a row
     static constexpr int KEYS = ES == 2 ? 32 : 16;         // of one step of the products
-    __device__ static __forceinline__ int slot(int row, int c) {
-        if constexpr (CPR == 16 || CPR == 32) return c ^ (row & 15);
-        else if constexpr (CPR == 8) return c ^ ((row >> 1) & 7);
-        else if constexpr (CPR == 12) { const int s = c + ((row >> 2) & 3); return s >= 12 ? s - 12 : s; }
-        else { static_assert(CPR == 24, "row length"); const int s = c + ((row >> 1) & 7); return s >= 24 ? s - 24 : s; }
+    static constexpr int ROT = CPR == 12 ? 4 : CPR == 8 || CPR == 24 ? 8 : 16;
+    // piece c of a row lies at c ^ twist(row): the low bits only, in which a row's start has none
+    __device__ static __forceinline__ int twist(int row) {
+        static_assert(CPR == 8 || CPR == 12 || CPR == 16 || CPR == 24 || CPR == 32, "row length");
+        return ROT == 16 ? row & 15 : ROT == 8 ? (row >> 1) & 7 : (row >> 2) & 3;
     }
-    __device__ static __forceinline__ int piece(int row, int s) {   // the inverse
-        if constexpr (CPR == 16 || CPR == 32) return s ^ (row & 15);
-        else if constexpr (CPR == 8) return s ^ ((row >> 1) & 7);
-        else if constexpr (CPR == 12) { const int c = s - ((row >> 2) & 3); return c < 0 ? c + 12 : c; }
-        else { const int c = s - ((row >> 1) & 7); return c < 0 ? c + 24 : c; }
+    // Where piece c + l of the rows row + 16 x (l < 4 a lane's part, c a multiple of 4, or l < 2 and of 2) lies, from
+    // base = row_at(row, l): one register for all c and x.
+    __device__ static __forceinline__ uint32_t row_at(int row, int l) { return row * ROWB + ((l ^ twist(row)) << 4); }
+    __device__ static __forceinline__ const lds_char* at(uint32_t base, int c, int rows) {
+        return (const lds_char*)(size_t)((base ^ ((c & (ROT - 1)) * 16)) + (c & ~(ROT - 1)) * 16 + rows * ROWB);
     }
 };
 
@@ -190,7 +190,7 @@ __device__ __forceinline__ int64_t piece_offset(const KvView& c, const int* ids,
     const int at = x * 64 + (threadIdx.x & 63), r = at / G::CPR;
     const int pos = min(j0 + r, end - 1), shift = c.page_shift;
     const int page = ids[(pos >> shift) - (j0 >> shift)];
-    return (page * c.page_stride + (pos & ((1 << shift) - 1)) * c.slot_stride + G::piece(r, at % G::CPR)) * 16;
+    return (page * c.page_stride + (pos & ((1 << shift) - 1)) * c.slot_stride + ((at % G::CPR) ^ G::twist(r))) * 16;
 }
 template <int N>
 __device__ __forceinline__ void wait_loads() {
@@ -201,9 +201,9 @@ __device__ __forceinline__ void wait_loads() {
 // it out; the bit of its key, or 0.  (Only tiles that some row does not see all of are looked through: in the
 // others what is not finite belongs in the results.)
 template <typename G>
-__device__ __forceinline__ uint64_t take_out(lds_char* v, int x) {
+__device__ __forceinline__ uint64_t take_out(uint32_t v, int x) {
     const int lane = threadIdx.x & 63;
-    auto* at = (__attribute__((address_space(3))) u32x4*)(v + x * 1024 + lane * 16);
+    auto* at = (__attribute__((address_space(3))) u32x4*)(lds_char*)(size_t)(v + x * 1024 + lane * 16);
     const u32x4 w = *at;
     bool inf = false;
 #pragma unroll
@@ -251,21 +251,32 @@ struct Core<uint16_t, D, NB> {
             q[nb][s] = __builtin_bit_cast(bf16x8, x);
         }
     }
-    // KEYS keys' scores into s[.][at ..]: s[nb][at + x][i] is key 16 x + 4 g + i
+    // where a lane's reads of K and of V start in a tile; opaque, so that what is added to them is added where it is
+    // used instead of being kept in a register each
+    __device__ __forceinline__ static uint32_t k_base(uint32_t tile) {
+        uint32_t x = tile + G::row_at(threadIdx.x & 15, (threadIdx.x & 63) >> 4);
+        asm volatile("" : "+v"(x));
+        return x;
+    }
+    __device__ __forceinline__ static uint32_t v_base(uint32_t tile) {
+        const int i = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+        uint32_t x = tile + G::row_at(4 * g + (i >> 2), (i & 3) >> 1) + (i & 1) * 8;
+        asm volatile("" : "+v"(x));
+        return x;
+    }
+    // scores of a tile of 16 Q keys: s[nb][x][i] is key 16 x + 4 g + i.  The blocks of 16 keys go side by side, so that
+    // a product does not wait for the one before it.
     template <int Q>
-    __device__ __forceinline__ void scores(const lds_char* k, f32x4 (&s)[NB][Q], int at) const {
-        const int m = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+    __device__ __forceinline__ void scores(uint32_t k, f32x4 (&s)[NB][Q]) const {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
+        for (int st = 0; st < QS; ++st)
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) s[nb][at + mt] = f32x4{0, 0, 0, 0};
+            for (int x = 0; x < Q; ++x) {
+                const bf16x8 a = *(const __attribute__((address_space(3))) bf16x8*)G::at(k, 4 * st, 16 * x);
 #pragma unroll
-            for (int st = 0; st < QS; ++st) {
-                const bf16x8 a = *(const __attribute__((address_space(3))) bf16x8*)(k + (16 * mt + m) * G::ROWB + G::slot(16 * mt + m, 4 * st + g) * 16);
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) s[nb][at + mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[nb][st], s[nb][at + mt], 0, 0, 0);
+                for (int nb = 0; nb < NB; ++nb)
+                    s[nb][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[nb][st], st ? s[nb][x] : f32x4{0, 0, 0, 0}, 0, 0, 0);
             }
-        }
     }
     // The weights of KEYS keys as the second product takes them.  As one bf16 term each they are off by up to
     // 2^-8, which over many keys averages out but shows where a few of them carry a row; with TWO the
@@ -285,17 +296,15 @@ struct Core<uint16_t, D, NB> {
             }
     }
     template <bool TWO>
-    __device__ __forceinline__ void add_values(const lds_char* v, const Weights& p) {
-        const int i = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+    __device__ __forceinline__ void add_values(uint32_t v, int key, const Weights& p) {
 #pragma unroll
         for (int db = 0; db < OB; ++db) {
             // four keys at this lane's dim each: the transposing read hands lane i column i of 4 rows x 16 dims
             bf16x8 a;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const int key = 16 * half + 4 * g + (i >> 2), c = 2 * db + ((i & 3) >> 1);
                 const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4*)(v + key * G::ROWB + G::slot(key, c) * 16 + (i & 1) * 8));
+                    (__attribute__((address_space(3))) s16x4*)G::at(v, 2 * db, key + 16 * half));
                 const bf16x4 y = __builtin_bit_cast(bf16x4, x);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) a[4 * half + e] = y[e];
@@ -307,6 +316,25 @@ struct Core<uint16_t, D, NB> {
                 for (int nb = 0; nb < NB; ++nb) o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p.rest[nb], o[nb][db], 0, 0, 0);
             }
         }
+    }
+    // Behind a tile's two products (SUB KEYS keys): reads run FLIGHT operands ahead of the products that take them.
+    // (Left to itself the compiler reads each right before its use, to save registers.)
+    template <int SUB>
+    __device__ __forceinline__ static void schedule_products() {
+        constexpr int KF = SUB * MT * QS, VF = SUB * OB, FLIGHT = 4;       // operands of K, of V (two reads each)
+#pragma unroll
+        for (int f = 0; f < FLIGHT; ++f) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+#pragma unroll
+        for (int f = FLIGHT; f < KF; ++f) {
+            __builtin_amdgcn_sched_group_barrier(0x8, NB, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+#pragma unroll
+        for (int f = 0; f < VF; ++f) {
+            __builtin_amdgcn_sched_group_barrier(0x8, NB, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x8, FLIGHT * NB, 0);
     }
     // first dim of the four that o[nb][x] .. hold: quad y of them, y < OB
     __device__ __forceinline__ static int quad_dim(int y) { return 16 * y + 4 * ((threadIdx.x & 63) >> 4); }
@@ -328,19 +356,29 @@ struct Core<float, D, NB> {
             if (row) q[nb][s] = *(const f32x4*)(row + (4 * s + ((threadIdx.x & 63) >> 4)) * 16);
         }
     }
+    __device__ __forceinline__ static uint32_t k_base(uint32_t tile) {
+        uint32_t x = tile + G::row_at(threadIdx.x & 15, (threadIdx.x & 63) >> 4);
+        asm volatile("" : "+v"(x));
+        return x;
+    }
+    __device__ __forceinline__ static uint32_t v_base(uint32_t tile) {     // (the rows of a V read are no constants)
+        uint32_t x = tile;
+        asm volatile("" : "+v"(x));
+        return x;
+    }
     template <int Q>
-    __device__ __forceinline__ void scores(const lds_char* k, f32x4 (&s)[NB][Q], int at) const {
-        const int m = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+    __device__ __forceinline__ void scores(uint32_t k, f32x4 (&s)[NB][Q]) const {
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) s[nb][at] = f32x4{0, 0, 0, 0};
+        for (int st = 0; st < QS; ++st)
 #pragma unroll
-        for (int st = 0; st < QS; ++st) {
-            const f32x4 a = *(const __attribute__((address_space(3))) f32x4*)(k + m * G::ROWB + G::slot(m, 4 * st + g) * 16);
+            for (int x = 0; x < Q; ++x) {
+                const f32x4 a = *(const __attribute__((address_space(3))) f32x4*)G::at(k, 4 * st, 16 * x);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < 4; ++e)
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) s[nb][at] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], q[nb][st][e], s[nb][at], 0, 0, 0);
-        }
+                    for (int nb = 0; nb < NB; ++nb)
+                        s[nb][x] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], q[nb][st][e], st + e ? s[nb][x] : f32x4{0, 0, 0, 0}, 0, 0, 0);
+            }
     }
     struct Weights {
         f32x4 w[NB];
@@ -351,20 +389,21 @@ struct Core<float, D, NB> {
         for (int nb = 0; nb < NB; ++nb) x.w[nb] = p[nb][at];
     }
     template <bool>
-    __device__ __forceinline__ void add_values(const lds_char* v, const Weights& p) {
+    __device__ __forceinline__ void add_values(uint32_t v, int key, const Weights& p) {
         const int m = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
 #pragma unroll
         for (int b = 0; b < OB / VE; ++b) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int key = 4 * g + i;
+                const int row = 4 * g + i;
+                const uint32_t at = v + (key + row) * G::ROWB;
                 float a[VE];
                 if constexpr (VE == 4) {
-                    const f32x4 x = *(const __attribute__((address_space(3))) f32x4*)(v + key * G::ROWB + G::slot(key, 16 * b + m) * 16);
+                    const f32x4 x = *(const __attribute__((address_space(3))) f32x4*)(const lds_char*)(size_t)(at + ((16 * b + m) ^ G::twist(row)) * 16);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) a[e] = x[e];
                 } else {
-                    const f32x2 x = *(const __attribute__((address_space(3))) f32x2*)(v + key * G::ROWB + G::slot(key, 8 * b + (m >> 1)) * 16 + (m & 1) * 8);
+                    const f32x2 x = *(const __attribute__((address_space(3))) f32x2*)(const lds_char*)(size_t)(at + ((8 * b + (m >> 1)) ^ G::twist(row)) * 16 + (m & 1) * 8);
                     a[0] = x[0];
                     a[1] = x[1];
                 }
@@ -376,6 +415,8 @@ struct Core<float, D, NB> {
             }
         }
     }
+    template <int SUB>
+    __device__ __forceinline__ static void schedule_products() {}
     // o[nb][b * VE + e][i] is dim 16 VE b + VE (4 g + i) + e: four neighbours are e = 0 .. 3 of one i, or
     // e = 0, 1 of two
     __device__ __forceinline__ static int quad_dim(int y) {
