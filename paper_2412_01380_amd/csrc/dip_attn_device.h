@@ -48,7 +48,6 @@ struct AttnParams {
     uint64_t* tickets;        // a word per row block, kTicketStride apart, whatever they hold
     uint64_t epoch;           // this launch's tag in them
 };
-constexpr int kTicketStride = 16;         // words: 128 bytes, so that atomics of different blocks do not queue
 
 // ---- which keys a block of rows sees -----------------------------------------------------------
 struct Range {
@@ -516,10 +515,7 @@ __device__ __forceinline__ void store_quad(char* row, int dim, f32x4 x) {
 }
 
 // ---- shares of one block of rows -------------------------------------------------------------------
-// A ticket word is the tag of a launch (upper 48 bits) and the tickets drawn in it; a word with another tag
-// counts as none, so nothing has to clear it.  The workgroup that draws the last ticket joins the shares.
-// They travel through agent-scope accesses, which the L2s of all dies agree on, and are ordered before the
-// ticket by waiting until the stores are acknowledged.
+// They travel through agent-scope accesses, which the L2s of all dies agree on.
 __device__ __forceinline__ void share_put(float* to, f32x4 x) {
     const uint64_t a = ((uint64_t)__float_as_uint(x[1]) << 32) | __float_as_uint(x[0]);
     const uint64_t b = ((uint64_t)__float_as_uint(x[3]) << 32) | __float_as_uint(x[2]);
@@ -530,18 +526,6 @@ __device__ __forceinline__ float2 share_pair(const float* from) {
     const uint64_t a = __hip_atomic_load((const uint64_t*)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return make_float2(__uint_as_float((uint32_t)a), __uint_as_float((uint32_t)(a >> 32)));
 }
-__device__ __forceinline__ void ticket_open(uint64_t* word, uint64_t epoch) {
-    uint64_t seen = __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if ((seen ^ epoch) >> 16)
-        __hip_atomic_compare_exchange_strong(word, &seen, epoch, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-// one thread, behind the barrier behind everybody's stores: whether this was the last of `n`
-__device__ __forceinline__ bool ticket_last(uint64_t* word, uint64_t epoch, int n) {
-    const bool last = __hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == epoch + (uint64_t)(n - 1);
-    if (last) __hip_atomic_store(word, epoch, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // (for a replay)
-    return last;
-}
-
 // What a sum with maximum m weighs when joined under the maximum `top` (no key at all: m is -inf, l 0)
 __device__ __forceinline__ float join_weight(float m, float top) { return m == -INFINITY ? 0.f : fast_exp2(m - top); }
 

@@ -58,6 +58,24 @@ __device__ __forceinline__ int entry_len(const KvView& c, int seq) {
     return min(max(c.seq_len[seq], 0), c.max_pages << c.page_shift);
 }
 
+// ---- the last workgroup of several -------------------------------------------------------------
+// A ticket word is the tag of a launch (upper 48 bits) and the tickets drawn in it; a word with another tag
+// counts as none, so nothing has to clear it.  Whoever draws the last ticket of a word goes on with what the
+// others stored, through agent-scope accesses, which the L2s of all dies agree on, and had acknowledged
+// (vmcnt 0) before their tickets.
+constexpr int kTicketStride = 16;         // words: 128 bytes, so that atomics on different words do not queue
+__device__ __forceinline__ void ticket_open(uint64_t* word, uint64_t epoch) {
+    uint64_t seen = __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if ((seen ^ epoch) >> 16)
+        __hip_atomic_compare_exchange_strong(word, &seen, epoch, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// one thread, behind the barrier behind everybody's stores: whether this was the last of `n`
+__device__ __forceinline__ bool ticket_last(uint64_t* word, uint64_t epoch, int n) {
+    const bool last = __hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == epoch + (uint64_t)(n - 1);
+    if (last) __hip_atomic_store(word, epoch, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // (for a replay)
+    return last;
+}
+
 }  // namespace dip
 
 #endif  // DIP_DECODE_INTERNAL_H_

@@ -4,10 +4,11 @@
 // after each refusal.  Written without the norms, the j-th r is (p - lam_j q)+ / G_j with
 // lam_0 = 0, G_0 = 1, lam_{j+1} = lam_j + G_j and G_j the sum of (p - lam_j q)+: for a node that
 // was refused j children everything about its rows is in the numbers lam_j and G_j, and a child's test
-// needs two probabilities and these.  So the walk itself is a few loads, done by every workgroup for
-// itself, and the passes over whole rows are plain sums that split over any number of workgroups:
-// G_1 .. G_{m-1} of the nodes with several children (one launch each: lam_{j+1} needs G_j), then the sum
-// over the row at which the walk ends, then the draw.
+// needs two probabilities and these.  So the walk itself is a few loads, done by every workgroup for itself,
+// and the passes over whole rows are plain sums that split over any number of workgroups: G_1 .. G_{m-1} of the
+// nodes with several children (one launch each: lam_{j+1} needs G_j; only nodes that the walk can still
+// reach and whose first j children are refused), then the sum over the row at which the walk ends, whose last
+// workgroup to finish draws the token.
 // Sums and comparisons are in fp64: the outputs are decisions, and with sums that are 1e-16 off in
 // whatever order they are taken, all orders decide alike (an fp32 sum of 128000 terms leaves 1 in 10^5
 // draws open).  fp64 adds at half the fp32 rate cost nothing here: the kernels wait for memory.
@@ -19,7 +20,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxChunks = 64;            // of a row; a lane of one wavefront sums each
-constexpr int kMinChunk = 4096;           // entries: 16 a thread
+constexpr int kPer = 16;                  // entries of a thread at a time: in flight together
+constexpr int kMinChunk = kThreads * kPer;
 
 struct VerifyParams {
     BatchView b;
@@ -39,8 +41,8 @@ struct VerifyParams {
     double* g_part;           // [max_kids - 1][n_rows][chunks]: G_1 ..
     double* w_part;           // [n_batch][chunks] sums of (p - lam q)+ at the last node
     double* p_part;           // [n_batch][chunks] sums of p there
-    int32_t* last_row;        // n_batch (-1: no walk)
-    double* last_lam;         // n_batch
+    uint64_t* tickets;        // a word per entry
+    uint64_t epoch;
     int32_t* keep;
     int32_t* path;
     int32_t* token;
@@ -54,27 +56,31 @@ template <>
 __device__ __forceinline__ float prob_at<uint16_t>(const char* row, int x) {
     return __uint_as_float((uint32_t)((const uint16_t*)row)[x] << 16);
 }
-// 16 bytes of a row, widened (exactly)
+// kPer entries of a row from x on, widened (exactly); zeros from `end` on.  Rows of an odd vocabulary start
+// anywhere: 16-byte loads that ask for no more than E's alignment.
 template <typename E>
-struct Piece {
-    static constexpr int N = 16 / sizeof(E);
-    float f[N];
-    __device__ __forceinline__ void load(const char* row, int x) {
-        // (rows of an odd vocabulary start anywhere: a 16-byte load that asks for no more than E's alignment)
-        struct __attribute__((packed, aligned(sizeof(E)))) Any { uint32_t w[4]; };
-        const Any r = *(const Any*)(row + (size_t)x * sizeof(E));
-        const uint32_t* w = r.w;
+__device__ __forceinline__ void load_entries(const char* row, int x, int end, float (&f)[kPer]) {
+    constexpr int N = 16 / sizeof(E);
+    struct __attribute__((packed, aligned(sizeof(E)))) Any { uint32_t w[4]; };
+    if (x + kPer <= end) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (sizeof(E) == 4) {
-                f[i] = __uint_as_float(w[i]);
-            } else {
-                f[2 * i] = __uint_as_float(w[i] << 16);
-                f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        for (int y = 0; y < kPer / N; ++y) {
+            const Any r = *(const Any*)(row + (size_t)(x + y * N) * sizeof(E));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (sizeof(E) == 4) {
+                    f[y * N + i] = __uint_as_float(r.w[i]);
+                } else {
+                    f[y * N + 2 * i] = __uint_as_float(r.w[i] << 16);
+                    f[y * N + 2 * i + 1] = __uint_as_float(r.w[i] & 0xffff0000u);
+                }
             }
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) f[i] = x + i < end ? prob_at<E>(row, x + i) : 0.f;
     }
-};
+}
 
 __device__ __forceinline__ double weight(float p, float q, double lam) {
     const double w = (double)p - lam * (double)q;
@@ -97,35 +103,28 @@ __device__ __forceinline__ double block_sum(double x, double* waves) {
     return s;
 }
 
-// sums over a chunk of a row: *w of (p - lam q)+, *all of p
-template <typename E, bool BOTH>
-__device__ __forceinline__ void chunk_sums(const VerifyParams& a, const char* p, const char* q, double lam, int chunk, double* w, double* all) {
-    constexpr int N = Piece<E>::N;
+// a thread's part of the sums over a chunk of a row: *w of (p - lam q)+, *all of p
+template <typename E>
+__device__ __forceinline__ void chunk_sums(const VerifyParams& a, int row, double lam, int chunk, double* w, double* all) {
+    const char* p = a.p + row * a.p_stride;
+    const char* q = a.q + row * a.q_stride;
     const int end = min((chunk + 1) * a.chunk, a.n_vocab);
     double sw = 0.0, sp = 0.0;
-    for (int x = chunk * a.chunk + threadIdx.x * N; x < end; x += kThreads * N) {
-        if (x + N <= end) {
-            Piece<E> pp, qq;
-            pp.load(p, x);
-            qq.load(q, x);
+    for (int x = chunk * a.chunk + threadIdx.x * kPer; x < end; x += kThreads * kPer) {
+        float pf[kPer], qf[kPer];
+        load_entries<E>(p, x, end, pf);
+        load_entries<E>(q, x, end, qf);
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                sw += weight(pp.f[i], qq.f[i], lam);
-                if (BOTH) sp += (double)pp.f[i];
-            }
-        } else {
-            for (int y = x; y < end; ++y) {
-                const float pv = prob_at<E>(p, y);
-                sw += weight(pv, prob_at<E>(q, y), lam);
-                if (BOTH) sp += (double)pv;
-            }
+        for (int i = 0; i < kPer; ++i) {
+            sw += weight(pf[i], qf[i], lam);
+            sp += (double)pf[i];
         }
     }
     *w = sw;
     *all = sp;
 }
 
-// G_j (j >= 1) of a row: its chunks' sums, added by one thread in order
+// G_j (j >= 1) of a row: its chunks' sums, added in order
 __device__ __forceinline__ double g_of(const VerifyParams& a, int j, int row) {
     const double* part = a.g_part + ((size_t)(j - 1) * a.b.n_rows + row) * a.chunks;
     double s = 0.0;
@@ -133,123 +132,168 @@ __device__ __forceinline__ double g_of(const VerifyParams& a, int j, int row) {
     return s;
 }
 
-// ---- G_round of every node with more than `round` children: grid (chunks, nodes, entries) ----------
+// One wavefront, lane t for node t: which children are taken, as far as G_1 .. G_{known} say.
+struct Walk {
+    uint64_t kids;            // this node's children
+    uint64_t refused;         // nodes tried and refused ...
+    uint64_t taken;           // ... and taken, where every earlier sibling was refused
+    bool reached;             // this node stands, or may do so once more is known
+};
+template <typename E>
+__device__ __forceinline__ Walk walk(const VerifyParams& a, const EntryRows& er, int known) {
+    const int lane = threadIdx.x & 63, row = er.first + lane;
+    const bool is = lane < er.rows;
+    const int parent = is ? a.parents[row] : -2;
+    const int x = is ? a.tokens[row] : -1;
+    const double u = is ? (double)a.u[row] : 0.0;
+    const bool child = parent >= 0 && parent < lane;
+    const int of = child ? parent : -3, up = er.first + (child ? parent : 0);
+    const bool fits = child && (unsigned)x < (unsigned)a.n_vocab;
+    float pv = 0.f, qv = 0.f;
+    if (fits) {
+        pv = prob_at<E>(a.p + up * a.p_stride, x);
+        qv = prob_at<E>(a.q + up * a.q_stride, x);
+    }
+    Walk w;
+    uint64_t earlier = 0;                             // siblings before this node
+    w.kids = 0;
+    for (int s = 0; s < er.rows; ++s) {
+        const int other = __builtin_amdgcn_readlane(of, s);
+        if (other == of && s < lane) earlier |= 1ull << s;
+        if (other == lane) w.kids |= 1ull << s;
+    }
+    const int order = child ? __popcll(earlier) : -1;
+    w.refused = w.taken = 0;
+    uint64_t open = 0;                                // children whose test is not known yet
+    for (int k = 0; k < a.max_kids; ++k) {
+        const bool mine = order == k && (earlier & ~(w.refused | open)) == 0;
+        if (!__any(mine)) break;
+        if (k > known) {
+            open |= __ballot(mine);
+            continue;
+        }
+        bool take = false;
+        if (mine && fits) {
+            double lam = 0.0, G = 1.0;
+            for (int j = 1; j <= k; ++j) {
+                lam += G;
+                G = g_of(a, j, up);
+            }
+            take = u * (double)qv * G < weight(pv, qv, lam);
+        }
+        w.taken |= __ballot(mine && take);
+        w.refused |= __ballot(mine && !take);
+    }
+    // a node is reached if it and all its ancestors up to node 0 are: pointers jump 1, 2, 4 .. steps up
+    bool all = ((w.taken | open) >> lane) & 1;
+    int at = child ? parent : -2;
+    if (lane == 0 && parent == -1) {
+        all = true;
+        at = -1;
+    }
+#pragma unroll
+    for (int i = 0; i < 6; ++i) {
+        const int from = at < 0 ? lane : at;
+        const bool theirs = __shfl((int)all, from);
+        const int next = __shfl(at, from);
+        if (at >= 0) {
+            all = all && theirs;
+            at = next;
+        }
+    }
+    w.reached = all && at == -1;
+    return w;
+}
+
+// ---- G_round of the nodes that can be reached and have refused `round` children, with more to come: grid
+// (chunks, entries) -------------------------------------------------------------------------------------
 template <typename E>
 __global__ void __launch_bounds__(kThreads) verify_sums_kernel(const VerifyParams a) {
     __shared__ double s_waves[kThreads / 64];
-    __shared__ double s_lam;
-    const EntryRows er = entry_rows(a.b, blockIdx.z);
-    const int t = blockIdx.y;
-    if (t >= er.rows) return;
+    __shared__ uint64_t s_nodes;
+    __shared__ double s_lam[64];
+    const EntryRows er = entry_rows(a.b, blockIdx.y);
     const int lane = threadIdx.x & 63;
-    // (every wavefront counts for itself)
-    const int parent = lane < er.rows && lane > t ? a.parents[er.first + lane] : -1;
-    if (__popcll(__ballot(parent == t)) <= a.round) return;
-    const int row = er.first + t;
-    if (threadIdx.x == 0) {
+    if (threadIdx.x < 64) {
+        const Walk w = walk<E>(a, er, a.round - 1);
+        const bool need = w.reached && __popcll(w.kids) > a.round && __popcll(w.kids & w.refused) == a.round;
+        const uint64_t nodes = __ballot(need);
         double lam = 1.0;
-        for (int j = 1; j < a.round; ++j) lam += g_of(a, j, row);
-        s_lam = lam;
+        if (need)
+            for (int j = 1; j < a.round; ++j) lam += g_of(a, j, er.first + lane);
+        s_lam[lane] = lam;
+        if (lane == 0) s_nodes = nodes;
     }
     __syncthreads();
-    double w, all;
-    chunk_sums<E, false>(a, a.p + row * a.p_stride, a.q + row * a.q_stride, s_lam, blockIdx.x, &w, &all);
-    w = block_sum(w, s_waves);
-    if (threadIdx.x == 0) a.g_part[((size_t)(a.round - 1) * a.b.n_rows + row) * a.chunks + blockIdx.x] = w;
+    for (uint64_t left = s_nodes; left; left &= left - 1) {
+        const int t = __ffsll((unsigned long long)left) - 1;
+        double w, all;
+        chunk_sums<E>(a, er.first + t, s_lam[t], blockIdx.x, &w, &all);
+        w = block_sum(w, s_waves);
+        if (threadIdx.x == 0) a.g_part[((size_t)(a.round - 1) * a.b.n_rows + er.first + t) * a.chunks + blockIdx.x] = w;
+    }
 }
 
-// ---- the walk, and the sums over the row where it ends: grid (chunks, entries) ------------------------
+__device__ __forceinline__ void put(double* to, double x) { __hip_atomic_store(to, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ double get(const double* from) { return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// ---- the walk, the sums over the row where it ends, and the draw: grid (chunks, entries) ------------------
 template <typename E>
 __global__ void __launch_bounds__(kThreads) verify_walk_kernel(const VerifyParams a) {
     __shared__ double s_waves[kThreads / 64];
-    __shared__ int s_row;
-    __shared__ double s_lam;
-    const int e = blockIdx.y;
+    __shared__ double s_lam, s_target;
+    __shared__ int s_row, s_chunk, s_found, s_lastpos;
+    const int e = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const EntryRows er = entry_rows(a.b, e);
-    const int lane = threadIdx.x & 63;
-    if (threadIdx.x < 64) {
-        const bool is = lane < er.rows;
-        const int row = er.first + lane;
-        const int parent = is ? a.parents[row] : -2;
-        const bool child = parent >= 0 && parent < lane;
-        int order = 0;                                // earlier children of the same node
-        const int of = child ? parent : -3;
-        for (int s = 0; s < er.rows; ++s) {
-            const int other = __shfl(of, s);          // (every lane takes part)
-            order += s < lane && other == of;
-        }
-        bool taken = false;
-        if (child && order < a.max_kids) {
-            const int x = a.tokens[row], up = er.first + parent;
-            if ((unsigned)x < (unsigned)a.n_vocab) {
-                const float pv = prob_at<E>(a.p + up * a.p_stride, x), qv = prob_at<E>(a.q + up * a.q_stride, x);
-                double lam = 0.0, G = 1.0;
-                for (int j = 0; j < order; ++j) {
-                    lam += G;
-                    G = g_of(a, j + 1, up);
-                }
-                taken = (double)a.u[row] * (double)qv * G < weight(pv, qv, lam);
-            }
-        }
-        const uint64_t take = __ballot(taken);
-        int node = -1, kept = 0, at_path = -1;        // lane i keeps the walk's i-th node
-        if (er.rows > 0 && __shfl(parent, 0) == -1) {
-            node = 0;
-            for (;;) {
-                if (lane == kept) at_path = node;
-                ++kept;
-                const uint64_t next = __ballot(child && parent == node) & take;
-                if (!next) break;
-                node = __ffsll((unsigned long long)next) - 1;   // (children lie behind their parent: this ends)
-            }
-        }
+    uint64_t* ticket = a.tickets + (size_t)e * kTicketStride;
+    if (tid < 64) {
+        if (lane == 0) ticket_open(ticket, a.epoch);
+        const Walk w = walk<E>(a, er, a.max_kids);
+        const uint64_t path = __ballot(w.reached);
+        const int kept = __popcll(path), last = path ? 63 - __clzll((long long)path) : 0;
         if (blockIdx.x == 0) {
-            if (is) a.path[row] = at_path;
+            if (w.reached) a.path[er.first + __popcll(path & ((1ull << lane) - 1))] = lane;
+            if (lane >= kept && lane < er.rows) a.path[er.first + lane] = -1;
             if (lane == 0) a.keep[e] = kept;
         }
-        const int kids = min(__popcll(__ballot(child && parent == node)), a.max_kids);
-        if (lane == 0) {
+        if (lane == last) {
+            const int kids = min(__popcll(w.kids), a.max_kids);
             double lam = 0.0;
-            if (node >= 0)
-                for (int j = 0; j < kids; ++j) lam += j ? g_of(a, j, er.first + node) : 1.0;
-            s_row = node < 0 ? -1 : er.first + node;
+            if (kept)
+                for (int j = 0; j < kids; ++j) lam += j ? g_of(a, j, er.first + last) : 1.0;
+            s_row = kept ? er.first + last : -1;
             s_lam = lam;
-            if (blockIdx.x == 0) {
-                a.last_row[e] = s_row;
-                a.last_lam[e] = lam;
-            }
+            s_found = 0x7fffffff;
+            s_lastpos = -1;
         }
     }
     __syncthreads();
     const int row = s_row;
-    if (row < 0) return;
-    double w, all;
-    chunk_sums<E, true>(a, a.p + row * a.p_stride, a.q + row * a.q_stride, s_lam, blockIdx.x, &w, &all);
-    w = block_sum(w, s_waves);
-    all = block_sum(all, s_waves);
-    if (threadIdx.x == 0) {
-        a.w_part[(size_t)e * a.chunks + blockIdx.x] = w;
-        a.p_part[(size_t)e * a.chunks + blockIdx.x] = all;
-    }
-}
-
-// ---- the draw: one workgroup per entry -------------------------------------------------------------
-// The chunk in which the running sum passes u * sum, then the entry within it.
-template <typename E>
-__global__ void __launch_bounds__(kThreads) verify_draw_kernel(const VerifyParams a) {
-    __shared__ double s_waves[kThreads / 64];
-    __shared__ double s_target, s_lam;
-    __shared__ int s_chunk, s_found, s_lastpos;
-    const int e = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int row = a.last_row[e];
     if (row < 0) {
-        if (tid == 0) a.token[e] = -1;
+        if (blockIdx.x == 0 && tid == 0) a.token[e] = -1;
         return;
     }
+    double w, all;
+    chunk_sums<E>(a, row, s_lam, blockIdx.x, &w, &all);
+    w = block_sum(w, s_waves);
+    all = block_sum(all, s_waves);
+    double* w_part = a.w_part + (size_t)e * a.chunks;
+    double* p_part = a.p_part + (size_t)e * a.chunks;
+    if (tid == 0) {
+        put(w_part + blockIdx.x, w);
+        put(p_part + blockIdx.x, all);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        s_chunk = ticket_last(ticket, a.epoch, a.chunks);
+    }
+    __syncthreads();
+    if (!s_chunk) return;
+
+    // the draw: the chunk in which the running sum passes u * sum, then the entry within it
+    __syncthreads();
     if (tid < 64) {
         // running sums over the chunks, lane c up to chunk c
         auto running = [&](const double* part) {
-            double x = lane < a.chunks ? part[(size_t)e * a.chunks + lane] : 0.0;
+            double x = lane < a.chunks ? get(part + lane) : 0.0;
 #pragma unroll
             for (int off = 1; off < 64; off <<= 1) {
                 const double y = __shfl_up(x, off);
@@ -257,12 +301,12 @@ __global__ void __launch_bounds__(kThreads) verify_draw_kernel(const VerifyParam
             }
             return x;
         };
-        double lam = a.last_lam[e];
-        double upto = running(a.w_part);
+        double lam = s_lam;
+        double upto = running(w_part);
         double total = __shfl(upto, 63);
         if (!(total > 0.0)) {                         // p == q everywhere: the target itself
             lam = 0.0;
-            upto = running(a.p_part);
+            upto = running(p_part);
             total = __shfl(upto, 63);
         }
         const double target = (double)a.u_sample[e] * total;
@@ -277,8 +321,6 @@ __global__ void __launch_bounds__(kThreads) verify_draw_kernel(const VerifyParam
             s_chunk = total > 0.0 ? at : -1;
             s_target = target - skip;
             s_lam = lam;
-            s_found = 0x7fffffff;
-            s_lastpos = -1;
         }
     }
     __syncthreads();
@@ -290,32 +332,20 @@ __global__ void __launch_bounds__(kThreads) verify_draw_kernel(const VerifyParam
     const char* p = a.p + row * a.p_stride;
     const char* q = a.q + row * a.q_stride;
     const double lam = s_lam, target = s_target;
-    constexpr int N = Piece<E>::N;
     const int end = min((c + 1) * a.chunk, a.n_vocab);
     double before = 0.0;                              // sum of the chunk's earlier tiles
-    for (int x0 = c * a.chunk; x0 < end; x0 += kThreads * N) {
-        const int x = x0 + tid * N;
-        double w[N], mine = 0.0;
-        float pf[N], qf[N];
-        if (x + N <= end) {
-            Piece<E> pp, qq;
-            pp.load(p, x);
-            qq.load(q, x);
-#pragma unroll
-            for (int i = 0; i < N; ++i) { pf[i] = pp.f[i]; qf[i] = qq.f[i]; }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                pf[i] = x + i < end ? prob_at<E>(p, x + i) : 0.f;
-                qf[i] = x + i < end ? prob_at<E>(q, x + i) : 0.f;
-            }
-        }
+    for (int x0 = c * a.chunk; x0 < end; x0 += kThreads * kPer) {
+        const int x = x0 + tid * kPer;
+        float pf[kPer], qf[kPer];
+        load_entries<E>(p, x, end, pf);
+        load_entries<E>(q, x, end, qf);
+        double mine = 0.0;
         int lastpos = -1;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            w[i] = weight(pf[i], qf[i], lam);
-            mine += w[i];
-            if (w[i] > 0.0) lastpos = x + i;
+        for (int i = 0; i < kPer; ++i) {
+            const double y = weight(pf[i], qf[i], lam);
+            mine += y;
+            if (y > 0.0) lastpos = x + i;
         }
         double upto = mine;                           // inclusive running sum over the threads
 #pragma unroll
@@ -332,14 +362,14 @@ __global__ void __launch_bounds__(kThreads) verify_draw_kernel(const VerifyParam
             tile += s_waves[v];
         }
         double run = ahead + (upto - mine);
+        int found = 0x7fffffff;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            run += w[i];
-            if (w[i] > 0.0 && run > target) {
-                atomicMin(&s_found, x + i);
-                break;
-            }
+        for (int i = 0; i < kPer; ++i) {
+            const double y = weight(pf[i], qf[i], lam);
+            run += y;
+            if (y > 0.0 && run > target) found = min(found, x + i);
         }
+        if (found != 0x7fffffff) atomicMin(&s_found, found);
         if (lastpos >= 0) atomicMax(&s_lastpos, lastpos);
         before += tile;
         __syncthreads();
@@ -350,13 +380,13 @@ __global__ void __launch_bounds__(kThreads) verify_draw_kernel(const VerifyParam
 
 struct VerifyPlan {
     int chunk, chunks, rounds;
-    size_t off_g, off_w, off_p, off_lam, off_row, total;
+    size_t off_g, off_w, off_p, off_tickets, total;
 };
 VerifyPlan plan_verify(const dip_batch* b, int n_vocab, int max_kids) {
     VerifyPlan pl;
     int chunk = (n_vocab + kMaxChunks - 1) / kMaxChunks;
     if (chunk < kMinChunk) chunk = kMinChunk;
-    pl.chunk = (chunk + 7) / 8 * 8;
+    pl.chunk = (chunk + kPer - 1) / kPer * kPer;
     pl.chunks = (n_vocab + pl.chunk - 1) / pl.chunk;
     const int widest = rows_bound(b) - 1;             // children that one node can have
     pl.rounds = (max_kids < widest ? max_kids : widest) - 1;
@@ -366,8 +396,7 @@ VerifyPlan plan_verify(const dip_batch* b, int n_vocab, int max_kids) {
     pl.off_g = take(sizeof(double) * pl.rounds * b->n_rows * pl.chunks);
     pl.off_w = take(sizeof(double) * b->n_batch * pl.chunks);
     pl.off_p = take(sizeof(double) * b->n_batch * pl.chunks);
-    pl.off_lam = take(sizeof(double) * b->n_batch);
-    pl.off_row = take(sizeof(int32_t) * b->n_batch);
+    pl.off_tickets = take(sizeof(uint64_t) * kTicketStride * b->n_batch);
     pl.total = o;
     return pl;
 }
@@ -385,15 +414,13 @@ template <typename E>
 int32_t launch_verify(VerifyParams& a, const VerifyPlan& pl, hipStream_t stream) {
     for (int j = 1; j <= pl.rounds; ++j) {
         a.round = j;
-        const int32_t st = check_hip(launch_timed(verify_sums_kernel<E>, dim3(pl.chunks, a.b.max_rows, a.b.n_batch), dim3(kThreads), stream,
+        const int32_t st = check_hip(launch_timed(verify_sums_kernel<E>, dim3(pl.chunks, a.b.n_batch), dim3(kThreads), stream,
                                                   DIP_KERNEL_VERIFY, a), "verify_sums launch");
         if (st) return st;
     }
-    const int32_t st = check_hip(launch_timed(verify_walk_kernel<E>, dim3(pl.chunks, a.b.n_batch), dim3(kThreads), stream,
-                                              DIP_KERNEL_VERIFY, a), "verify_walk launch");
-    if (st) return st;
-    return check_hip(launch_timed(verify_draw_kernel<E>, dim3(a.b.n_batch), dim3(kThreads), stream, DIP_KERNEL_VERIFY, a),
-                     "verify_draw launch");
+    a.epoch = next_epoch();
+    return check_hip(launch_timed(verify_walk_kernel<E>, dim3(pl.chunks, a.b.n_batch), dim3(kThreads), stream, DIP_KERNEL_VERIFY, a),
+                     "verify_walk launch");
 }
 
 }  // namespace
@@ -442,8 +469,8 @@ int32_t dip_verify_tree(const dip_batch* batch, const int32_t* tokens, const int
     a.g_part = (double*)(base + pl.off_g);
     a.w_part = (double*)(base + pl.off_w);
     a.p_part = (double*)(base + pl.off_p);
-    a.last_row = (int32_t*)(base + pl.off_row);
-    a.last_lam = (double*)(base + pl.off_lam);
+    a.tickets = (uint64_t*)(base + pl.off_tickets);
+    a.epoch = 0;
     a.keep = keep;
     a.path = path;
     a.token = token;

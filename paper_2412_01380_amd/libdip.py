@@ -238,8 +238,11 @@ def _ptr(t, dtype=None) -> Optional[int]:
 
 
 def _stream(stream) -> Optional[int]:
-    import torch
     if stream is None:
+        import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # the handle itself: 0.2 us, its object 2.7 us
+        if raw is not None:
+            return raw(torch.cuda.current_device()) or None
         return torch.cuda.current_stream().cuda_stream or None
     if isinstance(stream, int):
         return stream or None
