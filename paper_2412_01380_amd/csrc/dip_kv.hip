@@ -361,60 +361,71 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams 
 }
 
 // ---- compact ------------------------------------------------------------------------------
-// Row path[j] moves to row j <= path[j].  Every lane moves 16 bytes of one head through all rows in
-// ascending order, so that a row is read before it is written over and no barrier is needed; up to
-// MOVES rows are in flight.
+// Row path[j] moves to row j <= path[j].  A workgroup takes some heads' rows of a layer, all of k or of v, and
+// reads a batch of rows into registers before it writes any: what is written over is behind, or was read.
+// (Batches go in ascending order: a later one reads rows that no earlier one wrote, since path[j] >= j.)
 struct CompactParams {
     KvView c;
     BatchView b;
     const int32_t* path;      // nullable
     const int32_t* keep;      // nullable
+    int heads;                // of a workgroup
 };
 __device__ __forceinline__ int kept_rows(const CompactParams& p, const EntryRows& er) {
     return p.keep ? min(max(p.keep[blockIdx.x], 0), er.rows) : er.rows;
 }
+constexpr int kMoves = 16;                // 16-byte pieces of a thread in flight
 __global__ void __launch_bounds__(kThreads) kv_move_kernel(const CompactParams p) {
-    constexpr int MOVES = 16;
     const EntryRows er = entry_rows(p.b, blockIdx.x);
     const int kept = kept_rows(p, er);
     const int seq = entry_seq(p.b, p.c, blockIdx.x);
     if (seq < 0 || kept == 0) return;
-    const int i = blockIdx.z * kThreads + threadIdx.x;       // (k or v, head, piece)
-    const int per = p.c.n_heads * p.c.pieces;
-    if (i >= 2 * per) return;
-    const int h = (i % per) / p.c.pieces, x = (i % per) % p.c.pieces;
-    piece_t* base = (piece_t*)(i < per ? p.c.k : p.c.v) + (int64_t)blockIdx.y * p.c.layer_stride + h * p.c.head_stride + x;
+    const int groups = (p.c.n_heads + p.heads - 1) / p.heads;
+    const int h0 = (blockIdx.z % groups) * p.heads, heads = min(p.heads, p.c.n_heads - h0);
+    piece_t* base = (piece_t*)(blockIdx.z / groups ? p.c.v : p.c.k) + (int64_t)blockIdx.y * p.c.layer_stride + h0 * p.c.head_stride;
     const int len = entry_len(p.c, seq);
     const int32_t* table = p.c.table + (size_t)seq * p.c.max_pages;
     const int32_t* path = p.path + er.first;
     const int slot_mask = (1 << p.c.page_shift) - 1;
-    auto place = [&](int row, int64_t* off) {
+    auto place = [&](int row) -> int64_t {
         const int64_t pos = (int64_t)len + row;
-        if ((pos >> p.c.page_shift) >= p.c.max_pages) return false;
+        if ((pos >> p.c.page_shift) >= p.c.max_pages) return -1;
         const int page = table[pos >> p.c.page_shift];
-        if (!is_page(p.c, page)) return false;
-        *off = page * p.c.page_stride + ((int)pos & slot_mask) * p.c.slot_stride;
-        return true;
+        return is_page(p.c, page) ? page * p.c.page_stride + ((int)pos & slot_mask) * p.c.slot_stride : -1;
     };
-    for (int j0 = 0; j0 < kept; j0 += MOVES) {
-        piece_t val[MOVES];
-        int64_t to[MOVES];
-        uint32_t moves = 0;
-#pragma unroll
-        for (int m = 0; m < MOVES; ++m) {
-            const int j = j0 + m;
-            if (j < kept) {
-                const int src = path[j];
-                int64_t from;
-                if (src > j && src < er.rows && place(src, &from) && place(j, &to[m])) {
-                    val[m] = base[from];
-                    moves |= 1u << m;
-                }
+    const int per = heads * p.c.pieces;               // pieces of a row
+    // rows of a batch; a row of more pieces than a workgroup holds goes in parts, each through all rows
+    const int wide_most = min(per, kMoves * kThreads), rows = min(kMoves * kThreads / wide_most, kThreads);
+    __shared__ int64_t s_from[kThreads], s_to[kThreads];   // of the batch's rows; s_from < 0: stays
+    for (int c0 = 0; c0 < per; c0 += wide_most) {
+        const int wide = min(wide_most, per - c0);
+        for (int j0 = 0; j0 < kept; j0 += rows) {
+            const int n_rows = min(rows, kept - j0), n = n_rows * wide;
+            if ((int)threadIdx.x < n_rows) {
+                const int j = j0 + threadIdx.x, src = path[j];
+                const int64_t from = src > j && src < er.rows ? place(src) : -1, to = place(j);
+                s_from[threadIdx.x] = to < 0 ? -1 : from;
+                s_to[threadIdx.x] = to;
             }
-        }
+            __syncthreads();
+            piece_t val[kMoves];
 #pragma unroll
-        for (int m = 0; m < MOVES; ++m)
-            if ((moves >> m) & 1) base[to[m]] = val[m];
+            for (int m = 0; m < kMoves; ++m) {
+                if (m * kThreads >= n) break;
+                const int i = m * kThreads + threadIdx.x;
+                const int j = i / wide, c = c0 + i - j * wide, h = c / p.c.pieces;
+                if (i < n && s_from[j] >= 0) val[m] = base[s_from[j] + h * p.c.head_stride + (c - h * p.c.pieces)];
+            }
+            __syncthreads();                          // (the batch is read)
+#pragma unroll
+            for (int m = 0; m < kMoves; ++m) {
+                if (m * kThreads >= n) break;
+                const int i = m * kThreads + threadIdx.x;
+                const int j = i / wide, c = c0 + i - j * wide, h = c / p.c.pieces;
+                if (i < n && s_from[j] >= 0) base[s_to[j] + h * p.c.head_stride + (c - h * p.c.pieces)] = val[m];
+            }
+            __syncthreads();                          // (and written, before the next one is read)
+        }
     }
 }
 __global__ void __launch_bounds__(kThreads) kv_commit_kernel(const CompactParams p) {
@@ -564,12 +575,17 @@ int32_t dip_kv_compact(const dip_kv_cache* cache, const dip_batch* batch, const 
     int32_t st = validate_kv(cache);
     if (!st) st = validate_batch(batch, true);
     if (st) return st;
-    const CompactParams p = {view_of(cache), view_of(batch), path, keep};
+    CompactParams p = {view_of(cache), view_of(batch), path, keep, 1};
     if (path) {
-        const int64_t lanes = 2 * (int64_t)cache->n_kv_heads * p.c.pieces;
-        if (lanes > (int64_t)65535 * kThreads) return fail(DIP_ERR_UNSUPPORTED, "cache: heads too wide");
-        st = check_hip(launch_timed(kv_move_kernel, dim3(batch->n_batch, cache->n_layers, (unsigned)((lanes + kThreads - 1) / kThreads)),
-                                    dim3(kThreads), (hipStream_t)stream, DIP_KERNEL_KV, p), "kv_move launch");
+        // as many heads to a workgroup as its registers take rows of
+        const int64_t most = (int64_t)p.b.max_rows * p.c.pieces;
+        int64_t heads = kMoves * kThreads / (most > 0 ? most : 1);
+        heads = heads < 1 ? 1 : heads > cache->n_kv_heads ? cache->n_kv_heads : heads;
+        p.heads = (int)heads;
+        const int64_t groups = 2 * ((cache->n_kv_heads + heads - 1) / heads);
+        if (groups > 65535) return fail(DIP_ERR_UNSUPPORTED, "cache: too many heads");
+        st = check_hip(launch_timed(kv_move_kernel, dim3(batch->n_batch, cache->n_layers, (unsigned)groups), dim3(kThreads),
+                                    (hipStream_t)stream, DIP_KERNEL_KV, p), "kv_move launch");
         if (st) return st;
     }
     return check_hip(launch_timed(kv_commit_kernel, dim3(batch->n_batch), dim3(kThreads), (hipStream_t)stream, DIP_KERNEL_KV, p),

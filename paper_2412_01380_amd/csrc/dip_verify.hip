@@ -243,12 +243,13 @@ __global__ void __launch_bounds__(kThreads) verify_walk_kernel(const VerifyParam
     __shared__ double s_waves[kThreads / 64];
     __shared__ double s_lam, s_target;
     __shared__ int s_row, s_chunk, s_found, s_lastpos;
+    const double u_sample = (double)a.u_sample[blockIdx.y];
     const int e = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const EntryRows er = entry_rows(a.b, e);
     uint64_t* ticket = a.tickets + (size_t)e * kTicketStride;
     if (tid < 64) {
-        if (lane == 0) ticket_open(ticket, a.epoch);
         const Walk w = walk<E>(a, er, a.max_kids);
+        if (lane == 0) ticket_open(ticket, a.epoch);  // (behind the walk's loads, which return in order)
         const uint64_t path = __ballot(w.reached);
         const int kept = __popcll(path), last = path ? 63 - __clzll((long long)path) : 0;
         if (blockIdx.x == 0) {
@@ -309,7 +310,7 @@ __global__ void __launch_bounds__(kThreads) verify_walk_kernel(const VerifyParam
             upto = running(p_part);
             total = __shfl(upto, 63);
         }
-        const double target = (double)a.u_sample[e] * total;
+        const double target = u_sample * total;
         const double left = __shfl_up(upto, 1);
         const double before = lane ? left : 0.0;
         const uint64_t past = __ballot(upto > target);
@@ -386,6 +387,9 @@ VerifyPlan plan_verify(const dip_batch* b, int n_vocab, int max_kids) {
     VerifyPlan pl;
     int chunk = (n_vocab + kMaxChunks - 1) / kMaxChunks;
     if (chunk < kMinChunk) chunk = kMinChunk;
+    // twice as much to a workgroup where there are more than the chip holds at a time: every one walks the tree
+    // (64 entries of 128256: 41 us; with 4096 to a workgroup 46, with 16384 and half the workgroups 50)
+    if (chunk == kMinChunk && (int64_t)b->n_batch * ((n_vocab + chunk - 1) / chunk) > 1024) chunk *= 2;
     pl.chunk = (chunk + kPer - 1) / kPer * kPer;
     pl.chunks = (n_vocab + pl.chunk - 1) / pl.chunk;
     const int widest = rows_bound(b) - 1;             // children that one node can have
