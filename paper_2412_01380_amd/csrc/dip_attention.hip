@@ -1,7 +1,8 @@
 // Attention over a paged key/value cache: dip_window_attention, dip_tree_attention.
 //
 // The rows of an entry that share a key/value head -- its tokens or nodes times the query heads of the
-// group -- form blocks of 16, 32 or 64; a workgroup takes a block and a share of the keys that it sees.
+// group -- form blocks of 16, 32 or 64 (attn_rows_kernel), 128 or 256 (attn_block_kernel); a workgroup takes a
+// block and a share of the keys that it sees.
 
 #include <cmath>
 
@@ -11,54 +12,53 @@ namespace dip {
 namespace attn {
 namespace {
 
-#ifndef KW
-#define KW 4
-#define KT 512
-#endif
-constexpr int kWaves = KW;
-constexpr int kRowsTarget = KT;
-constexpr int kThreads = kWaves * 64;
-constexpr int kIds = 1024;                // page numbers of a share, in LDS
 constexpr int kRing = 2;                  // tiles of a wavefront in LDS: one in use, one on its way
+constexpr int kIds = 256;                 // page numbers of a wavefront in LDS at a time
 
-// Every wavefront streams tiles of its own through LDS (no barrier in the loop) and keeps a softmax of its
-// own; they are joined in LDS at the end.
-template <typename E, int D, int NB>
-__global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams p) {
+// WAVES wavefronts, each of which streams tiles of its own through LDS (no barrier in the loop) and keeps a
+// softmax of its own; they are joined in LDS at the end.
+template <typename E, int D, int NB, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64, 1) attn_rows_kernel(const AttnParams p) {
     typedef Geo<E, D> G;
     typedef Core<E, D, NB> C;
+    constexpr int THREADS = WAVES * 64;
     constexpr int KEYS = G::KEYS, TILE = KEYS * G::ROWB, LOADS = TILE / 1024, ROWS = 16 * NB;
     static_assert(TILE % 1024 == 0, "whole loads");
-    __shared__ __align__(1024) char s_ring[kWaves * kRing * 2 * TILE];
-    __shared__ int s_ids[kIds];
+    __shared__ __align__(1024) char s_ring[WAVES * kRing * 2 * TILE];
+    __shared__ int s_ids[WAVES][kIds];
     __shared__ uint64_t s_tree[64];
-    __shared__ float s_m[kWaves][ROWS], s_l[kWaves][ROWS];
+    __shared__ float s_m[WAVES][ROWS], s_l[WAVES][ROWS];
     __shared__ int s_last;
+    __shared__ Unit s_unit;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int split = blockIdx.x % p.splits;
-    const int block = blockIdx.x / p.splits;             // (entry, head, block of rows)
-    const int rb = block % p.row_blocks;
-    const int head = block / p.row_blocks % p.c.n_heads;
-    const int e = block / p.row_blocks / p.c.n_heads;
-
-    const EntryRows er = entry_rows(p.b, e);
-    const int r0 = rb * ROWS, n_rows = min(ROWS, er.rows * p.group - r0);
-    if (n_rows <= 0) return;
-    const int seq = entry_seq(p.b, p.c, e);
-    const int len = seq >= 0 ? min(entry_len(p.c, seq), p.max_len) : 0;
-    Range range = key_range<KEYS>(p, len, er.rows, r0 / p.group, (r0 + n_rows - 1) / p.group);
-    if (seq < 0) range.tiles = 0;
-    const int shares = (range.tiles + p.tiles_per_split - 1) / p.tiles_per_split;
-    const int begin = split * p.tiles_per_split, end = min(range.tiles, begin + p.tiles_per_split);
-    if (begin >= end && split > 0) return;
-
-    // the share's page numbers, `per` of a tile
-    const int per = max(1, KEYS >> p.c.page_shift);
-    page_ids<KEYS, kThreads>(p.c, seq, range, begin, end - begin, per, s_ids);
-    if (shares > 1 && tid == 0) ticket_open(p.tickets + (size_t)block * kTicketStride, p.epoch);
-    if (p.parents && wave == 0) tree_masks(p.parents + er.first, er.rows, s_tree);
+    if (wave == 0) Units<KEYS, ROWS>(p, 2 * WAVES).find(blockIdx.x, &s_unit);
     __syncthreads();
+    const Unit u = uniform(s_unit);
+    if (u.rows == 0) return;
+    const int seq = u.seq, len = u.len, r0 = u.r0, n_rows = u.n_rows, head = u.head;
+    Range range = key_range<KEYS>(p, len, u.rows, r0 / p.group, (r0 + n_rows - 1) / p.group);
+    if (seq < 0) range.tiles = 0;
+    const int shares = u.cut(range.tiles);
+    const int begin = u.share * u.size, end = u.end(range.tiles);
+    if (begin >= end && u.share > 0) return;
+
+    // the wavefront's tiles are begin + wave, + WAVES, ..; the page numbers of the next `span` of them are in LDS
+    constexpr int KEYS_LOG2 = KEYS == 32 ? 5 : 4;
+    const int per_log2 = max(0, KEYS_LOG2 - p.c.page_shift), per = 1 << per_log2, span = min(64, kIds >> per_log2);
+    const int mine = max(0, (end - begin - wave + WAVES - 1) / WAVES);
+    auto tile_of = [&](int i) { return tile_at(range, begin + wave + WAVES * i) * KEYS; };
+    auto ids = [&](int i0) {
+        for (int i = lane; i < min(span, mine - i0) * per; i += 64) {
+            const int at = (tile_of(i0 + (i >> per_log2)) >> p.c.page_shift) + (i & (per - 1));
+            const int page = at < p.c.max_pages ? p.c.table[(size_t)seq * p.c.max_pages + at] : 0;
+            s_ids[wave][i] = (unsigned)page < (unsigned)p.c.n_pages ? page : 0;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    };
+    ids(0);
+    if (p.parents && wave == 0) tree_masks(p.parents + u.first_row, u.rows, s_tree);
+    if (p.parents) __syncthreads();
 
     C core;
     RowSees row[NB];
@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams
         const int t = is ? r / p.group : 0;
         row[nb] = row_sees(p, len, t, s_tree);
         alive[nb] = is && (row[nb].hi > 0 || row[nb].tree);
-        core.load_q(nb, is ? p.q + (int64_t)(er.first + t) * p.q_stride + (int64_t)(head * p.group + r % p.group) * (D * G::ES) : nullptr);
+        core.load_q(nb, is ? p.q + (int64_t)(u.first_row + t) * p.q_stride + (int64_t)(head * p.group + r % p.group) * (D * G::ES) : nullptr);
     }
     Softmax<E, D, NB> soft;
     soft.start(core);
@@ -78,23 +78,24 @@ __global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams
     const char* kbase = p.c.k + p.c.head_stride * head * 16;
     const char* vbase = p.c.v + p.c.head_stride * head * 16;
     const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_offset(s_ring) + wave * (kRing * 2 * TILE));
-    const int mine = max(0, (end - begin - wave + kWaves - 1) / kWaves);
-
     auto fetch = [&](int i) {
-        const int vt = begin + wave + kWaves * i, j0 = tile_at(range, vt) * KEYS;
+        if (i && (i & (span - 1)) == 0) ids(i);
+        const int j0 = tile_of(i);
         const uint32_t to = ring_at + (i & (kRing - 1)) * (2 * TILE);
 #pragma unroll
         for (int x = 0; x < LOADS; ++x) {
-            const int64_t off = piece_offset<G>(p.c, s_ids + (vt - begin) * per, j0, range.end, x);
+            const int64_t off = piece_offset<G>(p.c, s_ids[wave] + (i & (span - 1)) * per, j0, range.end, x);
             load_to_lds(kbase + off, to + x * 1024);
             load_to_lds(vbase + off, to + TILE + x * 1024);
         }
     };
+
     if (mine > 0) fetch(0);
     if (mine > 1) fetch(1);
+    if (shares > 1 && tid == 0) ticket_open(p.tickets + (size_t)u.first * kTicketStride, p.epoch);
     for (int i = 0; i < mine; ++i) {
         if (i + 1 < mine) wait_loads<2 * LOADS>(); else wait_loads<0>();
-        const int j0 = tile_at(range, begin + wave + kWaves * i) * KEYS;
+        const int j0 = tile_of(i);
         const uint32_t tile = ring_at + (i & (kRing - 1)) * (2 * TILE);
         f32x4 s[NB][C::MT];
         core.scores(C::k_base(tile), s);
@@ -130,13 +131,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams
     __syncthreads();                                      // (and every wavefront is done with its tiles)
     constexpr int QUADS = D / 4;
     float* s_o = (float*)s_ring;                          // [wave][row][quad, rotated by the row][4]
-    static_assert(kWaves * ROWS * D * 4 <= (int)sizeof(s_ring), "the joined rows fit the ring");
+    static_assert(WAVES * ROWS * D * 4 <= (int)sizeof(s_ring), "the joined rows fit the ring");
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         const int r = 16 * nb + (lane & 15);
         float top = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, s_m[w][r]);
         const float a = join_weight(s_m[wave][r], top);
 #pragma unroll
         for (int y = 0; y < C::OB; ++y) {
@@ -145,18 +146,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams
         }
     }
     __syncthreads();
-    for (int i = tid; i < n_rows * QUADS; i += kThreads) {
+    for (int i = tid; i < n_rows * QUADS; i += THREADS) {
         const int r = i / QUADS, quad = i % QUADS;
         float top = -INFINITY, l = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, s_m[w][r]);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) l += s_m[w][r] == -INFINITY ? s_l[w][r] : s_l[w][r] * fast_exp2(s_m[w][r] - top);
+        for (int w = 0; w < WAVES; ++w) l += s_m[w][r] == -INFINITY ? s_l[w][r] : s_l[w][r] * fast_exp2(s_m[w][r] - top);
         f32x4 o = {0, 0, 0, 0};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) o += *(const f32x4*)(s_o + ((w * ROWS + r) * QUADS + (quad + r) % QUADS) * 4);
+        for (int w = 0; w < WAVES; ++w) o += *(const f32x4*)(s_o + ((w * ROWS + r) * QUADS + (quad + r) % QUADS) * 4);
         if (shares > 1) {
-            const size_t at = ((size_t)block * p.splits + split) * ROWS + r;
+            const size_t at = (size_t)(u.first + u.share) * ROWS + r;
             share_put(p.part_o + at * D + quad * 4, o);
             if (quad == 0)
                 __hip_atomic_store((uint64_t*)(p.part_ml + at), ((uint64_t)__float_as_uint(l) << 32) | __float_as_uint(top),
@@ -164,15 +165,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_rows_kernel(const AttnParams
         } else {
             const int t = (r0 + r) / p.group, h = head * p.group + (r0 + r) % p.group;
             const f32x4 zero = {0, 0, 0, 0};
-            store_quad<E>(p.out + (int64_t)(er.first + t) * p.out_stride + (int64_t)h * (D * G::ES), quad * 4, l == 0.f ? zero : o * (1.f / l));
+            store_quad<E>(p.out + (int64_t)(u.first_row + t) * p.out_stride + (int64_t)h * (D * G::ES), quad * 4, l == 0.f ? zero : o * (1.f / l));
         }
     }
     if (shares <= 1) return;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (tid == 0) s_last = ticket_last(p.tickets + (size_t)block * kTicketStride, p.epoch, shares);
+    if (tid == 0) s_last = ticket_last(p.tickets + (size_t)u.first * kTicketStride, p.epoch, shares);
     __syncthreads();
-    if (s_last) join_shares<E, D, ROWS, kThreads, true>(p, block, shares, er.first, head, r0, 0, n_rows);
+    if (s_last) join_shares<E, D, ROWS, THREADS, true>(p, u.first, shares, u.first_row, head, r0, 0, n_rows);
 }
 
 // Rows enough to fill the matrix cores: eight wavefronts of 16 NB rows each share the tiles, one barrier a tile.
@@ -195,31 +196,28 @@ __global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const Attn
     __shared__ int s_ids[kIdTiles * KEYS];
     __shared__ uint64_t s_tree[64];
     __shared__ uint32_t s_bad[2][2];
+    __shared__ Unit s_unit;
 
-    // XCD x gets consecutive blocks, so that blocks of one head find its keys in their L2
-    const int per_xcd = (p.grid + 7) / 8, unit = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-    if (unit >= p.grid) return;
+    // XCD x gets consecutive units, so that blocks of one head find its keys in their L2
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int split = unit % p.splits;
-    const int block = unit / p.splits;
-    const int rb = block % p.row_blocks;
-    const int head = block / p.row_blocks % p.c.n_heads;
-    const int e = block / p.row_blocks / p.c.n_heads;
-
-    const EntryRows er = entry_rows(p.b, e);
-    const int r0 = rb * ROWS, n_rows = min(ROWS, er.rows * p.group - r0);
-    if (n_rows <= 0) return;
-    const int seq = entry_seq(p.b, p.c, e);
-    const int len = seq >= 0 ? min(entry_len(p.c, seq), p.max_len) : 0;
-    Range range = key_range<KEYS>(p, len, er.rows, r0 / p.group, (r0 + n_rows - 1) / p.group);
+    if (wave == 0) {
+        const Units<KEYS, ROWS> units(p, 8);
+        const int per_xcd = (units.total + 7) / 8, at = blockIdx.x >> 3;
+        units.find(at < per_xcd ? (int)(blockIdx.x & 7) * per_xcd + at : units.total, &s_unit);
+    }
+    __syncthreads();
+    const Unit u = uniform(s_unit);
+    if (u.rows == 0) return;
+    const int seq = u.seq, len = u.len, r0 = u.r0, n_rows = u.n_rows, head = u.head;
+    Range range = key_range<KEYS>(p, len, u.rows, r0 / p.group, (r0 + n_rows - 1) / p.group);
     if (seq < 0) range.tiles = 0;
-    const int shares = (range.tiles + p.tiles_per_split - 1) / p.tiles_per_split;
-    const int begin = split * p.tiles_per_split, n = max(0, min(range.tiles - begin, p.tiles_per_split));
-    if (n == 0 && split > 0) return;
+    const int shares = u.cut(range.tiles);
+    const int begin = u.share * u.size, n = max(0, u.end(range.tiles) - begin);
+    if (n == 0 && u.share > 0) return;
 
     const int per = max(1, KEYS >> p.c.page_shift);
     page_ids<KEYS, kBlockThreads>(p.c, seq, range, begin, min(n, kIdTiles), per, s_ids);
-    if (p.parents && wave == 0) tree_masks(p.parents + er.first, er.rows, s_tree);
+    if (p.parents && wave == 0) tree_masks(p.parents + u.first_row, u.rows, s_tree);
     if (tid < 4) s_bad[tid >> 1][tid & 1] = 0;
     __syncthreads();
 
@@ -228,7 +226,7 @@ __global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const Attn
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         const int r = w0 + 16 * nb + (lane & 15), t = (r0 + r) / p.group;
-        core.load_q(nb, r < n_rows ? p.q + (int64_t)(er.first + t) * p.q_stride + (int64_t)(head * p.group + (r0 + r) % p.group) * (D * G::ES) : nullptr);
+        core.load_q(nb, r < n_rows ? p.q + (int64_t)(u.first_row + t) * p.q_stride + (int64_t)(head * p.group + (r0 + r) % p.group) * (D * G::ES) : nullptr);
     }
     // what the lane's rows see, worked out where it is asked for rather than kept in registers (`lane` from
     // fresh(): the compiler would keep it all the same)
@@ -310,14 +308,14 @@ __global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const Attn
             soft.step(core, s, p.scale_log2);
             const uint32_t v = C::v_base(tile_of(i) + TILE);
 #pragma unroll
-            for (int u = 0; u < SUB; ++u) {
+            for (int b = 0; b < SUB; ++b) {
                 typename C::Weights w;
                 if (few) {
-                    C::template pack<true>(s, u * C::MT, w);
-                    core.template add_values<true>(v, u * G::KEYS, w);
+                    C::template pack<true>(s, b * C::MT, w);
+                    core.template add_values<true>(v, b * G::KEYS, w);
                 } else {
-                    C::template pack<false>(s, u * C::MT, w);
-                    core.template add_values<false>(v, u * G::KEYS, w);
+                    C::template pack<false>(s, b * C::MT, w);
+                    core.template add_values<false>(v, b * G::KEYS, w);
                 }
             }
         }
@@ -330,12 +328,12 @@ __global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const Attn
         auto weigh = [&]() {
             soft.step(core, s, p.scale_log2);
 #pragma unroll
-            for (int u = 0; u < SUB; ++u) C::template pack<false>(s, u * C::MT, w[u]);
+            for (int b = 0; b < SUB; ++b) C::template pack<false>(s, b * C::MT, w[b]);
         };
         auto values = [&](int i) {
             const uint32_t v = C::v_base(tile_of(i) + TILE);
 #pragma unroll
-            for (int u = 0; u < SUB; ++u) core.template add_values<false>(v, u * G::KEYS, w[u]);
+            for (int b = 0; b < SUB; ++b) core.template add_values<false>(v, b * G::KEYS, w[b]);
         };
         arrive(from);
         scores(from, s);
@@ -368,13 +366,13 @@ __global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const Attn
         const float l = alive ? column_sum(soft.l[nb]) : 0.f;
         if (r >= n_rows) continue;
         if (shares > 1) {
-            const size_t at = ((size_t)block * p.splits + split) * ROWS + r;
+            const size_t at = (size_t)(u.first + u.share) * ROWS + r;
 #pragma unroll
             for (int y = 0; y < C::OB; ++y) *(f32x4*)(p.part_o + at * D + C::quad_dim(y)) = core.quad(nb, y);
             if (lane < 16) p.part_ml[at] = make_float2(alive ? soft.m[nb] : -INFINITY, l);
         } else {
             const int t = (r0 + r) / p.group, h = head * p.group + (r0 + r) % p.group;
-            char* out = p.out + (int64_t)(er.first + t) * p.out_stride + (int64_t)h * (D * G::ES);
+            char* out = p.out + (int64_t)(u.first_row + t) * p.out_stride + (int64_t)h * (D * G::ES);
             const f32x4 zero = {0, 0, 0, 0};
             const float inv = 1.f / l;
 #pragma unroll
@@ -389,100 +387,82 @@ constexpr int kJoinRows = 8;
 template <typename E, int D, int NB>
 __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p) {
     constexpr int ROWS = 16 * NB * kBlockWaves;
+    constexpr int KEYS = kBlockSub * Geo<E, D>::KEYS;
+    __shared__ Unit s_unit;
     const int block = blockIdx.x / (ROWS / kJoinRows), part = blockIdx.x % (ROWS / kJoinRows);
-    const int rb = block % p.row_blocks;
-    const int head = block / p.row_blocks % p.c.n_heads;
-    const int e = block / p.row_blocks / p.c.n_heads;
-    const EntryRows er = entry_rows(p.b, e);
-    const int r0 = rb * ROWS, n_rows = min(ROWS, er.rows * p.group - r0);
-    if (n_rows <= part * kJoinRows) return;
-    const int seq = entry_seq(p.b, p.c, e);
-    if (seq < 0) return;
-    const int len = min(entry_len(p.c, seq), p.max_len);
-    const Range range = key_range<kBlockSub * Geo<E, D>::KEYS>(p, len, er.rows, r0 / p.group, (r0 + n_rows - 1) / p.group);
-    const int shares = (range.tiles + p.tiles_per_split - 1) / p.tiles_per_split;
-    if (shares > 1) join_shares<E, D, ROWS, 256, false>(p, block, shares, er.first, head, r0, part * kJoinRows, min(n_rows, (part + 1) * kJoinRows));
+    const int per_entry = p.row_blocks * p.c.n_heads;
+    if (threadIdx.x < 64) Units<KEYS, ROWS>(p, 8).find_block(block / per_entry, block % per_entry, &s_unit);
+    __syncthreads();
+    const Unit u = uniform(s_unit);
+    if (u.rows == 0 || u.seq < 0 || u.n_rows <= part * kJoinRows) return;
+    const Range range = key_range<KEYS>(p, u.len, u.rows, u.r0 / p.group, (u.r0 + u.n_rows - 1) / p.group);
+    const int shares = u.cut(range.tiles);
+    if (shares > 1)
+        join_shares<E, D, ROWS, 256, false>(p, u.first, shares, u.first_row, u.head, u.r0, part * kJoinRows, min(u.n_rows, (part + 1) * kJoinRows));
 }
 
 // ---- launch plan ----------------------------------------------------------------------------------
 struct Plan {
     bool shared;              // attn_block_kernel
-    int nb, rows, row_blocks, splits, tiles_per_split;
-    int64_t blocks;
+    int nb, rows, waves, row_blocks, slots;
+    int64_t blocks, grid;
+    bool cut;                 // blocks may be cut into shares
     size_t off_ml, off_tickets, total;
 };
 int reach(const dip_kv_cache* c, const dip_batch* b) {
     const int fit = c->max_pages * c->page_size;
     return b->max_len && b->max_len < fit ? b->max_len : fit;
 }
-Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads, int window, int sinks) {
+Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads) {
     Plan pl;
     const int64_t rows = (int64_t)rows_bound(b) * (n_q_heads / c->n_kv_heads);
     // more than 64 rows share tiles; not in fp32, whose products take sixteen times as long and hide any traffic
     pl.shared = rows > 64 && c->dtype == DIP_BF16;
     pl.nb = pl.shared ? (rows <= 16 * kBlockWaves ? 1 : 2) : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     pl.rows = 16 * pl.nb * (pl.shared ? kBlockWaves : 1);
-    const int keys = (c->dtype == DIP_F32 ? 16 : 32) * (pl.shared ? kBlockSub : 1);
     pl.row_blocks = (int)((rows + pl.rows - 1) / pl.rows);
     pl.blocks = (int64_t)b->n_batch * c->n_kv_heads * pl.row_blocks;
-    // most tiles that a block of rows sees
-    int64_t tiles = ((int64_t)reach(c, b) + keys - 1) / keys;
-    if (window) {
-        const int64_t w = ((int64_t)sinks + keys - 1) / keys + ((int64_t)window + rows_bound(b)) / keys + 2;
-        if (w < tiles) tiles = w;
-    }
-    // enough workgroups for the chip, but no share under two tiles a wavefront (eight shared ones), and none
-    // with more page numbers than LDS holds
-    const int64_t want = ((pl.shared ? 768 : kRowsTarget) + pl.blocks - 1) / pl.blocks;
-    int64_t per = (tiles + want - 1) / want;
-    if (per < 8) per = 8;
-    if (!pl.shared) {
-        per = (per + kWaves - 1) / kWaves * kWaves;
-        const int ids = keys / c->page_size > 1 ? keys / c->page_size : 1;
-        if (per > kIds / ids) per = kIds / ids;
-    }
-    pl.tiles_per_split = (int)per;
-    pl.splits = (int)((tiles + per - 1) / per);
-    if (pl.splits < 1) pl.splits = 1;
+    // Four wavefronts to a workgroup, as many workgroups to a compute unit as their rings of tiles leave room for;
+    // where the blocks alone are more than that, two: the start and the end of one workgroup, when it streams
+    // nothing, then lie beside another's middle.
+    const auto fit = [&](int waves) { return 256 * ((160 * 1024 - 1024) / (waves * 256 * c->head_dim + 6144)); };
+    pl.waves = pl.shared ? kBlockWaves : pl.blocks <= fit(4) ? 4 : 2;
+    pl.slots = pl.shared ? 256 : fit(pl.waves);
+    pl.cut = pl.blocks < pl.slots || b->n_batch > 1 || pl.row_blocks > 1;   // (the device may count fewer blocks)
+    pl.grid = pl.blocks > pl.slots ? pl.blocks : pl.slots;
     size_t o = 0;
-    if (pl.splits > 1) {
-        const size_t rows_all = (size_t)pl.blocks * pl.splits * pl.rows;
-        o = align_up(rows_all * c->head_dim * sizeof(float), 256);
-        pl.off_ml = o;
-        o += align_up(rows_all * sizeof(float2), 256);
-        pl.off_tickets = o;
-        if (!pl.shared) o += sizeof(uint64_t) * kTicketStride * (size_t)pl.blocks;
-    } else {
-        pl.off_ml = pl.off_tickets = 0;
-    }
-    pl.total = o < 256 ? 256 : o;
+    // only a cut into at most `slots` units has shares
+    const size_t units = (size_t)pl.slots;
+    o = align_up(units * pl.rows * c->head_dim * sizeof(float), 256);
+    pl.off_ml = o;
+    o += align_up(units * pl.rows * sizeof(float2), 256);
+    pl.off_tickets = o;
+    if (!pl.shared) o += sizeof(uint64_t) * kTicketStride * units;
+    pl.total = o;
     return pl;
 }
 
+template <typename E, int D, int NB>
+hipError_t launch_rows(const AttnParams& p, const Plan& pl, hipStream_t stream) {
+    const dim3 grid((unsigned)p.grid);
+    if (pl.waves == 4) return launch_timed(attn_rows_kernel<E, D, NB, 4>, grid, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
+    return launch_timed(attn_rows_kernel<E, D, NB, 2>, grid, dim3(128), stream, DIP_KERNEL_ATTENTION, p);
+}
+template <int D, int NB>
+hipError_t launch_block(const AttnParams& p, const Plan& pl, hipStream_t stream) {
+    const dim3 grid((unsigned)((p.grid + 7) / 8 * 8)), join((unsigned)(pl.blocks * (pl.rows / kJoinRows)));
+    const hipError_t err = launch_timed(attn_block_kernel<uint16_t, D, NB>, grid, dim3(kBlockThreads), stream, DIP_KERNEL_ATTENTION, p);
+    if (err != hipSuccess || !pl.cut) return err;
+    return launch_timed(attn_join_kernel<uint16_t, D, NB>, join, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
+}
 template <typename E, int D>
 int32_t launch(const AttnParams& p, const Plan& pl, hipStream_t stream) {
     hipError_t err;
-    const dim3 grid((unsigned)p.grid), block(kThreads);
-    if (pl.shared) {
-        if constexpr (sizeof(E) == 2) {
-            const dim3 bgrid((unsigned)((p.grid + 7) / 8 * 8)), bblock(kBlockThreads);
-            if (pl.nb == 1) err = launch_timed(attn_block_kernel<E, D, 1>, bgrid, bblock, stream, DIP_KERNEL_ATTENTION, p);
-            else err = launch_timed(attn_block_kernel<E, D, 2>, bgrid, bblock, stream, DIP_KERNEL_ATTENTION, p);
-            if (err == hipSuccess && pl.splits > 1) {
-                const dim3 join((unsigned)(pl.blocks * (pl.rows / kJoinRows)));
-                if (pl.nb == 1) err = launch_timed(attn_join_kernel<E, D, 1>, join, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
-                else err = launch_timed(attn_join_kernel<E, D, 2>, join, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
-            }
-        } else {
-            return fail(DIP_ERR_UNSUPPORTED, "attention: no launch for this shape");
-        }
-    } else if (pl.nb == 1) {
-        err = launch_timed(attn_rows_kernel<E, D, 1>, grid, block, stream, DIP_KERNEL_ATTENTION, p);
-    } else if (pl.nb == 2) {
-        err = launch_timed(attn_rows_kernel<E, D, 2>, grid, block, stream, DIP_KERNEL_ATTENTION, p);
-    } else {
-        err = launch_timed(attn_rows_kernel<E, D, 4>, grid, block, stream, DIP_KERNEL_ATTENTION, p);
-    }
+    if constexpr (sizeof(E) == 2)
+        if (pl.shared) return check_hip(pl.nb == 1 ? launch_block<D, 1>(p, pl, stream) : launch_block<D, 2>(p, pl, stream), "attention launch");
+    if (pl.nb == 1) err = launch_rows<E, D, 1>(p, pl, stream);
+    else if (pl.nb == 2) err = launch_rows<E, D, 2>(p, pl, stream);
+    else err = launch_rows<E, D, 4>(p, pl, stream);
     return check_hip(err, "attention launch");
 }
 template <typename E>
@@ -504,8 +484,8 @@ int32_t check_attention(const dip_kv_cache* c, const dip_batch* b, int32_t n_q_h
     if (window < 0 || sinks < 0) return fail(DIP_ERR_INVALID_ARG, "attention: window and sinks must be >= 0");
     const int64_t rows = (int64_t)rows_bound(b) * (n_q_heads / c->n_kv_heads);
     if (rows >= 1 << 30) return fail(DIP_ERR_UNSUPPORTED, "attention: too many rows of one entry");
-    const Plan pl = plan_attention(c, b, n_q_heads, window, sinks);
-    if (pl.blocks * (pl.splits > 32 ? pl.splits : 32) >= (int64_t)1 << 30) return fail(DIP_ERR_UNSUPPORTED, "attention: too many rows for one call");
+    const Plan pl = plan_attention(c, b, n_q_heads);
+    if (pl.blocks * 32 >= (int64_t)1 << 31) return fail(DIP_ERR_UNSUPPORTED, "attention: too many rows for one call");
     return DIP_OK;
 }
 
@@ -522,7 +502,7 @@ int32_t attend(const dip_kv_cache* c, int32_t layer, const dip_batch* b, const i
     if (q_stride < width || out_stride < width) return fail(DIP_ERR_INVALID_ARG, "attention: strides smaller than a row");
     if (q_stride * es % 16 || out_stride * es % 16 || !aligned16(q) || !aligned16(out))
         return fail(DIP_ERR_UNSUPPORTED, "attention: rows of q and out must start on 16-byte boundaries");
-    const Plan pl = plan_attention(c, b, n_q_heads, window, sinks);
+    const Plan pl = plan_attention(c, b, n_q_heads);
     st = validate_ws(ws, ws_bytes, pl.total);
     if (st) return st;
     AttnParams p;
@@ -541,14 +521,13 @@ int32_t attend(const dip_kv_cache* c, int32_t layer, const dip_batch* b, const i
     p.window = window;
     p.sinks = sinks;
     p.max_len = reach(c, b);
-    p.splits = pl.splits;
-    p.tiles_per_split = pl.tiles_per_split;
+    p.slots = pl.slots;
+    p.grid = (int)pl.grid;
     p.row_blocks = pl.row_blocks;
-    p.grid = (int)(pl.blocks * pl.splits);
     p.part_o = (float*)ws;
     p.part_ml = (float2*)((char*)ws + pl.off_ml);
     p.tickets = (uint64_t*)((char*)ws + pl.off_tickets);
-    p.epoch = pl.splits > 1 ? next_epoch() : 0;
+    p.epoch = next_epoch();
     return c->dtype == DIP_F32 ? launch_dim<float>(p, pl, c->head_dim, (hipStream_t)stream)
                                : launch_dim<uint16_t>(p, pl, c->head_dim, (hipStream_t)stream);
 }
@@ -563,7 +542,7 @@ extern "C" {
 
 size_t dip_attention_workspace_bytes(const dip_kv_cache* cache, const dip_batch* batch, int32_t n_q_heads, int32_t window, int32_t sinks) {
     if (attn::check_attention(cache, batch, n_q_heads, window, sinks)) return 0;
-    return attn::plan_attention(cache, batch, n_q_heads, window, sinks).total;
+    return attn::plan_attention(cache, batch, n_q_heads).total;
 }
 
 int32_t dip_window_attention(const dip_kv_cache* cache, int32_t layer, const dip_batch* batch, const void* q, int64_t q_stride,

@@ -11,6 +11,8 @@
 #ifndef DIP_ATTN_DEVICE_H_
 #define DIP_ATTN_DEVICE_H_
 
+#include <type_traits>
+
 #include "dip_decode_internal.h"
 
 namespace dip {
@@ -39,13 +41,12 @@ struct AttnParams {
     int window;               // 0: no bound
     int sinks;
     int max_len;
-    int splits;               // shares that a row block's keys are cut into
-    int tiles_per_split;
-    int row_blocks;           // of an entry and key/value head
-    int grid;                 // row blocks times splits
-    float* part_o;            // [row block][split][rows of a block][D], not normalised
-    float2* part_ml;          // [row block][split][rows of a block]: maximum (times scale_log2), sum
-    uint64_t* tickets;        // a word per row block, kTicketStride apart, whatever they hold
+    int slots;                // workgroups that the chip holds at a time, or what to pretend it does
+    int grid;                 // most units there can be
+    int row_blocks;           // most blocks of rows of an entry and key/value head
+    float* part_o;            // [unit][rows of a block][D], not normalised
+    float2* part_ml;          // [unit][rows of a block]: maximum (times scale_log2), sum
+    uint64_t* tickets;        // a word per unit, kTicketStride apart, whatever they hold
     uint64_t epoch;           // this launch's tag in them
 };
 
@@ -137,11 +138,185 @@ __device__ __forceinline__ RowSees row_sees(const AttnParams& p, int len, int t,
     return r;
 }
 
-// The page numbers of `tiles` tiles from virtual tile `from` on, `per` of each, by the whole workgroup
-// (numbers that are none become page 0).
+// ---- units of work ---------------------------------------------------------------------------
+// A unit is a block of rows (of an entry and key/value head) and a share of the tiles that it sees.  How long the
+// sequences are is known on the device alone, so every workgroup cuts the work up for itself, all alike:
+// shares of `size` tiles, the smallest size that makes no more units than the chip holds at a time -- one
+// round, of units as alike as can be whatever the lengths.  (With blocks enough for that, a block is a unit.)
+struct Unit {
+    int entry, first_row, rows, seq, len;      // rows == 0: no unit
+    int head, r0, n_rows;                      // its rows: r0 .. r0 + n_rows - 1 of rows x group
+    int first;                                 // unit of the block's first share
+    int share, shares, size;                   // this one begins at tile share * size, the last takes all that is left
+    // how many shares a block that sees `tiles` tiles is cut into, and where this one ends
+    __device__ __forceinline__ int cut(int tiles) const { return min(shares, (tiles + size - 1) / size); }
+    __device__ __forceinline__ int end(int tiles) const { return share + 1 >= cut(tiles) ? tiles : min(tiles, (share + 1) * size); }
+};
+// (the same for all lanes: into scalar registers)
+__device__ __forceinline__ Unit uniform(const Unit& u) {
+    Unit x;
+    constexpr int N = sizeof(Unit) / sizeof(int);
+    int raw[N];
+    __builtin_memcpy(raw, &u, sizeof(u));
+#pragma unroll
+    for (int i = 0; i < N; ++i) raw[i] = __builtin_amdgcn_readfirstlane(raw[i]);
+    __builtin_memcpy(&x, raw, sizeof(x));
+    return x;
+}
+template <int KEYS, int ROWS>
+struct Units {
+    struct Entry {
+        int first, rows, seq, len, row_blocks, blocks, tiles;
+    };
+    const AttnParams& p;
+    Entry cached;
+    int size;
+    float per_size;
+    int total;
+    __device__ __forceinline__ Entry entry(int e) const {
+        Entry x = {0, 0, -1, 0, 0, 0, 0};
+        if (e >= p.b.n_batch) return x;
+        const EntryRows er = entry_rows(p.b, e);
+        x.first = er.first;
+        x.rows = er.rows;
+        x.seq = entry_seq(p.b, p.c, e);
+        x.len = x.seq >= 0 ? min(entry_len(p.c, x.seq), p.max_len) : 0;
+        const int all = er.rows * p.group;
+        x.row_blocks = (all + ROWS - 1) / ROWS;
+        x.blocks = x.row_blocks * p.c.n_heads;
+        if (all > 0) {            // (about as many as any of its blocks sees; one that sees nothing is a unit all the same)
+            const Range r = key_range<KEYS>(p, x.len, er.rows, max(0, all - ROWS) / p.group, er.rows - 1);
+            x.tiles = x.seq >= 0 ? max(1, r.tiles) : 1;
+        }
+        return x;
+    }
+    __device__ __forceinline__ Entry at(int chunk) const { return chunk == 0 ? cached : entry(chunk * 64 + (int)(threadIdx.x & 63)); }
+    // (a share more or less does not matter, as long as everybody says the same: the last one takes what is left)
+    __device__ __forceinline__ int shares_of(const Entry& x) const { return max(1, (int)ceilf((float)x.tiles * per_size)); }
+    __device__ __forceinline__ int units_of(const Entry& x) const { return x.blocks * shares_of(x); }
+    // running sums over the lanes in data-parallel moves within rows of 16, then the rows' sums by scalar
+    __device__ __forceinline__ static int running(int x) {
+        x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);      // row_shr 1, 2, 4, 8
+        x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+        x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+        const int a = __builtin_amdgcn_readlane(x, 15), b = __builtin_amdgcn_readlane(x, 31), c = __builtin_amdgcn_readlane(x, 47);
+        const int row = (threadIdx.x & 63) >> 4;
+        return x + (row > 0 ? a : 0) + (row > 1 ? b : 0) + (row > 2 ? c : 0);
+    }
+    __device__ __forceinline__ static int sum(int x) { return __builtin_amdgcn_readlane(running(x), 63); }
+    __device__ __forceinline__ static float sum_of(float x) {
+        const auto from = [](float y, auto ctrl) {
+            return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), decltype(ctrl)::value, 0xf, 0xf, true));
+        };
+        x += from(x, std::integral_constant<int, 0x111>());
+        x += from(x, std::integral_constant<int, 0x112>());
+        x += from(x, std::integral_constant<int, 0x114>());
+        x += from(x, std::integral_constant<int, 0x118>());
+        const auto row = [&](int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane)); };
+        return (row(15) + row(31)) + (row(47) + row(63));
+    }
+    __device__ __forceinline__ static int least_of(int x) {
+        x = min(x, __builtin_amdgcn_update_dpp(x, x, 0x111, 0xf, 0xf, false));
+        x = min(x, __builtin_amdgcn_update_dpp(x, x, 0x112, 0xf, 0xf, false));
+        x = min(x, __builtin_amdgcn_update_dpp(x, x, 0x114, 0xf, 0xf, false));
+        x = min(x, __builtin_amdgcn_update_dpp(x, x, 0x118, 0xf, 0xf, false));
+        return min(min(__builtin_amdgcn_readlane(x, 15), __builtin_amdgcn_readlane(x, 31)),
+                   min(__builtin_amdgcn_readlane(x, 47), __builtin_amdgcn_readlane(x, 63)));
+    }
+    // one wavefront; all its lanes get the answer
+    __device__ __forceinline__ Units(const AttnParams& params, int least) : p(params) {
+        cached = entry(threadIdx.x & 63);
+        const int chunks = (p.b.n_batch + 63) / 64;
+        float work = 0.f;                                  // (the same bits for everybody: that is all it takes)
+        int most = -1;
+        total = 0;
+        for (int c = 0; c < chunks; ++c) {
+            const Entry x = at(c);
+            total += sum(x.blocks);
+            most = max(most, -least_of(-x.tiles));
+            work += sum_of((float)x.blocks * (float)x.tiles);
+        }
+        whole(max(1, most));
+        if (total >= p.slots) return;
+        int next = max(least, (int)(work / (float)p.slots));
+        while (next < most) {
+            set(next);
+            // the units there would be, and the next size at which some entry has a share less
+            int units = 0, step = most;
+            for (int c = 0; c < chunks; ++c) {
+                const Entry x = at(c);
+                units += sum(units_of(x));
+                const int k = shares_of(x);
+                step = min(step, least_of(k > 1 ? (int)ceilf((float)x.tiles / (float)(k - 1)) : most));
+            }
+            if (units <= p.slots) {
+                total = units;
+                return;
+            }
+            next = max(next + 1 + (next >> 5), step);
+        }
+        whole(max(1, most));
+    }
+    __device__ __forceinline__ void set(int n) {
+        size = n;
+        per_size = 1.f / (float)n;
+    }
+    __device__ __forceinline__ void whole(int most) {      // every block one unit, to the letter
+        size = most;
+        per_size = 0.f;
+    }
+    // the unit `w`, or the first one of block `b` of entry `e`
+    __device__ __forceinline__ void find(int w, Unit* out) const {
+        const int lane = threadIdx.x & 63;
+        int before = 0;
+        for (int c = 0; c * 64 < p.b.n_batch; ++c) {
+            const Entry x = at(c);
+            const int upto = running(units_of(x));
+            const int mine = before + upto - units_of(x);
+            if (w >= mine && w < before + upto) fill(x, c * 64 + lane, mine, w - mine, out);
+            before += __builtin_amdgcn_readlane(upto, 63);
+            if (w < before) return;
+        }
+        if (lane == 0) out->rows = 0;
+    }
+    __device__ __forceinline__ void find_block(int e, int block, Unit* out) const {
+        const int lane = threadIdx.x & 63;
+        int before = 0;
+        for (int c = 0; c * 64 <= e; ++c) {
+            const Entry x = at(c);
+            const int mine = c * 64 + lane < e ? units_of(x) : 0;
+            before += sum(mine);
+            if (c * 64 + lane == e) {
+                const int shares = shares_of(x);
+                if (block < x.blocks) fill(x, e, -1, block * shares, out);
+                else out->rows = 0;
+            }
+        }
+        if (lane == (e & 63) && out->rows) out->first += before + 1;
+    }
+    __device__ __forceinline__ void fill(const Entry& x, int e, int at_unit, int local, Unit* out) const {
+        const int shares = shares_of(x), block = local / shares;
+        out->entry = e;
+        out->first_row = x.first;
+        out->rows = x.rows;
+        out->seq = x.seq;
+        out->len = x.len;
+        out->head = block / x.row_blocks;
+        out->r0 = (block - out->head * x.row_blocks) * ROWS;
+        out->n_rows = min(ROWS, x.rows * p.group - out->r0);
+        out->first = at_unit + block * shares;
+        out->share = local - block * shares;
+        out->shares = shares;
+        out->size = size;
+    }
+};
+
+// The page numbers of `tiles` tiles from virtual tile `from` on, `per` of each, by the threads of a workgroup or
+// of a wavefront (numbers that are none become page 0).
 template <int KEYS, int THREADS>
 __device__ __forceinline__ void page_ids(const KvView& c, int seq, const Range& range, int from, int tiles, int per, int* ids) {
-    for (int i = threadIdx.x; i < tiles * per; i += THREADS) {
+    for (int i = threadIdx.x & (THREADS - 1); i < tiles * per; i += THREADS) {
         const int vt = i / per;
         const int at = ((tile_at(range, from + vt) * KEYS) >> c.page_shift) + (i - vt * per);
         const int page = at < c.max_pages ? c.table[(size_t)seq * c.max_pages + at] : 0;
@@ -536,9 +711,9 @@ __device__ __forceinline__ float2 share_get(const float* from) {
     else return *(const float2*)from;
 }
 template <typename E, int D, int ROWS, int THREADS, bool AGENT>
-__device__ __forceinline__ void join_shares(const AttnParams& p, int block, int shares, int first_row, int head, int r0, int from, int to) {
+__device__ __forceinline__ void join_shares(const AttnParams& p, int first, int shares, int first_row, int head, int r0, int from, int to) {
     constexpr int QUADS = D / 4, FLIGHT = 4;
-    const size_t base = (size_t)block * p.splits * ROWS;
+    const size_t base = (size_t)first * ROWS;
     for (int i = threadIdx.x; i < (to - from) * QUADS; i += THREADS) {
         const int r = from + i / QUADS, quad = i % QUADS;
         // running maximum over the shares, FLIGHT of them on their way at a time
