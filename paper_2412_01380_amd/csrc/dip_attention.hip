@@ -406,7 +406,7 @@ struct Plan {
     bool shared;              // attn_block_kernel
     int nb, rows, waves, row_blocks, slots;
     int64_t blocks, grid;
-    bool cut;                 // blocks may be cut into shares
+    bool cut;                 // blocks may be cut into shares (slots > 0)
     size_t off_ml, off_tickets, total;
 };
 int reach(const dip_kv_cache* c, const dip_batch* b) {
@@ -428,17 +428,20 @@ Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads) {
     const auto fit = [&](int waves) { return 256 * ((160 * 1024 - 1024) / (waves * 256 * c->head_dim + 6144)); };
     pl.waves = pl.shared ? kBlockWaves : pl.blocks <= fit(4) ? 4 : 2;
     pl.slots = pl.shared ? 256 : fit(pl.waves);
-    pl.cut = pl.blocks < pl.slots || b->n_batch > 1 || pl.row_blocks > 1;   // (the device may count fewer blocks)
+    // attn_block_kernel's shares are joined by a launch of its own, which costs 10 us even where there turn out to
+    // be none: with far more blocks than the chip holds at a time none are made
+    pl.cut = !pl.shared || pl.blocks < 4 * pl.slots;
+    if (!pl.cut) pl.slots = 0;
     pl.grid = pl.blocks > pl.slots ? pl.blocks : pl.slots;
     size_t o = 0;
-    // only a cut into at most `slots` units has shares
+    // (only a cut into at most `slots` units has shares)
     const size_t units = (size_t)pl.slots;
     o = align_up(units * pl.rows * c->head_dim * sizeof(float), 256);
     pl.off_ml = o;
     o += align_up(units * pl.rows * sizeof(float2), 256);
     pl.off_tickets = o;
     if (!pl.shared) o += sizeof(uint64_t) * kTicketStride * units;
-    pl.total = o;
+    pl.total = o < 256 ? 256 : o;
     return pl;
 }
 

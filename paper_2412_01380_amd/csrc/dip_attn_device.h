@@ -712,7 +712,7 @@ __device__ __forceinline__ float2 share_get(const float* from) {
 }
 template <typename E, int D, int ROWS, int THREADS, bool AGENT>
 __device__ __forceinline__ void join_shares(const AttnParams& p, int first, int shares, int first_row, int head, int r0, int from, int to) {
-    constexpr int QUADS = D / 4, FLIGHT = 4;
+    constexpr int QUADS = D / 4, FLIGHT = 8;
     const size_t base = (size_t)first * ROWS;
     for (int i = threadIdx.x; i < (to - from) * QUADS; i += THREADS) {
         const int r = from + i / QUADS, quad = i % QUADS;
