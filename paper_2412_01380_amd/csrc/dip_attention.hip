@@ -113,6 +113,7 @@ __global__ void __launch_bounds__(WAVES * 64, 1) attn_rows_kernel(const AttnPara
         typename C::Weights w;
         C::template pack<true>(s, 0, w);
         core.template add_values<true>(C::v_base(tile + TILE), 0, w);
+        C::schedule_values();
         if (i + kRing < mine) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (everything read from the tile that goes)
             fetch(i + kRing);
@@ -418,7 +419,8 @@ Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads) {
     const int64_t rows = (int64_t)rows_bound(b) * (n_q_heads / c->n_kv_heads);
     // more than 64 rows share tiles; not in fp32, whose products take sixteen times as long and hide any traffic
     pl.shared = rows > 64 && c->dtype == DIP_BF16;
-    pl.nb = pl.shared ? (rows <= 16 * kBlockWaves ? 1 : 2) : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    pl.nb = pl.shared ? (rows <= 16 * kBlockWaves ? 1 : 2) : rows <= 16 ? 1 : rows <= 32 || (c->dtype == DIP_F32 && c->head_dim == 128) ? 2 : 4;
+    // (fp32 at 128 dims: four blocks of 16 rows do not fit the registers)
     pl.rows = 16 * pl.nb * (pl.shared ? kBlockWaves : 1);
     pl.row_blocks = (int)((rows + pl.rows - 1) / pl.rows);
     pl.blocks = (int64_t)b->n_batch * c->n_kv_heads * pl.row_blocks;
@@ -465,7 +467,8 @@ int32_t launch(const AttnParams& p, const Plan& pl, hipStream_t stream) {
         if (pl.shared) return check_hip(pl.nb == 1 ? launch_block<D, 1>(p, pl, stream) : launch_block<D, 2>(p, pl, stream), "attention launch");
     if (pl.nb == 1) err = launch_rows<E, D, 1>(p, pl, stream);
     else if (pl.nb == 2) err = launch_rows<E, D, 2>(p, pl, stream);
-    else err = launch_rows<E, D, 4>(p, pl, stream);
+    else if constexpr (sizeof(E) == 2 || D < 128) err = launch_rows<E, D, 4>(p, pl, stream);
+    else return fail(DIP_ERR_UNSUPPORTED, "attention: no kernel for this shape");
     return check_hip(err, "attention launch");
 }
 template <typename E>

@@ -510,6 +510,18 @@ struct Core<uint16_t, D, NB> {
         }
         __builtin_amdgcn_sched_group_barrier(0x8, FLIGHT * NB, 0);
     }
+    // Behind a tile's second product with TWO terms alone.
+    __device__ __forceinline__ static void schedule_values() {
+        constexpr int FLIGHT = 4;
+#pragma unroll
+        for (int f = 0; f < FLIGHT; ++f) __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+#pragma unroll
+        for (int f = FLIGHT; f < OB; ++f) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 2 * NB, 1);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x8, 2 * FLIGHT * NB, 1);
+    }
     // first dim of the four that o[nb][x] .. hold: quad y of them, y < OB
     __device__ __forceinline__ static int quad_dim(int y) { return 16 * y + 4 * ((threadIdx.x & 63) >> 4); }
     __device__ __forceinline__ f32x4 quad(int nb, int y) const { return o[nb][y]; }
@@ -591,6 +603,7 @@ struct Core<float, D, NB> {
     }
     template <int SUB>
     __device__ __forceinline__ static void schedule_products() {}
+    __device__ __forceinline__ static void schedule_values() {}
     // o[nb][b * VE + e][i] is dim 16 VE b + VE (4 g + i) + e: four neighbours are e = 0 .. 3 of one i, or
     // e = 0, 1 of two
     __device__ __forceinline__ static int quad_dim(int y) {

@@ -557,3 +557,111 @@ def test_compact_many_rows_and_strided_new_rows():
         for j, src in enumerate(paths[e]):
             pg, sl = table[j // 16], j % 16
             assert torch.equal(k[:, pg, :, sl], k_new[:, first + src]) and torch.equal(v[:, pg, :, sl], v_new[:, first + src])
+
+
+# ---- shares, large batches, long tables --------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_batches_of_more_entries_than_a_wavefront_has_lanes(dtype):
+    rng = np.random.default_rng(6)
+    lens = [int(x) for x in rng.integers(0, 300, 150)]
+    lens[70], lens[149] = 2600, 1500
+    rows = [int(x) for x in rng.integers(0, 4, 150)]
+    rows[0], rows[70], rows[149] = 0, 2, 3
+    s = Setup(dtype, lens, rows, 2, 1, 64, 16, seed=4)
+    for window, sinks in [(0, 0), (200, 5)]:
+        s.check(s.run(window, sinks), window, sinks)
+    par = [random_tree(rng, n) for n in rows]
+    s.check(s.run(0, 0, par), 0, 0, par)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,page", [(128, 16), (96, 64), (64, 1)])
+def test_wide_trees_in_shares(dtype, d, page):
+    rng = np.random.default_rng(d)
+    s = Setup(dtype, [3000, 700], [64, 50], 8, 2, d, page, seed=d)
+    par = [random_tree(rng, 64, absent=True), random_tree(rng, 50)]
+    for window, sinks in [(0, 0), (1500, 70)]:
+        s.check(s.run(window, sinks, par), window, sinks, par)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 96, 128])
+def test_pieces_of_prompts(dtype, d):
+    s = Setup(dtype, [1500, 0, 64], [200, 150, 129], 4, 2, d, 32, slot_major=True, seed=d)
+    for window, sinks in [(0, 0), (500, 70), (600, 1), (64, 0), (3, 100)]:
+        s.check(s.run(window, sinks), window, sinks)
+
+
+@pytest.mark.parametrize("page", [1, 8])
+def test_one_token_over_many_small_pages(page):
+    s = Setup("bf16", [9000, 4097], [1, 2], 4, 1, 128, page, seed=3)
+    s.check(s.run())
+
+
+def test_prompts_where_something_is_not_finite():
+    clean = Setup("bf16", [900], [130], 8, 2, 128, 16, seed=8)
+    ref = clean.run(700, 4)
+    s = Setup("bf16", [900], [130], 8, 2, 128, 16, seed=8)
+    for pos in (10, 150, 200):                       # in front of every row's window
+        s.put(0, pos, NAN)
+    assert torch.equal(s.run(700, 4), ref)
+    s.put(0, 960, math.inf)                          # row 60: seen by the rows from there on
+    out = s.run(700, 4)
+    assert torch.equal(out[:60], ref[:60])
+    assert not torch.isfinite(out[60:].float()).all(-1).any()
+    s.put(0, 960, float(s.k[0][959, 0, 0]))
+    s.put(0, 600, NAN, "v")                          # seen by all of them: in whole tiles it goes where it belongs
+    out = s.run(700, 4)
+    assert torch.isnan(out.float()).all()
+
+
+def test_shares_of_wide_trees_in_a_graph():
+    s = Setup("bf16", [2500, 40], [40, 33], 8, 2, 128, 16, seed=2)
+    rng = np.random.default_rng(0)
+    par = [random_tree(rng, n) for n in s.rows]
+    q, out, ws = s.q.cuda(), torch.empty(73, 8, 128, dtype=torch.bfloat16, device="cuda"), workspace(64 << 20)
+    parents = ints([x for p in par for x in p])
+    import paper_2412_01380_amd as D
+    call = lambda o: D.dip_tree_attention(s.cache, 1, s.batch, parents, q, 0.1, 0, 0, o, ws)
+    call(out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out)
+    for n in (2500, 100, 1800, 0):
+        s.cache.seq_len[s.seqs[0]] = n
+        eager = torch.empty_like(out)
+        call(eager)
+        out.fill_(NAN)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
+
+
+def test_verify_in_a_graph_and_many_entries():
+    import paper_2412_01380_amd as D
+    rng = np.random.default_rng(5)
+    trees = [random_tree(rng, int(n)) for n in rng.integers(1, 9, 90)]
+    p, q, tokens, u, us = verify_inputs(rng, trees, 5000)
+    check_verify(trees, p, q, tokens, u, us, 3)
+    rows = [len(t) for t in trees]
+    b = D.Batch(starts(rows), sum(rows), max(rows))
+    keep, path, token = (torch.zeros(m, dtype=torch.int32, device="cuda") for m in (90, sum(rows), 90))
+    ws = workspace(D.dip_verify_tree_workspace_bytes(b, 5000, 3))
+    args = (ints(tokens), ints([x for t in trees for x in t]), p.cuda(), q.cuda(), torch.from_numpy(u).cuda(),
+            torch.from_numpy(us).cuda())
+    call = lambda: D.dip_verify_tree(b, *args, 3, keep, path, token, ws)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in range(4):
+        args[4].copy_(torch.from_numpy(rng.random(sum(rows)).astype(np.float32)))
+        call()
+        eager = [t.clone() for t in (keep, path, token)]
+        for t in (keep, path, token):
+            t.fill_(-5)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, (keep, path, token)))
