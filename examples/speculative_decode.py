@@ -48,10 +48,12 @@ class Decoder:
         self.window, self.sinks, self.dtype = window, sinks, dtype
         self.k_in, self.k_mid = max(1, int(keep * d)), max(1, int(keep * d_ff))
         self.emb = normal(vocab, d)
+        # what a token leads to on its own: a fixed successor, more or less
+        self.unemb = self.emb[torch.randperm(vocab, generator=g, device="cuda")] + normal(vocab, d, scale=0.5)
         self.qkv = [normal(d, (heads + 2 * kv_heads) * head_dim, scale=d ** -0.5) for _ in range(layers)]
-        self.proj = [normal(d, d, scale=0.8 * d ** -0.5) for _ in range(layers)]
+        self.proj = [normal(d, d, scale=2.0 * d ** -0.5) for _ in range(layers)]
         self.mlps = [D.Mlp(D.Weight(normal(d, 2 * d_ff, scale=d ** -0.5).bfloat16()),
-                           D.Weight(normal(d_ff, d, scale=0.8 * d_ff ** -0.5).bfloat16())) for _ in range(layers)]
+                           D.Weight(normal(d_ff, d, scale=2.0 * d_ff ** -0.5).bfloat16())) for _ in range(layers)]
         pages = n_seqs * max_tokens // page
         kv = lambda: torch.empty(layers, pages, kv_heads, page, head_dim, dtype=dtype, device="cuda")
         self.cache = D.KvCache(kv(), kv(), ints([[0] * (max_tokens // page)] * n_seqs), ints([0] * n_seqs), ints([0] * pages))
@@ -95,11 +97,11 @@ class Decoder:
                 D.dip_swiglu_mlp_forward_batched(mlp, h[r:r + b], b, self.k_in, self.k_mid, None, None, 1.0, y[r:r + b], None,
                                                  None, None, self.mlp_ws)
             x = x + y
-        return norm(x) @ self.emb.t() * self.d ** -0.5 * 4.0
+        return norm(x) @ self.unemb.t() * (9.0 / self.d)
 
     def draft_logits(self, token):
         """The drafter: the model without its layers."""
-        return torch.nn.functional.rms_norm(self.emb[token], (self.d,)) @ self.emb.t() * self.d ** -0.5 * 4.0
+        return torch.nn.functional.rms_norm(self.emb[token], (self.d,)) @ self.unemb.t() * (9.0 / self.d)
 
 
 def probabilities(logits, greedy):

@@ -323,6 +323,10 @@ __global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const Attn
     };
     // the others: the second product lags one tile behind the first, so that both are at hand together
     auto middle = [&](int from, int to) {
+        if (w0 >= n_rows) {                               // a wavefront without rows keeps the others' time
+            for (int i = from; i < to; ++i) arrive(i);
+            return;
+        }
         if (from >= to) return;
         f32x4 s[NB][Q];
         typename C::Weights w[SUB];

@@ -124,12 +124,19 @@ __device__ __forceinline__ void chunk_sums(const VerifyParams& a, int row, doubl
     *all = sp;
 }
 
-// G_j (j >= 1) of a row: its chunks' sums, added in order
+// G_j (j >= 1) of a row, by a wavefront: a lane takes a chunk's sum, all get theirs
 __device__ __forceinline__ double g_of(const VerifyParams& a, int j, int row) {
-    const double* part = a.g_part + ((size_t)(j - 1) * a.b.n_rows + row) * a.chunks;
-    double s = 0.0;
-    for (int c = 0; c < a.chunks; ++c) s += part[c];
-    return s;
+    const int lane = threadIdx.x & 63;
+    return wave_sum(lane < a.chunks ? a.g_part[((size_t)(j - 1) * a.b.n_rows + row) * a.chunks + lane] : 0.0);
+}
+// lam and G behind `k` refused children of a row, by a wavefront
+__device__ __forceinline__ void behind(const VerifyParams& a, int k, int row, double* lam, double* G) {
+    *lam = 0.0;
+    *G = 1.0;
+    for (int j = 1; j <= k; ++j) {
+        *lam += *G;
+        *G = g_of(a, j, row);
+    }
 }
 
 // One wavefront, lane t for node t: which children are taken, as far as G_1 .. G_{known} say.
@@ -172,15 +179,19 @@ __device__ __forceinline__ Walk walk(const VerifyParams& a, const EntryRows& er,
             open |= __ballot(mine);
             continue;
         }
-        bool take = false;
-        if (mine && fits) {
-            double lam = 0.0, G = 1.0;
-            for (int j = 1; j <= k; ++j) {
-                lam += G;
-                G = g_of(a, j, up);
+        double lam = 0.0, G = 1.0;
+        if (k > 0) {                                  // (the same for all lanes: the nodes one after the other)
+            for (uint64_t left = __ballot(mine); left; left &= left - 1) {
+                const int t = __ffsll((unsigned long long)left) - 1;
+                double l, g;
+                behind(a, k, __builtin_amdgcn_readlane(up, t), &l, &g);
+                if (lane == t) {
+                    lam = l;
+                    G = g;
+                }
             }
-            take = u * (double)qv * G < weight(pv, qv, lam);
         }
+        const bool take = mine && fits && u * (double)qv * G < weight(pv, qv, lam);
         w.taken |= __ballot(mine && take);
         w.refused |= __ballot(mine && !take);
     }
@@ -218,10 +229,12 @@ __global__ void __launch_bounds__(kThreads) verify_sums_kernel(const VerifyParam
         const Walk w = walk<E>(a, er, a.round - 1);
         const bool need = w.reached && __popcll(w.kids) > a.round && __popcll(w.kids & w.refused) == a.round;
         const uint64_t nodes = __ballot(need);
-        double lam = 1.0;
-        if (need)
-            for (int j = 1; j < a.round; ++j) lam += g_of(a, j, er.first + lane);
-        s_lam[lane] = lam;
+        for (uint64_t left = nodes; left; left &= left - 1) {
+            const int t = __ffsll((unsigned long long)left) - 1;
+            double lam, G;
+            behind(a, a.round - 1, er.first + t, &lam, &G);
+            if (lane == 0) s_lam[t] = lam + G;
+        }
         if (lane == 0) s_nodes = nodes;
     }
     __syncthreads();
@@ -257,13 +270,13 @@ __global__ void __launch_bounds__(kThreads) verify_walk_kernel(const VerifyParam
             if (lane >= kept && lane < er.rows) a.path[er.first + lane] = -1;
             if (lane == 0) a.keep[e] = kept;
         }
-        if (lane == last) {
-            const int kids = min(__popcll(w.kids), a.max_kids);
-            double lam = 0.0;
-            if (kept)
-                for (int j = 0; j < kids; ++j) lam += j ? g_of(a, j, er.first + last) : 1.0;
+        const int kids = min((int)__popcll(((uint64_t)__builtin_amdgcn_readlane((int)(w.kids >> 32), last) << 32) |
+                                           (uint32_t)__builtin_amdgcn_readlane((int)w.kids, last)), a.max_kids);
+        double lam = 0.0, G = 0.0;
+        if (kept && kids) behind(a, kids - 1, er.first + last, &lam, &G);
+        if (lane == 0) {
             s_row = kept ? er.first + last : -1;
-            s_lam = lam;
+            s_lam = lam + G;
             s_found = 0x7fffffff;
             s_lastpos = -1;
         }
