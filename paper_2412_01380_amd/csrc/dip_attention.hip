@@ -177,21 +177,34 @@ __global__ void __launch_bounds__(WAVES * 64, 1) attn_rows_kernel(const AttnPara
     if (s_last) join_shares<E, D, ROWS, THREADS, true>(p, u.first, shares, u.first_row, head, r0, 0, n_rows);
 }
 
-// Rows enough to fill the matrix cores: eight wavefronts of 16 NB rows each share the tiles, one barrier a tile.
-// Four tiles of LDS: V of the last one, the current one, two on their way.
-constexpr int kBlockWaves = 8;
-constexpr int kBlockSub = 2;              // key blocks of the products in a tile: 64 keys
-constexpr int kBlockThreads = kBlockWaves * 64;
+// Rows enough to fill the matrix cores: the wavefronts of a workgroup, 16 NB rows each, share the tiles, one barrier
+// a tile.  Four tiles of LDS: V of the last one, the current one, two on their way.
+// bf16: 64 keys to a tile, eight wavefronts, one workgroup to a compute unit.
+template <typename E>
+struct Block {
+    static constexpr int WAVES = 8, SUB = 2;
+    static constexpr int per_simd(int) { return 2; }
+};
+// fp32: 16 keys, and small workgroups, several to a compute unit (its products take sixteen times as long: what
+// counts is that some wavefront of a SIMD always has one).  Against attn_rows_kernel over the same rows: 2 x 100
+// rows, 64 dims, 3000 keys 61 -> 37 us; 2048 rows x 4 heads, 128 dims 555 -> 420 us; 32 trees of 96 rows, 64 dims,
+// 2000 keys 124 -> 89 us; at 96 dims within 4 % either way (214 and 221 us at 4 x 600 rows, 1600 keys).
+template <>
+struct Block<float> {
+    static constexpr int WAVES = 4, SUB = 1;
+    static constexpr int per_simd(int dims) { return 6 - dims / 32; }
+};
 constexpr int kBlockRing = 4;
 constexpr int kFewKeys = 512;             // of a row: below that its weights go in as two terms where they are at an edge
 constexpr int kIdTiles = 64;              // tiles whose page numbers are in LDS at a time
 
 template <typename E, int D, int NB>
-__global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const AttnParams p) {
+__global__ void __launch_bounds__(Block<E>::WAVES * 64, Block<E>::per_simd(D)) attn_block_kernel(const AttnParams p) {
     typedef Geo<E, D> G;
     typedef Core<E, D, NB> C;
-    constexpr int SUB = kBlockSub, KEYS = SUB * G::KEYS, TILE = KEYS * G::ROWB, LOADS = TILE / 1024, ROWS = 16 * NB * kBlockWaves;
-    constexpr int MINE = (LOADS + kBlockWaves - 1) / kBlockWaves;     // loads of a wavefront (some twice where uneven)
+    constexpr int WAVES = Block<E>::WAVES, THREADS = WAVES * 64, SUB = Block<E>::SUB;
+    constexpr int KEYS = SUB * G::KEYS, TILE = KEYS * G::ROWB, LOADS = TILE / 1024, ROWS = 16 * NB * WAVES;
+    constexpr int MINE = (LOADS + WAVES - 1) / WAVES;     // loads of a wavefront (some twice where uneven)
     constexpr int Q = SUB * C::MT;
     __shared__ __align__(1024) char s_ring[kBlockRing * 2 * TILE];
     __shared__ int s_ids[kIdTiles * KEYS];
@@ -217,7 +230,7 @@ __global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const Attn
     if (n == 0 && u.share > 0) return;
 
     const int per = max(1, KEYS >> p.c.page_shift);
-    page_ids<KEYS, kBlockThreads>(p.c, seq, range, begin, min(n, kIdTiles), per, s_ids);
+    page_ids<KEYS, THREADS>(p.c, seq, range, begin, min(n, kIdTiles), per, s_ids);
     if (p.parents && wave == 0) tree_masks(p.parents + u.first_row, u.rows, s_tree);
     if (tid < 4) s_bad[tid >> 1][tid & 1] = 0;
     __syncthreads();
@@ -270,7 +283,7 @@ __global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const Attn
         barrier();
         if (i + 2 < n) {
             if (((i + 2) & (kIdTiles - 1)) == 0) {
-                page_ids<KEYS, kBlockThreads>(p.c, seq, range, begin + i + 2, min(n - i - 2, kIdTiles), per, s_ids);
+                page_ids<KEYS, THREADS>(p.c, seq, range, begin + i + 2, min(n - i - 2, kIdTiles), per, s_ids);
                 barrier();
             }
             fetch(i + 2);
@@ -391,8 +404,8 @@ __global__ void __launch_bounds__(kBlockThreads, 2) attn_block_kernel(const Attn
 constexpr int kJoinRows = 8;
 template <typename E, int D, int NB>
 __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p) {
-    constexpr int ROWS = 16 * NB * kBlockWaves;
-    constexpr int KEYS = kBlockSub * Geo<E, D>::KEYS;
+    constexpr int ROWS = 16 * NB * Block<E>::WAVES;
+    constexpr int KEYS = Block<E>::SUB * Geo<E, D>::KEYS;
     __shared__ Unit s_unit;
     const int block = blockIdx.x / (ROWS / kJoinRows), part = blockIdx.x % (ROWS / kJoinRows);
     const int per_entry = p.row_blocks * p.c.n_heads;
@@ -421,19 +434,20 @@ int reach(const dip_kv_cache* c, const dip_batch* b) {
 Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads) {
     Plan pl;
     const int64_t rows = (int64_t)rows_bound(b) * (n_q_heads / c->n_kv_heads);
-    // more than 64 rows share tiles; not in fp32, whose products take sixteen times as long and hide any traffic
-    pl.shared = rows > 64 && c->dtype == DIP_BF16;
-    pl.nb = pl.shared ? (rows <= 16 * kBlockWaves ? 1 : 2) : rows <= 16 ? 1 : rows <= 32 || (c->dtype == DIP_F32 && c->head_dim == 128) ? 2 : 4;
+    const bool bf16 = c->dtype == DIP_BF16;
+    const int block_waves = bf16 ? Block<uint16_t>::WAVES : Block<float>::WAVES;
+    pl.shared = rows > 64;
+    pl.nb = pl.shared ? (!bf16 || rows <= 16 * block_waves ? 1 : 2) : rows <= 16 ? 1 : rows <= 32 || (!bf16 && c->head_dim == 128) ? 2 : 4;
     // (fp32 at 128 dims: four blocks of 16 rows do not fit the registers)
-    pl.rows = 16 * pl.nb * (pl.shared ? kBlockWaves : 1);
+    pl.rows = 16 * pl.nb * (pl.shared ? block_waves : 1);
     pl.row_blocks = (int)((rows + pl.rows - 1) / pl.rows);
     pl.blocks = (int64_t)b->n_batch * c->n_kv_heads * pl.row_blocks;
     // Four wavefronts to a workgroup, as many workgroups to a compute unit as their rings of tiles leave room for;
     // where the blocks alone are more than that, two: the start and the end of one workgroup, when it streams
     // nothing, then lie beside another's middle.
     const auto fit = [&](int waves) { return 256 * ((160 * 1024 - 1024) / (waves * 256 * c->head_dim + 6144)); };
-    pl.waves = pl.shared ? kBlockWaves : pl.blocks <= fit(4) ? 4 : 2;
-    pl.slots = pl.shared ? 256 : fit(pl.waves);
+    pl.waves = pl.shared ? block_waves : pl.blocks <= fit(4) ? 4 : 2;
+    pl.slots = !pl.shared ? fit(pl.waves) : bf16 ? 256 : 256 * (160 * 1024 / (512 * c->head_dim + 5120));
     // attn_block_kernel's shares are joined by a launch of its own, which costs 10 us even where there turn out to
     // be none: with far more blocks than the chip holds at a time none are made
     pl.cut = !pl.shared || pl.blocks < 4 * pl.slots;
@@ -457,18 +471,22 @@ hipError_t launch_rows(const AttnParams& p, const Plan& pl, hipStream_t stream) 
     if (pl.waves == 4) return launch_timed(attn_rows_kernel<E, D, NB, 4>, grid, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
     return launch_timed(attn_rows_kernel<E, D, NB, 2>, grid, dim3(128), stream, DIP_KERNEL_ATTENTION, p);
 }
-template <int D, int NB>
+template <typename E, int D, int NB>
 hipError_t launch_block(const AttnParams& p, const Plan& pl, hipStream_t stream) {
     const dim3 grid((unsigned)((p.grid + 7) / 8 * 8)), join((unsigned)(pl.blocks * (pl.rows / kJoinRows)));
-    const hipError_t err = launch_timed(attn_block_kernel<uint16_t, D, NB>, grid, dim3(kBlockThreads), stream, DIP_KERNEL_ATTENTION, p);
+    const hipError_t err = launch_timed(attn_block_kernel<E, D, NB>, grid, dim3(Block<E>::WAVES * 64), stream, DIP_KERNEL_ATTENTION, p);
     if (err != hipSuccess || !pl.cut) return err;
-    return launch_timed(attn_join_kernel<uint16_t, D, NB>, join, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
+    return launch_timed(attn_join_kernel<E, D, NB>, join, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
 }
 template <typename E, int D>
 int32_t launch(const AttnParams& p, const Plan& pl, hipStream_t stream) {
     hipError_t err;
-    if constexpr (sizeof(E) == 2)
-        if (pl.shared) return check_hip(pl.nb == 1 ? launch_block<D, 1>(p, pl, stream) : launch_block<D, 2>(p, pl, stream), "attention launch");
+    if (pl.shared) {
+        if (pl.nb == 1) err = launch_block<E, D, 1>(p, pl, stream);
+        else if constexpr (sizeof(E) == 2) err = launch_block<E, D, 2>(p, pl, stream);
+        else return fail(DIP_ERR_UNSUPPORTED, "attention: no kernel for this shape");
+        return check_hip(err, "attention launch");
+    }
     if (pl.nb == 1) err = launch_rows<E, D, 1>(p, pl, stream);
     else if (pl.nb == 2) err = launch_rows<E, D, 2>(p, pl, stream);
     else if constexpr (sizeof(E) == 2 || D < 128) err = launch_rows<E, D, 4>(p, pl, stream);
