@@ -399,30 +399,33 @@ __global__ void __launch_bounds__(Block<E>::WAVES * 64, Block<E>::per_simd(D)) a
     }
 }
 
-// The shares of attn_block_kernel's rows, 8 rows to a workgroup: what one workgroup, the last to arrive, would
-// take far longer over (256 rows of 20 shares: 120 us alone, 9 us in a launch of its own).
+// The shares of attn_block_kernel's rows, spread over the chip: with the last workgroup of a block to join its 256
+// rows of 20 shares by itself, wide trees took 465 us instead of 390.  At least kJoinRows rows to a workgroup,
+// and no more than about kJoinGrid workgroups: each works out for itself what the blocks were cut into, 13.8 us for
+// 9984 workgroups that then find nothing cut.
 constexpr int kJoinRows = 8;
+constexpr int kJoinGrid = 1024;
 template <typename E, int D, int NB>
 __global__ void __launch_bounds__(256) attn_join_kernel(const AttnParams p) {
     constexpr int ROWS = 16 * NB * Block<E>::WAVES;
     constexpr int KEYS = Block<E>::SUB * Geo<E, D>::KEYS;
     __shared__ Unit s_unit;
-    const int block = blockIdx.x / (ROWS / kJoinRows), part = blockIdx.x % (ROWS / kJoinRows);
+    const int join_rows = p.join_rows, parts = ROWS / join_rows, block = blockIdx.x / parts, part = blockIdx.x - block * parts;
     const int per_entry = p.row_blocks * p.c.n_heads;
     if (threadIdx.x < 64) Units<KEYS, ROWS>(p, 8).find_block(block / per_entry, block % per_entry, &s_unit);
     __syncthreads();
     const Unit u = uniform(s_unit);
-    if (u.rows == 0 || u.seq < 0 || u.n_rows <= part * kJoinRows) return;
+    if (u.rows == 0 || u.seq < 0 || u.n_rows <= part * join_rows) return;
     const Range range = key_range<KEYS>(p, u.len, u.rows, u.r0 / p.group, (u.r0 + u.n_rows - 1) / p.group);
     const int shares = u.cut(range.tiles);
     if (shares > 1)
-        join_shares<E, D, ROWS, 256, false>(p, u.first, shares, u.first_row, u.head, u.r0, part * kJoinRows, min(u.n_rows, (part + 1) * kJoinRows));
+        join_shares<E, D, ROWS, 256, false>(p, u.first, shares, u.first_row, u.head, u.r0, part * join_rows, min(u.n_rows, (part + 1) * join_rows));
 }
 
 // ---- launch plan ----------------------------------------------------------------------------------
 struct Plan {
     bool shared;              // attn_block_kernel
-    int nb, rows, waves, row_blocks, slots;
+    int nb, rows, waves, row_blocks, slots, join_rows;
     int64_t blocks, grid;
     bool cut;                 // blocks may be cut into shares (slots > 0)
     size_t off_ml, off_tickets, total;
@@ -452,6 +455,8 @@ Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads) {
     // be none: with far more blocks than the chip holds at a time none are made
     pl.cut = !pl.shared || pl.blocks < 4 * pl.slots;
     if (!pl.cut) pl.slots = 0;
+    pl.join_rows = pl.rows;
+    while (pl.join_rows > kJoinRows && pl.blocks * (pl.rows / pl.join_rows) < kJoinGrid) pl.join_rows /= 2;
     pl.grid = pl.blocks > pl.slots ? pl.blocks : pl.slots;
     size_t o = 0;
     // (only a cut into at most `slots` units has shares)
@@ -473,9 +478,10 @@ hipError_t launch_rows(const AttnParams& p, const Plan& pl, hipStream_t stream) 
 }
 template <typename E, int D, int NB>
 hipError_t launch_block(const AttnParams& p, const Plan& pl, hipStream_t stream) {
-    const dim3 grid((unsigned)((p.grid + 7) / 8 * 8)), join((unsigned)(pl.blocks * (pl.rows / kJoinRows)));
+    const dim3 grid((unsigned)((p.grid + 7) / 8 * 8));
     const hipError_t err = launch_timed(attn_block_kernel<E, D, NB>, grid, dim3(Block<E>::WAVES * 64), stream, DIP_KERNEL_ATTENTION, p);
     if (err != hipSuccess || !pl.cut) return err;
+    const dim3 join((unsigned)(pl.blocks * (pl.rows / p.join_rows)));
     return launch_timed(attn_join_kernel<E, D, NB>, join, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
 }
 template <typename E, int D>
@@ -543,7 +549,6 @@ int32_t attend(const dip_kv_cache* c, int32_t layer, const dip_batch* b, const i
     p.out = (char*)out;
     p.q_stride = q_stride * es;
     p.out_stride = out_stride * es;
-    p.n_q_heads = n_q_heads;
     p.group = n_q_heads / c->n_kv_heads;
     p.scale_log2 = scale * 1.44269504088896340736f;
     p.window = window;
@@ -552,6 +557,7 @@ int32_t attend(const dip_kv_cache* c, int32_t layer, const dip_batch* b, const i
     p.slots = pl.slots;
     p.grid = (int)pl.grid;
     p.row_blocks = pl.row_blocks;
+    p.join_rows = pl.join_rows;
     p.part_o = (float*)ws;
     p.part_ml = (float2*)((char*)ws + pl.off_ml);
     p.tickets = (uint64_t*)((char*)ws + pl.off_tickets);

@@ -35,7 +35,6 @@ struct AttnParams {
     char* out;
     int64_t q_stride;         // bytes
     int64_t out_stride;
-    int n_q_heads;
     int group;                // query heads of a key/value head
     float scale_log2;         // scale * log2(e)
     int window;               // 0: no bound
@@ -44,6 +43,7 @@ struct AttnParams {
     int slots;                // workgroups that the chip holds at a time, or what to pretend it does
     int grid;                 // most units there can be
     int row_blocks;           // most blocks of rows of an entry and key/value head
+    int join_rows;            // of a workgroup of attn_join_kernel
     float* part_o;            // [unit][rows of a block][D], not normalised
     float2* part_ml;          // [unit][rows of a block]: maximum (times scale_log2), sum
     uint64_t* tickets;        // a word per unit, kTicketStride apart, whatever they hold

@@ -87,10 +87,34 @@ __device__ __forceinline__ double weight(float p, float q, double lam) {
     return w > 0.0 ? w : 0.0;
 }
 
+// inclusive running sum over a wavefront: data-parallel moves within rows of 16 lanes, then the rows' sums by scalar
+template <int CTRL>
+__device__ __forceinline__ double moved(double x) {
+    const uint64_t b = __double_as_longlong(x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, 0xf, 0xf, true);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), CTRL, 0xf, 0xf, true);
+    return __longlong_as_double(((uint64_t)hi << 32) | lo);
+}
+__device__ __forceinline__ double of_lane(double x, int lane) {
+    const uint64_t b = __double_as_longlong(x);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)b, lane), hi = __builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane);
+    return __longlong_as_double(((uint64_t)hi << 32) | lo);
+}
+__device__ __forceinline__ double in_rows(double x) {
+    x += moved<0x111>(x);                             // row_shr 1, 2, 4, 8
+    x += moved<0x112>(x);
+    x += moved<0x114>(x);
+    return x + moved<0x118>(x);
+}
+__device__ __forceinline__ double running(double x) {
+    x = in_rows(x);
+    const double a = of_lane(x, 15), b = of_lane(x, 31), c = of_lane(x, 47);
+    const int row = (threadIdx.x & 63) >> 4;
+    return x + (row == 0 ? 0.0 : row == 1 ? a : row == 2 ? a + b : a + b + c);
+}
 __device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-    for (int off = 32; off; off >>= 1) x += __shfl_xor(x, off);
-    return x;
+    x = in_rows(x);
+    return of_lane(x, 15) + of_lane(x, 31) + of_lane(x, 47) + of_lane(x, 63);
 }
 // sum over the workgroup, in thread 0
 __device__ __forceinline__ double block_sum(double x, double* waves) {
@@ -124,26 +148,12 @@ __device__ __forceinline__ void chunk_sums(const VerifyParams& a, int row, doubl
     *all = sp;
 }
 
-// G_j (j >= 1) of a row, by a wavefront: a lane takes a chunk's sum, all get theirs
-__device__ __forceinline__ double g_of(const VerifyParams& a, int j, int row) {
-    const int lane = threadIdx.x & 63;
-    return wave_sum(lane < a.chunks ? a.g_part[((size_t)(j - 1) * a.b.n_rows + row) * a.chunks + lane] : 0.0);
-}
-// lam and G behind `k` refused children of a row, by a wavefront
-__device__ __forceinline__ void behind(const VerifyParams& a, int k, int row, double* lam, double* G) {
-    *lam = 0.0;
-    *G = 1.0;
-    for (int j = 1; j <= k; ++j) {
-        *lam += *G;
-        *G = g_of(a, j, row);
-    }
-}
-
 // One wavefront, lane t for node t: which children are taken, as far as G_1 .. G_{known} say.
 struct Walk {
     uint64_t kids;            // this node's children
     uint64_t refused;         // nodes tried and refused ...
     uint64_t taken;           // ... and taken, where every earlier sibling was refused
+    double next;              // lam_{j+1} of its parent, this node being child j <= known
     bool reached;             // this node stands, or may do so once more is known
 };
 template <typename E>
@@ -170,7 +180,23 @@ __device__ __forceinline__ Walk walk(const VerifyParams& a, const EntryRows& er,
         if (other == lane) w.kids |= 1ull << s;
     }
     const int order = child ? __popcll(earlier) : -1;
+    // G_j for every child j >= 1: a lane adds the chunks of its parent's row, 16 on their way at a time
+    double G = 1.0, lam = 0.0;
+    if (order >= 1 && order <= known && order < a.max_kids) {
+        constexpr int FLIGHT = 16;
+        const double* part = a.g_part + ((size_t)(order - 1) * a.b.n_rows + up) * a.chunks;
+        G = 0.0;
+        for (int c = 0; c < a.chunks; c += FLIGHT) {
+            double x[FLIGHT];
+#pragma unroll
+            for (int f = 0; f < FLIGHT; ++f) x[f] = part[min(c + f, a.chunks - 1)];
+#pragma unroll
+            for (int f = 0; f < FLIGHT; ++f) G += c + f < a.chunks ? x[f] : 0.0;
+        }
+    }
+    w.next = 1.0;
     w.refused = w.taken = 0;
+    const int elder = earlier ? 63 - __clzll((long long)earlier) : lane;
     uint64_t open = 0;                                // children whose test is not known yet
     for (int k = 0; k < a.max_kids; ++k) {
         const bool mine = order == k && (earlier & ~(w.refused | open)) == 0;
@@ -179,17 +205,10 @@ __device__ __forceinline__ Walk walk(const VerifyParams& a, const EntryRows& er,
             open |= __ballot(mine);
             continue;
         }
-        double lam = 0.0, G = 1.0;
-        if (k > 0) {                                  // (the same for all lanes: the nodes one after the other)
-            for (uint64_t left = __ballot(mine); left; left &= left - 1) {
-                const int t = __ffsll((unsigned long long)left) - 1;
-                double l, g;
-                behind(a, k, __builtin_amdgcn_readlane(up, t), &l, &g);
-                if (lane == t) {
-                    lam = l;
-                    G = g;
-                }
-            }
+        const double upto = __shfl(w.next, elder);
+        if (k > 0 && order == k) {
+            lam = upto;
+            w.next = upto + G;
         }
         const bool take = mine && fits && u * (double)qv * G < weight(pv, qv, lam);
         w.taken |= __ballot(mine && take);
@@ -228,13 +247,8 @@ __global__ void __launch_bounds__(kThreads) verify_sums_kernel(const VerifyParam
     if (threadIdx.x < 64) {
         const Walk w = walk<E>(a, er, a.round - 1);
         const bool need = w.reached && __popcll(w.kids) > a.round && __popcll(w.kids & w.refused) == a.round;
-        const uint64_t nodes = __ballot(need);
-        for (uint64_t left = nodes; left; left &= left - 1) {
-            const int t = __ffsll((unsigned long long)left) - 1;
-            double lam, G;
-            behind(a, a.round - 1, er.first + t, &lam, &G);
-            if (lane == 0) s_lam[t] = lam + G;
-        }
+        const uint64_t nodes = __ballot(need), tried = w.kids & w.refused;
+        s_lam[lane] = __shfl(w.next, tried ? 63 - __clzll((long long)tried) : lane);
         if (lane == 0) s_nodes = nodes;
     }
     __syncthreads();
@@ -270,13 +284,13 @@ __global__ void __launch_bounds__(kThreads) verify_walk_kernel(const VerifyParam
             if (lane >= kept && lane < er.rows) a.path[er.first + lane] = -1;
             if (lane == 0) a.keep[e] = kept;
         }
-        const int kids = min((int)__popcll(((uint64_t)__builtin_amdgcn_readlane((int)(w.kids >> 32), last) << 32) |
-                                           (uint32_t)__builtin_amdgcn_readlane((int)w.kids, last)), a.max_kids);
-        double lam = 0.0, G = 0.0;
-        if (kept && kids) behind(a, kids - 1, er.first + last, &lam, &G);
+        // all children of the last node (up to max_kids) were tried and refused
+        const uint64_t tried = w.kids & w.refused;
+        const double upto = __shfl(w.next, tried ? 63 - __clzll((long long)tried) : lane);
+        const double lam = of_lane(tried ? upto : 0.0, last);
         if (lane == 0) {
             s_row = kept ? er.first + last : -1;
-            s_lam = lam + G;
+            s_lam = lam;
             s_found = 0x7fffffff;
             s_lastpos = -1;
         }
@@ -306,22 +320,14 @@ __global__ void __launch_bounds__(kThreads) verify_walk_kernel(const VerifyParam
     __syncthreads();
     if (tid < 64) {
         // running sums over the chunks, lane c up to chunk c
-        auto running = [&](const double* part) {
-            double x = lane < a.chunks ? get(part + lane) : 0.0;
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const double y = __shfl_up(x, off);
-                if (lane >= off) x += y;
-            }
-            return x;
-        };
+        auto up_to = [&](const double* part) { return running(lane < a.chunks ? get(part + lane) : 0.0); };
         double lam = s_lam;
-        double upto = running(w_part);
-        double total = __shfl(upto, 63);
+        double upto = up_to(w_part);
+        double total = of_lane(upto, 63);
         if (!(total > 0.0)) {                         // p == q everywhere: the target itself
             lam = 0.0;
-            upto = running(p_part);
-            total = __shfl(upto, 63);
+            upto = up_to(p_part);
+            total = of_lane(upto, 63);
         }
         const double target = u_sample * total;
         const double left = __shfl_up(upto, 1);
@@ -361,12 +367,7 @@ __global__ void __launch_bounds__(kThreads) verify_walk_kernel(const VerifyParam
             mine += y;
             if (y > 0.0) lastpos = x + i;
         }
-        double upto = mine;                           // inclusive running sum over the threads
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const double y = __shfl_up(upto, off);
-            if (lane >= off) upto += y;
-        }
+        const double upto = running(mine);
         __syncthreads();
         if (lane == 63) s_waves[wave] = upto;
         __syncthreads();
