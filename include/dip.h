@@ -445,7 +445,7 @@ typedef struct dip_kv_cache {
     int32_t n_kv_heads;
     int32_t head_dim;     /* a multiple of 16 bytes; the attention calls: 64, 96 or 128      */
     int32_t n_seqs;
-    int32_t max_pages;    /* of one sequence; max_pages * page_size < 2^31                   */
+    int32_t max_pages;    /* of one sequence; max_pages * page_size <= 2^31 - 2^25           */
     int64_t layer_stride; /* in elements                                                     */
     int64_t page_stride;
     int64_t head_stride;
@@ -529,13 +529,14 @@ int32_t dip_kv_compact(const dip_kv_cache* cache, const dip_batch* batch, const 
  * outside [0, t): the node is absent, as are the nodes below an absent one); node t stands at pos =
  * seq_len + its depth, sees the ancestors that are nodes of the tree and itself, and of the committed
  * positions j < seq_len those with  j > pos - window  or  j < sinks.
- * window 0 means no bound (sinks then change nothing).  A row that sees nothing, and an absent node,
- * gets zeros.  Positions that a row does not see do not matter to it, whatever they hold.
+ * window 0 means no bound (sinks then change nothing).  A row that sees nothing, an absent node, and a row
+ * whose scores are all -inf get zeros.  Positions that a row does not see do not matter to it, whatever they hold.
  *   q, out   n_rows rows of n_q_heads * head_dim elements of the cache's type, q_stride / out_stride
  *            elements apart (multiples of 16 bytes); out may not overlap q
  *   scale > 0      n_q_heads a multiple of n_kv_heads      ws  *_workspace_bytes() bytes, 256-aligned
  * Scores, softmax statistics and sums are fp32; with a DIP_BF16 cache the weights p enter their product
- * with v as bf16.  The order of the sums is fixed by shapes, lengths and max_len (bit-repeatable).
+ * with v as the sum of two bf16 terms, but for entries of more than 64 rows x query heads per key/value
+ * head as one, except at the ends of the context of rows that see fewer than 512 keys.  The order of the sums is fixed by shapes, lengths and max_len (bit-repeatable).
  */
 size_t dip_attention_workspace_bytes(const dip_kv_cache* cache, const dip_batch* batch, int32_t n_q_heads,
                                      int32_t window, int32_t sinks);

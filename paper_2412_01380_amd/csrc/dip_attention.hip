@@ -1,8 +1,14 @@
 // Attention over a paged key/value cache: dip_window_attention, dip_tree_attention.
 //
 // The rows of an entry that share a key/value head -- its tokens or nodes times the query heads of the
-// group -- form blocks of 16, 32 or 64 (attn_rows_kernel), 128 or 256 (attn_block_kernel); a workgroup takes a
-// block and a share of the keys that it sees.
+// group -- form blocks, and a workgroup takes a block and a share of the keys that it sees:
+//   up to 64 rows          attn_rows_kernel: blocks of 16, 32 or 64; wavefronts stream keys of their own
+//   more                   attn_block_kernel: blocks of 64 (fp32), 128 or 256 whose wavefronts share the tiles
+// Keys are read once for all query heads of a group and all rows of a block.  With few rows what bounds the
+// call is reading them: 32 tokens of 40 heads on 10, a window of 2047, 79 us for the 336 MB of K and V (52 us
+// at the rate of a plain read).  With many it is the matrix cores and, beside them, the softmax's plain
+// instructions: a maximum, a multiply-add, an exponential, a sum and half a conversion for every weight, whose
+// two products are 256 multiply-adds at 128 dims.
 
 #include <cmath>
 
@@ -16,7 +22,13 @@ constexpr int kRing = 2;                  // tiles of a wavefront in LDS: one in
 constexpr int kIds = 256;                 // page numbers of a wavefront in LDS at a time
 
 // WAVES wavefronts, each of which streams tiles of its own through LDS (no barrier in the loop) and keeps a
-// softmax of its own; they are joined in LDS at the end.
+// softmax of its own; they are joined in LDS at the end, and shares of a block by the last of its workgroups.
+// LDS although no wavefront reads another's tile: a load to LDS holds no registers while it is on its way, and
+// the products want rows of K and columns of V, which memory has neither of side by side.  Two tiles of 32 keys
+// (16 in fp32) each: a third one costs a workgroup per compute unit.
+// Weights go in as two bf16 terms (Core::pack): the matrix cores wait for memory here, the second term is free.
+// Measured (bf16, 128 dims): 2 x 700 keys 10.4 us, of which 4.4 any launch takes; 8 trees of 8 nodes, 4 heads on
+// one, up to 8192 keys 40 us at 4.0 TB/s.  fp32, 3 trees of 7 nodes, 32 heads, 96 dims: 19 us.
 template <typename E, int D, int NB, int WAVES>
 __global__ void __launch_bounds__(WAVES * 64, 1) attn_rows_kernel(const AttnParams p) {
     typedef Geo<E, D> G;
@@ -179,6 +191,14 @@ __global__ void __launch_bounds__(WAVES * 64, 1) attn_rows_kernel(const AttnPara
 
 // Rows enough to fill the matrix cores: the wavefronts of a workgroup, 16 NB rows each, share the tiles, one barrier
 // a tile.  Four tiles of LDS: V of the last one, the current one, two on their way.
+// An operand read from LDS serves NB products: with one block of 16 rows the reads (570 bytes/ns of a compute
+// unit) take as long as the products, with two half; four do not fit the registers.  The softmax of a tile runs
+// beside the products of its neighbours: P V lags one tile behind K Q, so both are at hand when a wavefront
+// waits for exponentials.  What is left is that products and plain instructions of the two wavefronts of a SIMD
+// overlap only by half (alone 485 and 515 us of a probe, together 880).
+// Measured (bf16, 128 dims, 4 heads on one): 2 prompts of up to 4096 rows, window 2047: 385 to 420 us (710 TFLOP/s of
+// the 1152 of a large library product); 4 trees of 64 nodes over up to 49152 keys 186 to 212 us.  With
+// attn_rows_kernel: 1160 and 890 us.
 // bf16: 64 keys to a tile, eight wavefronts, one workgroup to a compute unit.
 template <typename E>
 struct Block {

@@ -453,7 +453,7 @@ struct Core<uint16_t, D, NB> {
             }
     }
     // The weights of KEYS keys as the second product takes them.  As one bf16 term each they are off by up to
-    // 2^-8, which over many keys averages out but shows where a few of them carry a row; with TWO the
+    // 2^-9, which over many keys averages out but shows where a few of them carry a row; with TWO the
     // remainder is a second term.
     struct Weights {
         bf16x8 w[NB], rest[NB];
