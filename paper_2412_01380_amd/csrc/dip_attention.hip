@@ -5,11 +5,12 @@
 //   up to 64 rows          attn_rows_kernel: blocks of 16, 32 or 64; wavefronts stream keys of their own
 //   more                   attn_block_kernel: blocks of 64 (fp32), 128 or 256 whose wavefronts share the tiles
 // Keys are read once for all query heads of a group and all rows of a block.  With few rows what bounds the
-// call is reading them: 32 tokens of 40 heads on 10, a window of 2047, 79 us for the 336 MB of K and V (52 us
+// call is reading them: 32 tokens of 40 heads on 10, a window of 2047, 75 us for the 332 MB of K and V (52 us
 // at the rate of a plain read).  With many it is the matrix cores and, beside them, the softmax's plain
 // instructions: a maximum, a multiply-add, an exponential, a sum and half a conversion for every weight, whose
 // two products are 256 multiply-adds at 128 dims.
 
+#include <algorithm>
 #include <cmath>
 
 #include "dip_attn_device.h"
@@ -28,8 +29,8 @@ constexpr int kIds = 256;                 // page numbers of a wavefront in LDS 
 // (16 in fp32) each: a third one costs a workgroup per compute unit.
 // Weights go in as two bf16 terms (Core::pack): the matrix cores wait for memory here, the second term is free.
 // Measured (bf16, 128 dims): 2 x 700 keys 10.4 us, of which 4.4 any launch takes; 8 trees of 8 nodes, 4 heads on
-// one, up to 8192 keys 40 us at 4.0 TB/s.  fp32, 3 trees of 7 nodes, 32 heads, 96 dims: 19 us.
-template <typename E, int D, int NB, int WAVES>
+// one, up to 8192 keys 46 us at 3.7 TB/s.  fp32, 3 trees of 7 nodes, 32 heads, 96 dims: 19 us.
+template <typename E, int D, int NB, int WAVES, bool ONCE>
 __global__ void __launch_bounds__(WAVES * 64, 1) attn_rows_kernel(const AttnParams p) {
     typedef Geo<E, D> G;
     typedef Core<E, D, NB> C;
@@ -97,8 +98,8 @@ __global__ void __launch_bounds__(WAVES * 64, 1) attn_rows_kernel(const AttnPara
 #pragma unroll
         for (int x = 0; x < LOADS; ++x) {
             const int64_t off = piece_offset<G>(p.c, s_ids[wave] + (i & (span - 1)) * per, j0, range.end, x);
-            load_to_lds(kbase + off, to + x * 1024);
-            load_to_lds(vbase + off, to + TILE + x * 1024);
+            load_to_lds<ONCE>(kbase + off, to + x * 1024);
+            load_to_lds<ONCE>(vbase + off, to + TILE + x * 1024);
         }
     };
 
@@ -197,7 +198,7 @@ __global__ void __launch_bounds__(WAVES * 64, 1) attn_rows_kernel(const AttnPara
 // waits for exponentials.  What is left is that products and plain instructions of the two wavefronts of a SIMD
 // overlap only by half (alone 485 and 515 us of a probe, together 880).
 // Measured (bf16, 128 dims, 4 heads on one): 2 prompts of up to 4096 rows, window 2047: 385 to 420 us (710 TFLOP/s of
-// the 1152 of a large library product); 4 trees of 64 nodes over up to 49152 keys 186 to 212 us.  With
+// the 1152 of a large library product); 4 trees of 64 nodes over up to 49152 keys 180 to 210 us.  With
 // attn_rows_kernel: 1160 and 890 us.
 // bf16: 64 keys to a tile, eight wavefronts, one workgroup to a compute unit.
 template <typename E>
@@ -218,7 +219,7 @@ constexpr int kBlockRing = 4;
 constexpr int kFewKeys = 512;             // of a row: below that its weights go in as two terms where they are at an edge
 constexpr int kIdTiles = 64;              // tiles whose page numbers are in LDS at a time
 
-template <typename E, int D, int NB>
+template <typename E, int D, int NB, bool ONCE>
 __global__ void __launch_bounds__(Block<E>::WAVES * 64, Block<E>::per_simd(D)) attn_block_kernel(const AttnParams p) {
     typedef Geo<E, D> G;
     typedef Core<E, D, NB> C;
@@ -287,8 +288,8 @@ __global__ void __launch_bounds__(Block<E>::WAVES * 64, Block<E>::per_simd(D)) a
         for (int m = 0; m < MINE; ++m) {
             const int x = (wave * MINE + m) % LOADS;
             const int64_t off = piece_offset<G>(p.c, ids, j0, range.end, x);
-            load_to_lds(kbase + off, to + x * 1024);
-            load_to_lds(vbase + off, to + TILE + x * 1024);
+            load_to_lds<ONCE>(kbase + off, to + x * 1024);
+            load_to_lds<ONCE>(vbase + off, to + TILE + x * 1024);
         }
     };
     auto barrier = [&]() {
@@ -448,13 +449,20 @@ struct Plan {
     int nb, rows, waves, row_blocks, slots, join_rows;
     int64_t blocks, grid;
     bool cut;                 // blocks may be cut into shares (slots > 0)
+    bool once;                // keys and values pass by the caches
     size_t off_ml, off_tickets, total;
 };
 int reach(const dip_kv_cache* c, const dip_batch* b) {
     const int fit = c->max_pages * c->page_size;
     return b->max_len && b->max_len < fit ? b->max_len : fit;
 }
-Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads) {
+// Non-temporal loads of keys and values from here on (bytes of a call), where one block of rows is all that reads
+// them.  At 170 MB and more of bf16: 49.3 -> 45.9 us (8 trees of 8 nodes), 78.4 -> 74.8 (32 tokens), 224 -> 210
+// (32 tokens over 12000 keys).  Less may still be in the last-level cache (256 MB) when it is read again, and what
+// several blocks read should stay there: 39 MB 19.4 -> 20.1 us, 4 MB 10.6 -> 11.0, prompts 390 -> 398.  (Of two
+// kernels: asking for each load costs more than it gains, 2 to 4 %.  fp32 blocks wait for their products: 184 us and 184.)
+constexpr double kOnceBytes = 64 << 20;
+Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads, int window, int sinks) {
     Plan pl;
     const int64_t rows = (int64_t)rows_bound(b) * (n_q_heads / c->n_kv_heads);
     const bool bf16 = c->dtype == DIP_BF16;
@@ -475,6 +483,9 @@ Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads) {
     // be none: with far more blocks than the chip holds at a time none are made
     pl.cut = !pl.shared || pl.blocks < 4 * pl.slots;
     if (!pl.cut) pl.slots = 0;
+    int64_t keys = reach(c, b);
+    if (window) keys = std::min(keys, (int64_t)window + sinks + rows_bound(b));
+    pl.once = pl.row_blocks == 1 && (double)keys * b->n_batch * c->n_kv_heads * c->head_dim * 2 * elem_bytes(c->dtype) >= kOnceBytes;
     pl.join_rows = pl.rows;
     while (pl.join_rows > kJoinRows && pl.blocks * (pl.rows / pl.join_rows) < kJoinGrid) pl.join_rows /= 2;
     pl.grid = pl.blocks > pl.slots ? pl.blocks : pl.slots;
@@ -492,14 +503,18 @@ Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads) {
 
 template <typename E, int D, int NB>
 hipError_t launch_rows(const AttnParams& p, const Plan& pl, hipStream_t stream) {
-    const dim3 grid((unsigned)p.grid);
-    if (pl.waves == 4) return launch_timed(attn_rows_kernel<E, D, NB, 4>, grid, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
-    return launch_timed(attn_rows_kernel<E, D, NB, 2>, grid, dim3(128), stream, DIP_KERNEL_ATTENTION, p);
+    const dim3 grid((unsigned)p.grid), block(pl.waves * 64);
+    const auto go = [&](auto kernel) { return launch_timed(kernel, grid, block, stream, DIP_KERNEL_ATTENTION, p); };
+    if (pl.waves == 4) return pl.once ? go(attn_rows_kernel<E, D, NB, 4, true>) : go(attn_rows_kernel<E, D, NB, 4, false>);
+    return pl.once ? go(attn_rows_kernel<E, D, NB, 2, true>) : go(attn_rows_kernel<E, D, NB, 2, false>);
 }
 template <typename E, int D, int NB>
 hipError_t launch_block(const AttnParams& p, const Plan& pl, hipStream_t stream) {
     const dim3 grid((unsigned)((p.grid + 7) / 8 * 8));
-    const hipError_t err = launch_timed(attn_block_kernel<E, D, NB>, grid, dim3(Block<E>::WAVES * 64), stream, DIP_KERNEL_ATTENTION, p);
+    const auto go = [&](auto kernel) { return launch_timed(kernel, grid, dim3(Block<E>::WAVES * 64), stream, DIP_KERNEL_ATTENTION, p); };
+    hipError_t err;
+    if constexpr (sizeof(E) == 2) err = pl.once ? go(attn_block_kernel<E, D, NB, true>) : go(attn_block_kernel<E, D, NB, false>);
+    else err = go(attn_block_kernel<E, D, NB, false>);
     if (err != hipSuccess || !pl.cut) return err;
     const dim3 join((unsigned)(pl.blocks * (pl.rows / p.join_rows)));
     return launch_timed(attn_join_kernel<E, D, NB>, join, dim3(256), stream, DIP_KERNEL_ATTENTION, p);
@@ -538,7 +553,7 @@ int32_t check_attention(const dip_kv_cache* c, const dip_batch* b, int32_t n_q_h
     if (window < 0 || sinks < 0) return fail(DIP_ERR_INVALID_ARG, "attention: window and sinks must be >= 0");
     const int64_t rows = (int64_t)rows_bound(b) * (n_q_heads / c->n_kv_heads);
     if (rows >= 1 << 30) return fail(DIP_ERR_UNSUPPORTED, "attention: too many rows of one entry");
-    const Plan pl = plan_attention(c, b, n_q_heads);
+    const Plan pl = plan_attention(c, b, n_q_heads, window, sinks);
     if (pl.blocks * 32 >= (int64_t)1 << 31) return fail(DIP_ERR_UNSUPPORTED, "attention: too many rows for one call");
     return DIP_OK;
 }
@@ -556,7 +571,7 @@ int32_t attend(const dip_kv_cache* c, int32_t layer, const dip_batch* b, const i
     if (q_stride < width || out_stride < width) return fail(DIP_ERR_INVALID_ARG, "attention: strides smaller than a row");
     if (q_stride * es % 16 || out_stride * es % 16 || !aligned16(q) || !aligned16(out))
         return fail(DIP_ERR_UNSUPPORTED, "attention: rows of q and out must start on 16-byte boundaries");
-    const Plan pl = plan_attention(c, b, n_q_heads);
+    const Plan pl = plan_attention(c, b, n_q_heads, window, sinks);
     st = validate_ws(ws, ws_bytes, pl.total);
     if (st) return st;
     AttnParams p;
@@ -596,7 +611,7 @@ extern "C" {
 
 size_t dip_attention_workspace_bytes(const dip_kv_cache* cache, const dip_batch* batch, int32_t n_q_heads, int32_t window, int32_t sinks) {
     if (attn::check_attention(cache, batch, n_q_heads, window, sinks)) return 0;
-    return attn::plan_attention(cache, batch, n_q_heads).total;
+    return attn::plan_attention(cache, batch, n_q_heads, window, sinks).total;
 }
 
 int32_t dip_window_attention(const dip_kv_cache* cache, int32_t layer, const dip_batch* batch, const void* q, int64_t q_stride,

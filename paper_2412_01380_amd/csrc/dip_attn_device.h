@@ -352,11 +352,16 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p) { return (uint32_t
 
 // 64 x 16 bytes from the lanes' addresses to LDS at `to` + 16 * lane.  Written in assembly because the
 // compiler would make every later LDS read wait for all of them; nothing but the counter says that they are
-// there, so readers wait with wait_loads().  (The load writes no register; m0 is put back.)
+// there, so readers wait with wait_loads().  (The load writes no register; m0 is put back.)  ONCE: non-temporal.
+template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const char* from, uint32_t to) {
     uint32_t m0;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
-                 : "=&s"(m0) : "v"(from), "s"(to) : "memory");
+    if constexpr (ONCE)
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt\n\ts_mov_b32 m0, %0"
+                     : "=&s"(m0) : "v"(from), "s"(to) : "memory");
+    else
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
+                     : "=&s"(m0) : "v"(from), "s"(to) : "memory");
 }
 // This lane's 16 bytes of load x of a tile: `off` from the start of the head.  ids: the tile's page numbers.
 template <typename G>
