@@ -6,8 +6,8 @@
 //
 // A decode step is reserve (two launches), append, compact (two): all wait for memory.  A few drafts of a few
 // branches are bound by the launches themselves (2 to 7 us each; six branches of 8 rows, 32 layers: 35 us with
-// fork and free, 7 launches); 16 branches of up to 256 rows, 40 layers, 10 heads of 128, by bytes: append 251 us,
-// move 110, copy on write 47 of 426 us, against 383 us for the bytes at the rate of a plain copy (4.83 TB/s).
+// fork and free, 7 launches); 16 branches of up to 256 rows, 40 layers, 10 heads of 128, by bytes: append 229 us,
+// move 119, copy on write 49 of 414 us, against 383 us for the bytes at the rate of a plain copy (4.83 TB/s).
 
 #include "dip_decode_internal.h"
 
@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(kThreads) kv_copy_kernel(const CopyParams p) {
 }
 
 // ---- append -------------------------------------------------------------------------------
-// A thread moves 16 bytes of k and the same of v.  Bound by bytes (1.7 GB read and written in 251 us at 16
+// A thread moves 16 bytes of k and the same of v.  Bound by bytes (1.1 GB read and written in 229 us at 16
 // entries of up to 256 rows, 40 layers), small ones by latency: hence fewer rows to a workgroup then.
 struct AppendParams {
     KvView c;
@@ -365,7 +365,8 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams 
         const int h = c / p.c.pieces, x = c - h * p.c.pieces;
         const int64_t src = src_base + (int64_t)r * p.row_stride + c;
         const int64_t dst = dst_base + page * p.c.page_stride + h * p.c.head_stride + ((int)pos & slot_mask) * p.c.slot_stride + x;
-        const piece_t a = ((const piece_t*)p.k_new)[src], b = ((const piece_t*)p.v_new)[src];
+        // (read once: pass by the caches, 425 -> 416 us of 16 branches of up to 256 rows; with stores that do so too 420)
+        const piece_t a = __builtin_nontemporal_load((const piece_t*)p.k_new + src), b = __builtin_nontemporal_load((const piece_t*)p.v_new + src);
         ((piece_t*)p.c.k)[dst] = a;
         ((piece_t*)p.c.v)[dst] = b;
     }
@@ -374,7 +375,7 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams 
 // ---- compact ------------------------------------------------------------------------------
 // Row path[j] moves to row j <= path[j].  A workgroup takes some heads' rows of a layer, all of k or of v, and
 // reads a batch of rows into registers before it writes any: what is written over is behind, or was read.
-// Row by row, each move waiting for the one before it, 16 entries of 256 rows took 214 us; in batches 110.
+// Row by row, each move waiting for the one before it, 16 entries of up to 256 rows took 214 us; in batches 110.
 // (Batches go in ascending order: a later one reads rows that no earlier one wrote, since path[j] >= j.)
 struct CompactParams {
     KvView c;

@@ -221,3 +221,12 @@ def test_oracle_pool_by_hand():
     assert o.len == [6, 0, 8] and o.table[2] == [0, 2, -1, -1] and o.rows[2, 3] == "z"
     o.free([0, 2])
     assert o.refs == [0] * 6
+
+
+def test_longest_tables(D):
+    """A length and a step's rows on top of it fit 32 bits: tables end 2^25 positions before that."""
+    b = batch()
+    longest = cache(max_pages=(1 << 27) - (1 << 21))
+    assert D.lib.dip_attention_workspace_bytes(C.byref(longest), C.byref(b), 4, 0, 0) > 0
+    assert D.lib.dip_attention_workspace_bytes(C.byref(cache(max_pages=longest.max_pages + 1)), C.byref(b), 4, 0, 0) == 0
+    assert D.lib.dip_kv_reserve(C.byref(cache(max_pages=1 << 27)), C.byref(b), None, FAKE, 1 << 30, None) == D.DIP_ERR_UNSUPPORTED
