@@ -665,3 +665,20 @@ def test_verify_in_a_graph_and_many_entries():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(eager, (keep, path, token)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("rows", [[1, 1], [8, 5], [33, 64]])
+def test_contexts_that_may_be_long(dtype, d, rows):
+    """Tables for far more keys than there are, and no bound on the lengths: the loads and the cut for large calls."""
+    import paper_2412_01380_amd as D
+    s = Setup(dtype, [1200, 77], rows, 8, 2, d, 16, seed=d + rows[0])
+    table = torch.full((len(s.table), 8192), -1, dtype=torch.int32)
+    table[:, :s.max_pages] = s.table
+    s.cache = D.KvCache(s.cache.k, s.cache.v, table.cuda(), s.cache.seq_len, s.cache.page_refs)
+    s.batch = D.Batch(starts(rows), sum(rows), max(rows), seqs=ints(s.seqs))
+    par = [random_tree(np.random.default_rng(d), n) for n in rows]
+    for window, sinks in [(0, 0), (100000, 3)]:
+        s.check(s.run(window, sinks), window, sinks)
+        s.check(s.run(window, sinks, par), window, sinks, par)
