@@ -430,6 +430,7 @@ int32_t dip_tiered_mlp_forward(const dip_tiered_mlp* mlp, const float* x, int32_
  * elements from its start, so that heads may come before slots or behind them; all starts and
  * strides are multiples of 16 bytes.  Position i of sequence q is slot i % page_size of page
  * page_table[q * max_pages + i / page_size].
+ * page_table, seq_len and page_refs are written by the calls below and read by whoever likes.
  * A table entry or sequence number outside its range is never followed out of bounds: rows that
  * would be written there are dropped, and what is read there is taken from page 0. */
 typedef struct dip_kv_cache {
@@ -492,8 +493,11 @@ int32_t dip_kv_copy_pages(const dip_kv_cache* cache, const int32_t* src, const i
  * hold too when the call starts is exchanged for a free one, and what the entry has of it is copied
  * (copy on write; all layers).  The lowest free pages are given out, to the entries in order and to
  * each in order of position.  An entry whose pages, with all that earlier entries asked for, exceed the
- * free ones (or whose rows do not fit the table) gets none: granted[b] = 0 and its table stays;
- * otherwise granted[b] = 1.  Calling it again for the same rows changes nothing.
+ * free ones (or whose rows do not fit the table) gets none and its table stays.
+ * granted[b] = 1 if, in the end, all rows of entry b have pages that no other sequence holds, be they new,
+ * its own before, or left to it by the others that held them; otherwise granted[b] = 0, and until room is made for
+ * it the entry's rows are passed over by dip_kv_append and dip_kv_compact, and what attention gives for
+ * them is unspecified.  Calling it again for the same rows changes nothing if all entries were granted theirs.
  *   granted  n_batch words or NULL      ws  *_workspace_bytes() bytes, 256-aligned
  */
 size_t dip_kv_reserve_workspace_bytes(const dip_kv_cache* cache, const dip_batch* batch);
@@ -504,6 +508,8 @@ int32_t dip_kv_reserve(const dip_kv_cache* cache, const dip_batch* batch, int32_
  * Write keys and values of the step's rows into layers layer .. layer + n_layers - 1.  Row r of
  * layer l: n_kv_heads * head_dim elements at l * new_layer_stride + r * row_stride of k_new and
  * v_new (elements; multiples of 16 bytes; l counts from 0).  seq_len stays (dip_kv_compact commits).
+ * An entry of which some row has no page, or one that another sequence holds too (dip_kv_reserve granted it
+ * nothing, or it was forked since), is passed over whole.
  */
 int32_t dip_kv_append(const dip_kv_cache* cache, int32_t layer, int32_t n_layers, const dip_batch* batch,
                       const void* k_new, const void* v_new, int64_t row_stride, int64_t new_layer_stride,
@@ -513,8 +519,8 @@ int32_t dip_kv_append(const dip_kv_cache* cache, int32_t layer, int32_t n_layers
  * Keep keep[b] rows of every entry (device; values are clamped to its rows; NULL: all of them) and
  * commit: row path[row_start[b] + j] of the entry moves to row j, j < keep[b], in every layer (path:
  * device, n_rows entries, ascending within an entry, path[j] >= j; NULL: the first keep[b] rows
- * stay where they are), seq_len += keep[b], and pages beyond the new length are given up.  Rows
- * that have no page (an entry that dip_kv_reserve granted nothing) are not committed.
+ * stay where they are), seq_len += keep[b], and pages beyond the new length are given up.  An
+ * entry that dip_kv_append passes over keeps nothing: its length stays.
  */
 int32_t dip_kv_compact(const dip_kv_cache* cache, const dip_batch* batch, const int32_t* path, const int32_t* keep,
                        void* stream);

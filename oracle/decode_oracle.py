@@ -99,7 +99,8 @@ def verify(parents, tokens, p: np.ndarray, q: np.ndarray, u, u_sample: float, ma
 
 # ---- pages -----------------------------------------------------------------------------------------------
 class Pool:
-    """Tables, lengths and counts of a cache as lists, with the rows themselves in a dict by (page, slot)."""
+    """Tables, lengths and counts of a cache as lists, with the rows themselves in a dict by (page, slot).  Which
+    entries of a step were granted nothing is remembered from reserve on: append and compact pass them over."""
 
     def __init__(self, n_pages: int, page: int, n_seqs: int, max_pages: int):
         self.page, self.max_pages = page, max_pages
@@ -107,6 +108,7 @@ class Pool:
         self.len = [0] * n_seqs
         self.refs = [0] * n_pages
         self.rows = {}
+        self.refused = set()
 
     def free(self, seqs):
         for s in seqs:
@@ -132,16 +134,19 @@ class Pool:
                 if (a, s) in self.rows:
                     self.rows[b, s] = self.rows[a, s]
 
+    def pages_of(self, s, n):
+        """Places in the table that positions len .. len + n - 1 fall into."""
+        return range(self.len[s] // self.page, -(-(self.len[s] + n) // self.page)) if n else range(0)
+
     def reserve(self, seqs, counts):
         free = [i for i, r in enumerate(self.refs) if r == 0]
         shared = [r > 1 for r in self.refs]
         asked, granted = 0, []
         for s, n in zip(seqs, counts):
-            last = -(-(self.len[s] + n) // self.page) if n else 0
-            if last > self.max_pages or (n == 0 and self.len[s] > self.max_pages * self.page):
+            if self.len[s] + n > self.max_pages * self.page:
                 granted.append(0)
                 continue
-            want = [j for j in range(self.len[s] // self.page, last) if self.table[s][j] < 0 or shared[self.table[s][j]]] if n else []
+            want = [j for j in self.pages_of(s, n) if self.table[s][j] < 0 or shared[self.table[s][j]]]
             ok = not want or asked + len(want) <= len(free)
             granted.append(int(ok))
             if ok:
@@ -155,6 +160,12 @@ class Pool:
                     self.refs[new] += 1
                     self.table[s][j] = new
             asked += len(want)
+        # who is left alone with all its pages, the others having taken new ones, has its room too
+        for i, (s, n) in enumerate(zip(seqs, counts)):
+            if self.len[s] + n <= self.max_pages * self.page:
+                if all(self.table[s][j] >= 0 and self.refs[self.table[s][j]] == 1 for j in self.pages_of(s, n)):
+                    granted[i] = 1
+        self.refused = {s for s, ok in zip(seqs, granted) if not ok}
         return granted
 
     def place(self, s, pos):
@@ -165,23 +176,19 @@ class Pool:
     def append(self, seqs, rows):
         """rows: one list of row names per entry."""
         for s, names in zip(seqs, rows):
-            for t, name in enumerate(names):
-                at = self.place(s, self.len[s] + t)
-                if at:
-                    self.rows[at] = name
+            for t, name in enumerate(names if s not in self.refused else []):
+                self.rows[self.place(s, self.len[s] + t)] = name
 
     def compact(self, seqs, counts, paths, keep):
         for i, (s, n) in enumerate(zip(seqs, counts)):
             kept = min(max(keep[i], 0), n) if keep is not None else n
+            if s in self.refused:
+                kept = 0
             if paths is not None:
                 for j in range(kept):
-                    a, b = self.place(s, self.len[s] + paths[i][j]), self.place(s, self.len[s] + j)
-                    if a and b and a in self.rows and j < paths[i][j] < n:
-                        self.rows[b] = self.rows[a]
-            t = 0
-            while t < kept and self.place(s, self.len[s] + t):
-                t += 1
-            self.len[s] += t
+                    if j < paths[i][j] < n:
+                        self.rows[self.place(s, self.len[s] + j)] = self.rows[self.place(s, self.len[s] + paths[i][j])]
+            self.len[s] += kept
             for j in range(-(-self.len[s] // self.page), self.max_pages):
                 if self.table[s][j] >= 0:
                     self.refs[self.table[s][j]] -= 1

@@ -3,6 +3,8 @@
 // that nobody names, and the lowest ones are given out first, so that which page goes where
 // follows from the tables alone -- no list whose order would depend on the order of atomics.
 // Counts are changed with integer atomics, whose order does not show in the result.
+// Rows are written and committed only where all of an entry's rows have pages that no other sequence holds: that is
+// what reserve leaves an entry with, or else it grants it nothing (lacks_room).
 //
 // A decode step is reserve (two launches), append, compact (two): all wait for memory.  A few drafts of a few
 // branches are bound by the launches themselves (2 to 7 us each; six branches of 8 rows, 32 layers: 35 us with
@@ -260,6 +262,7 @@ __global__ void __launch_bounds__(kReserveThreads) kv_reserve_kernel(const Reser
     __syncthreads();
 
     // hand them out
+    const bool refused = n_wanted > n_free;
     int given = 0;
     for (int base = 0; base < n_items; base += kReserveThreads) {
         const int item = base + tid;
@@ -279,6 +282,21 @@ __global__ void __launch_bounds__(kReserveThreads) kv_reserve_kernel(const Reser
             const int slots = s_len[e] & (page - 1);
             if (item == s_first[e] && slots) p.copies[e] = {old, fresh, slots, 0};
         }
+    }
+
+    // Entries that were refused, by wavefront: whoever is left alone with all its pages, the others that held them having
+    // taken new ones, has its room too.  (Counts past this compute unit's cache, which may hold them as they were.)
+    if (!refused || !p.granted) return;
+    __syncthreads();
+    for (int e = tid >> 6; e < p.b.n_batch; e += kReserveThreads / 64) {
+        const int first = s_first[e], end = s_first[e + 1];
+        if (s_need[e] || first == end) continue;
+        bool lacks = false;
+        for (int item = first + lane; item < end; item += 64) {
+            const int held = *table_at(item, e);
+            lacks |= !is_page(p.c, held) || __hip_atomic_load(&p.c.refs[held], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > 1;
+        }
+        if (!__any(lacks) && lane == 0) p.granted[e] = 1;
     }
 }
 
@@ -330,6 +348,20 @@ __global__ void __launch_bounds__(kThreads) kv_copy_kernel(const CopyParams p) {
     }
 }
 
+// Whether some row of an entry (of one or more) falls into no page or into one that another sequence holds: this
+// thread's part of the pages, true for any thread of a workgroup says that the entry has no room.
+// This may be asked while other entries give pages up: a page that two tables name came to be so by a fork, so that it
+// lies within the committed length of both, and only pages beyond that are given up meanwhile.
+__device__ __forceinline__ bool lacks_room(const KvView& c, const int32_t* table, int len, int rows) {
+    const int last = (len + rows - 1) >> c.page_shift;
+    bool lacks = last >= c.max_pages;
+    for (int j = (len >> c.page_shift) + threadIdx.x; j <= min(last, c.max_pages - 1); j += kThreads) {
+        const int page = table[j];
+        lacks |= !is_page(c, page) || c.refs[page] > 1;
+    }
+    return lacks;
+}
+
 // ---- append -------------------------------------------------------------------------------
 // A thread moves 16 bytes of k and the same of v.  Bound by bytes (1.1 GB read and written in 229 us at 16
 // entries of up to 256 rows, 40 layers), small ones by latency: hence fewer rows to a workgroup then.
@@ -356,19 +388,25 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams 
     const int slot_mask = (1 << p.c.page_shift) - 1;
     const int64_t src_base = (int64_t)blockIdx.z * p.new_layer_stride + (int64_t)(er.first + t0) * p.row_stride;
     const int64_t dst_base = (int64_t)(p.layer + (int)blockIdx.z) * p.c.layer_stride;
+    // (read once: pass by the caches, 425 -> 416 us of 16 branches of up to 256 rows; with stores that do so too 420.  The
+    // first pieces are on their way while the pages are looked at.)
+    piece_t a, b;
+    auto load = [&](int i) {
+        const int r = i / per_row;
+        const int64_t src = src_base + (int64_t)r * p.row_stride + (i - r * per_row);
+        a = __builtin_nontemporal_load((const piece_t*)p.k_new + src);
+        b = __builtin_nontemporal_load((const piece_t*)p.v_new + src);
+    };
+    if ((int)threadIdx.x < n) load(threadIdx.x);
+    if (__syncthreads_or(lacks_room(p.c, table, len, er.rows))) return;
     for (int i = threadIdx.x; i < n; i += kThreads) {
         const int r = i / per_row, c = i - r * per_row;
-        const int64_t pos = (int64_t)len + t0 + r;
-        if ((pos >> p.c.page_shift) >= p.c.max_pages) continue;
-        const int page = table[pos >> p.c.page_shift];
-        if (!is_page(p.c, page)) continue;
+        const int pos = len + t0 + r, page = table[pos >> p.c.page_shift];
         const int h = c / p.c.pieces, x = c - h * p.c.pieces;
-        const int64_t src = src_base + (int64_t)r * p.row_stride + c;
-        const int64_t dst = dst_base + page * p.c.page_stride + h * p.c.head_stride + ((int)pos & slot_mask) * p.c.slot_stride + x;
-        // (read once: pass by the caches, 425 -> 416 us of 16 branches of up to 256 rows; with stores that do so too 420)
-        const piece_t a = __builtin_nontemporal_load((const piece_t*)p.k_new + src), b = __builtin_nontemporal_load((const piece_t*)p.v_new + src);
+        const int64_t dst = dst_base + page * p.c.page_stride + h * p.c.head_stride + (pos & slot_mask) * p.c.slot_stride + x;
         ((piece_t*)p.c.k)[dst] = a;
         ((piece_t*)p.c.v)[dst] = b;
+        if (i + kThreads < n) load(i + kThreads);
     }
 }
 
@@ -398,13 +436,12 @@ __global__ void __launch_bounds__(kThreads) kv_move_kernel(const CompactParams p
     piece_t* base = (piece_t*)(blockIdx.z / groups ? p.c.v : p.c.k) + (int64_t)blockIdx.y * p.c.layer_stride + h0 * p.c.head_stride;
     const int len = entry_len(p.c, seq);
     const int32_t* table = p.c.table + (size_t)seq * p.c.max_pages;
+    const bool lacks = lacks_room(p.c, table, len, er.rows);
     const int32_t* path = p.path + er.first;
     const int slot_mask = (1 << p.c.page_shift) - 1;
-    auto place = [&](int row) -> int64_t {
-        const int64_t pos = (int64_t)len + row;
-        if ((pos >> p.c.page_shift) >= p.c.max_pages) return -1;
-        const int page = table[pos >> p.c.page_shift];
-        return is_page(p.c, page) ? page * p.c.page_stride + ((int)pos & slot_mask) * p.c.slot_stride : -1;
+    auto place = [&](int row) {                       // (of an entry that has room)
+        const int pos = len + row;
+        return table[min(pos >> p.c.page_shift, p.c.max_pages - 1)] * p.c.page_stride + (pos & slot_mask) * p.c.slot_stride;
     };
     const int per = heads * p.c.pieces;               // pieces of a row
     // rows of a batch; a row of more pieces than a workgroup holds goes in parts, each through all rows
@@ -416,11 +453,10 @@ __global__ void __launch_bounds__(kThreads) kv_move_kernel(const CompactParams p
             const int n_rows = min(rows, kept - j0), n = n_rows * wide;
             if ((int)threadIdx.x < n_rows) {
                 const int j = j0 + threadIdx.x, src = path[j];
-                const int64_t from = src > j && src < er.rows ? place(src) : -1, to = place(j);
-                s_from[threadIdx.x] = to < 0 ? -1 : from;
-                s_to[threadIdx.x] = to;
+                s_from[threadIdx.x] = src > j && src < er.rows ? place(src) : -1;
+                s_to[threadIdx.x] = place(j);
             }
-            __syncthreads();
+            if (__syncthreads_or(lacks)) return;
             piece_t val[kMoves];
 #pragma unroll
             for (int m = 0; m < kMoves; ++m) {
@@ -446,16 +482,9 @@ __global__ void __launch_bounds__(kThreads) kv_commit_kernel(const CompactParams
     const int kept = kept_rows(p, er);
     const int seq = entry_seq(p.b, p.c, blockIdx.x);
     if (seq < 0) return;
-    __shared__ int s_end;     // first place in the table without a page, from the committed length on
     const int before = entry_len(p.c, seq), page = 1 << p.c.page_shift;
     int32_t* row = p.c.table + (size_t)seq * p.c.max_pages;
-    if (threadIdx.x == 0) s_end = p.c.max_pages;
-    __syncthreads();
-    if (kept)
-        for (int j = (before >> p.c.page_shift) + threadIdx.x; j <= (before + kept - 1) >> p.c.page_shift && j < p.c.max_pages; j += kThreads)
-            if (!is_page(p.c, row[j])) atomicMin(&s_end, j);
-    __syncthreads();
-    const int len = min(before + kept, max(before, s_end << p.c.page_shift));
+    const int len = kept && !__syncthreads_or(lacks_room(p.c, row, before, er.rows)) ? before + kept : before;
     const int held = (len + page - 1) >> p.c.page_shift;
     for (int j = held + threadIdx.x; j < p.c.max_pages; j += kThreads) give_up(p.c, row + j);
     if (threadIdx.x == 0) p.c.seq_len[seq] = len;
