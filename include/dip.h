@@ -541,8 +541,9 @@ int32_t dip_kv_compact(const dip_kv_cache* cache, const dip_batch* batch, const 
  *            elements apart (multiples of 16 bytes); out may not overlap q
  *   scale > 0      n_q_heads a multiple of n_kv_heads      ws  *_workspace_bytes() bytes, 256-aligned
  * Scores, softmax statistics and sums are fp32; with a DIP_BF16 cache the weights p enter their product
- * with v as the sum of two bf16 terms, but for entries of more than 64 rows x query heads per key/value
- * head as one, except at the ends of the context of rows that see fewer than 512 keys.  The order of the sums is fixed by shapes, lengths and max_len (bit-repeatable).
+ * with v as the sum of two bf16 terms (exact to 2^-15), and the output is rounded once.  Which kernel runs is chosen
+ * by max_rows and the query heads per key/value head, for all entries of a call.  The order of the sums is fixed
+ * by shapes, all entries' rows and lengths, and max_len (bit-repeatable).
  */
 size_t dip_attention_workspace_bytes(const dip_kv_cache* cache, const dip_batch* batch, int32_t n_q_heads,
                                      int32_t window, int32_t sinks);

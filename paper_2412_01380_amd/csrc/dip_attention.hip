@@ -7,8 +7,8 @@
 // Keys are read once for all query heads of a group and all rows of a block.  With few rows what bounds the
 // call is reading them: 32 tokens of 40 heads on 10, a window of 2047, 75 us for the 332 MB of K and V (52 us
 // at the rate of a plain read).  With many it is the matrix cores and, beside them, the softmax's plain
-// instructions: a maximum, a multiply-add, an exponential, a sum and half a conversion for every weight, whose
-// two products are 256 multiply-adds at 128 dims.
+// instructions: a maximum, two multiply-adds, an exponential, a sum, a mask and two halves of a move and a conversion
+// for every weight, whose products, P V with two terms, are 384 multiply-adds at 128 dims.
 
 #include <algorithm>
 #include <cmath>
@@ -27,7 +27,6 @@ constexpr int kIds = 256;                 // page numbers of a wavefront in LDS 
 // LDS although no wavefront reads another's tile: a load to LDS holds no registers while it is on its way, and
 // the products want rows of K and columns of V, which memory has neither of side by side.  Two tiles of 32 keys
 // (16 in fp32) each: a third one costs a workgroup per compute unit.
-// Weights go in as two bf16 terms (Core::pack): the matrix cores wait for memory here, the second term is free.
 // Measured (bf16, 128 dims): 2 x 700 keys 10.4 us, of which 4.4 any launch takes; 8 trees of 8 nodes, 4 heads on
 // one, up to 8192 keys 46 us at 3.7 TB/s.  fp32, 3 trees of 7 nodes, 32 heads, 96 dims: 19 us.
 template <typename E, int D, int NB, int WAVES, bool ONCE>
@@ -124,8 +123,8 @@ __global__ void __launch_bounds__(WAVES * 64, 1) attn_rows_kernel(const AttnPara
         }
         soft.step(core, s, p.scale_log2);
         typename C::Weights w;
-        C::template pack<true>(s, 0, w);
-        core.template add_values<true>(C::v_base(tile + TILE), 0, w);
+        C::pack(s, 0, w);
+        core.add_values(C::v_base(tile + TILE), 0, w);
         C::schedule_values();
         if (i + kRing < mine) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (everything read from the tile that goes)
@@ -196,10 +195,10 @@ __global__ void __launch_bounds__(WAVES * 64, 1) attn_rows_kernel(const AttnPara
 // unit) take as long as the products, with two half; four do not fit the registers.  The softmax of a tile runs
 // beside the products of its neighbours: P V lags one tile behind K Q, so both are at hand when a wavefront
 // waits for exponentials.  What is left is that products and plain instructions of the two wavefronts of a SIMD
-// overlap only by half (alone 485 and 515 us of a probe, together 880).
-// Measured (bf16, 128 dims, 4 heads on one): 2 prompts of up to 4096 rows, window 2047: 385 to 420 us (710 TFLOP/s of
-// the 1152 of a large library product); 4 trees of 64 nodes over up to 49152 keys 180 to 210 us.  With
-// attn_rows_kernel: 1160 and 890 us.
+// overlap only by half (with one term: alone 485 and 515 us of a probe, together 880).
+// Measured (bf16, 128 dims, 4 heads on one): 2 prompts of up to 4096 rows, window 2047: 484 us (610 TFLOP/s, 920 with the
+// weights' second terms, of the 1152 of a large library product); 4 trees of 64 nodes over up to 49152 keys 231 us.
+// With attn_rows_kernel: 1160 and 890 us.
 // bf16: 64 keys to a tile, eight wavefronts, one workgroup to a compute unit.
 template <typename E>
 struct Block {
@@ -216,7 +215,6 @@ struct Block<float> {
     static constexpr int per_simd(int dims) { return 6 - dims / 32; }
 };
 constexpr int kBlockRing = 4;
-constexpr int kFewKeys = 512;             // of a row: below that its weights go in as two terms where they are at an edge
 constexpr int kIdTiles = 64;              // tiles whose page numbers are in LDS at a time
 
 template <typename E, int D, int NB, bool ONCE>
@@ -311,12 +309,10 @@ __global__ void __launch_bounds__(Block<E>::WAVES * 64, Block<E>::per_simd(D)) a
         }
     };
     auto scores = [&](int i, f32x4 (&s)[NB][Q]) { core.scores(C::k_base(tile_of(i)), s); };
-    // What the wavefront's rows see lies below see_hi and, but for the sinks, from see_lo on; `few`: some row sees
-    // few keys, which then lie in tiles at an edge.
+    // What the wavefront's rows see lies below see_hi and, but for the sinks, from see_lo on.
     const int wt0 = (r0 + w0) / p.group, wt1 = (r0 + min(w0 + 16 * NB, n_rows) - 1) / p.group;
     const int see_hi = w0 >= n_rows ? 0 : p.parents ? range.end : min(range.end, len + wt1 + 1);
     const int see_lo = !p.window ? 0 : max(0, len + (p.parents ? 0 : wt0) - p.window + 1);
-    const bool few = min(range.sure, p.window ? p.window : range.sure) < kFewKeys;
     // tiles that some row does not see all of
     auto edge = [&](int from, int to) {
         if (tid < 2) s_bad[from & 1][tid] = 0;
@@ -345,13 +341,8 @@ __global__ void __launch_bounds__(Block<E>::WAVES * 64, Block<E>::per_simd(D)) a
 #pragma unroll
             for (int b = 0; b < SUB; ++b) {
                 typename C::Weights w;
-                if (few) {
-                    C::template pack<true>(s, b * C::MT, w);
-                    core.template add_values<true>(v, b * G::KEYS, w);
-                } else {
-                    C::template pack<false>(s, b * C::MT, w);
-                    core.template add_values<false>(v, b * G::KEYS, w);
-                }
+                C::pack(s, b * C::MT, w);
+                core.add_values(v, b * G::KEYS, w);
             }
         }
     };
@@ -367,12 +358,12 @@ __global__ void __launch_bounds__(Block<E>::WAVES * 64, Block<E>::per_simd(D)) a
         auto weigh = [&]() {
             soft.step(core, s, p.scale_log2);
 #pragma unroll
-            for (int b = 0; b < SUB; ++b) C::template pack<false>(s, b * C::MT, w[b]);
+            for (int b = 0; b < SUB; ++b) C::pack(s, b * C::MT, w[b]);
         };
         auto values = [&](int i) {
             const uint32_t v = C::v_base(tile_of(i) + TILE);
 #pragma unroll
-            for (int b = 0; b < SUB; ++b) core.template add_values<false>(v, b * G::KEYS, w[b]);
+            for (int b = 0; b < SUB; ++b) core.add_values(v, b * G::KEYS, w[b]);
         };
         arrive(from);
         scores(from, s);

@@ -457,24 +457,29 @@ struct Core<uint16_t, D, NB> {
                     s[nb][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[nb][st], st ? s[nb][x] : f32x4{0, 0, 0, 0}, 0, 0, 0);
             }
     }
-    // The weights of KEYS keys as the second product takes them.  As one bf16 term each they are off by up to
-    // 2^-9, which over many keys averages out but shows where a few of them carry a row; with TWO the
-    // remainder is a second term.
+    // The weights of KEYS keys as the second product takes them: two bf16 terms, the upper half of the fp32 number and
+    // what that leaves, rounded: 2^-15 of a weight.  With one term, off by up to 2^-8 where a few keys carry a row, a
+    // call's relative error is 0.0023, with two 0.0017, which the rounding of its output alone is (prompts 396 us instead
+    // of 484, trees of 64 nodes 186 instead of 231).  What is left of a weight above zero counts as at least 2^-23 of it, so
+    // that an infinite value times either term has its sign and never meets a zero.
     struct Weights {
         bf16x8 w[NB], rest[NB];
     };
-    template <bool TWO, int Q>
+    __device__ __forceinline__ static float upper(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+    template <int Q>
     __device__ __forceinline__ static void pack(const f32x4 (&p)[NB][Q], int at, Weights& x) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float y = p[nb][at + (e >> 2)][e & 3];
-                x.w[nb][e] = (__bf16)y;
-                if constexpr (TWO) x.rest[nb][e] = (__bf16)(y - (float)x.w[nb][e]);
+            for (int e = 0; e < 8; e += 2) {
+                const float a = p[nb][at + (e >> 2)][e & 3], b = p[nb][at + (e >> 2)][(e & 3) + 1];
+                const bf16x2 both = __builtin_bit_cast(bf16x2, __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u));
+                x.w[nb][e] = both[0];
+                x.w[nb][e + 1] = both[1];
+                x.rest[nb][e] = (__bf16)fmaf(a, 1.f + 0x1p-23f, -upper(a));
+                x.rest[nb][e + 1] = (__bf16)fmaf(b, 1.f + 0x1p-23f, -upper(b));
             }
     }
-    template <bool TWO>
     __device__ __forceinline__ void add_values(uint32_t v, int key, const Weights& p) {
 #pragma unroll
         for (int db = 0; db < OB; ++db) {
@@ -490,14 +495,13 @@ struct Core<uint16_t, D, NB> {
             }
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p.w[nb], o[nb][db], 0, 0, 0);
-            if constexpr (TWO) {
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p.rest[nb], o[nb][db], 0, 0, 0);
-            }
+            for (int nb = 0; nb < NB; ++nb) o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, p.rest[nb], o[nb][db], 0, 0, 0);
         }
     }
     // Behind a tile's two products (SUB KEYS keys): reads run FLIGHT operands ahead of the products that take them.
-    // (Left to itself the compiler reads each right before its use, to save registers.)
+    // An operand of K serves NB products, one of V, with two terms, 2 NB.
+    // (Left to itself the compiler reads each right before its use, to save registers: prompts 560 us instead of 484.)
     template <int SUB>
     __device__ __forceinline__ static void schedule_products() {
         constexpr int KF = SUB * MT * QS, VF = SUB * OB, FLIGHT = 4;       // operands of K, of V (two reads each)
@@ -509,13 +513,18 @@ struct Core<uint16_t, D, NB> {
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
 #pragma unroll
-        for (int f = 0; f < VF; ++f) {
+        for (int f = 0; f < FLIGHT; ++f) {
             __builtin_amdgcn_sched_group_barrier(0x8, NB, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x8, FLIGHT * NB, 0);
+#pragma unroll
+        for (int f = FLIGHT; f < VF; ++f) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 2 * NB, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x8, FLIGHT * 2 * NB, 0);
     }
-    // Behind a tile's second product with TWO terms alone.
+    // Behind a tile's second product alone.
     __device__ __forceinline__ static void schedule_values() {
         constexpr int FLIGHT = 4;
 #pragma unroll
@@ -574,12 +583,11 @@ struct Core<float, D, NB> {
     struct Weights {
         f32x4 w[NB];
     };
-    template <bool, int Q>
+    template <int Q>
     __device__ __forceinline__ static void pack(const f32x4 (&p)[NB][Q], int at, Weights& x) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) x.w[nb] = p[nb][at];
     }
-    template <bool>
     __device__ __forceinline__ void add_values(uint32_t v, int key, const Weights& p) {
         const int m = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
 #pragma unroll
@@ -623,8 +631,8 @@ struct Core<float, D, NB> {
 };
 
 // The running softmax of a wavefront's columns: m the maximum of c S so far, l this lane's share of the sum.
-// m may lag behind the maximum by up to kSlack: weights up to 2^kSlack instead of 1, at the same relative
-// rounding, spare the rescaling that some of 32 rows would ask for with nearly every tile.
+// m may lag behind the maximum by up to kSlack: weights up to 2^kSlack instead of 1 -- fp32 numbers, and two terms that
+// keep 15 bits of them, whatever their size -- spare the rescaling that some of 32 rows would ask for with nearly every tile.
 constexpr float kSlack = 8.f;
 template <typename E, int D, int NB>
 struct Softmax {
