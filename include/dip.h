@@ -456,8 +456,8 @@ typedef struct dip_kv_cache {
 /* The rows of one step.  Entry b is sequence seqs[b] with rows row_start[b] .. row_start[b+1] - 1
  * of every row-indexed array; its row t stands at position seq_len + t (in a tree: node t).  The
  * host fields size the launches: rows of an entry beyond max_rows, and rows from n_rows on, are
- * not looked at, and a sequence longer than max_len (its new rows included) is read up to max_len
- * positions only. */
+ * not looked at, and of a sequence longer than max_len (its new rows included), or than its table,
+ * positions from there on are seen by nobody. */
 typedef struct dip_batch {
     const int32_t* seqs;      /* device; n_batch distinct sequences (dip_verify_tree: may be NULL)  */
     const int32_t* row_start; /* device; n_batch + 1 entries, ascending from 0 to n_rows            */

@@ -123,6 +123,7 @@ __device__ __forceinline__ void tree_masks(const int32_t* parents, int rows, uin
     out[lane] = up == -1 ? mask : 0;
 }
 
+// (Nothing from max_len on: a tile that it cuts holds other positions' keys there.)
 __device__ __forceinline__ RowSees row_sees(const AttnParams& p, int len, int t, const uint64_t* masks) {
     RowSees r;
     int pos = len + t;
@@ -131,9 +132,11 @@ __device__ __forceinline__ RowSees row_sees(const AttnParams& p, int len, int t,
         r.tree = masks[t];
         pos = len + __popcll(r.tree) - 1;
         r.hi = r.tree ? len : 0;
+        r.tree &= below(p.max_len - len);
     } else {
         r.hi = pos + 1;
     }
+    r.hi = min(r.hi, p.max_len);
     r.lo = p.window ? max(0, pos - p.window + 1) : 0;
     return r;
 }
@@ -180,7 +183,7 @@ struct Units {
         x.first = er.first;
         x.rows = er.rows;
         x.seq = entry_seq(p.b, p.c, e);
-        x.len = x.seq >= 0 ? min(entry_len(p.c, x.seq), p.max_len) : 0;
+        x.len = x.seq >= 0 ? entry_len(p.c, x.seq) : 0;
         const int all = er.rows * p.group;
         x.row_blocks = (all + ROWS - 1) / ROWS;
         x.blocks = x.row_blocks * p.c.n_heads;
