@@ -537,6 +537,9 @@ int32_t dip_kv_compact(const dip_kv_cache* cache, const dip_batch* batch, const 
  * positions j < seq_len those with  j > pos - window  or  j < sinks.
  * window 0 means no bound (sinks then change nothing).  A row that sees nothing, an absent node, and a row
  * whose scores are all -inf get zeros.  Positions that a row does not see do not matter to it, whatever they hold.
+ * A value that is not finite at a position that a row sees makes that channel of the row what the sum gives
+ * (infinite, or NaN where a NaN or both infinities meet, or where its weight vanishes in fp32); the other channels are as
+ * they were.
  *   q, out   n_rows rows of n_q_heads * head_dim elements of the cache's type, q_stride / out_stride
  *            elements apart (multiples of 16 bytes); out may not overlap q
  *   scale > 0      n_q_heads a multiple of n_kv_heads      ws  *_workspace_bytes() bytes, 256-aligned

@@ -105,21 +105,19 @@ __global__ void __launch_bounds__(WAVES * 64, 1) attn_rows_kernel(const AttnPara
     if (mine > 0) fetch(0);
     if (mine > 1) fetch(1);
     if (shares > 1 && tid == 0) ticket_open(p.tickets + (size_t)u.first * kTicketStride, p.epoch);
+    bool spoilt = false;                                  // (something was taken out of a tile)
+    auto whole = [&](int j0) { return j0 + KEYS <= range.sure && (j0 >= range.from || j0 + KEYS <= p.sinks); };
     for (int i = 0; i < mine; ++i) {
         if (i + 1 < mine) wait_loads<2 * LOADS>(); else wait_loads<0>();
         const int j0 = tile_of(i);
         const uint32_t tile = ring_at + (i & (kRing - 1)) * (2 * TILE);
         f32x4 s[NB][C::MT];
         core.scores(C::k_base(tile), s);
-        const bool whole = j0 + KEYS <= range.sure && (j0 >= range.from || j0 + KEYS <= p.sinks);
-        if (!whole) {
-            uint64_t bad = 0;
+        if (!whole(j0)) {
 #pragma unroll
-            for (int x = 0; x < LOADS; ++x) bad |= take_out<G>(tile + TILE, x);
-            if (__any(bad != 0))
-                for (int off = 1; off < 64; off <<= 1) bad |= __shfl_xor((uint32_t)bad, off);
+            for (int x = 0; x < LOADS; ++x) spoilt |= take_out<G>(tile + TILE, x);
             asm volatile("" ::: "memory");
-            apply_sees(s, row, j0, p.sinks, len, bad);
+            apply_sees(s, row, j0, p.sinks, len);
         }
         soft.step(core, s, p.scale_log2);
         typename C::Weights w;
@@ -131,6 +129,9 @@ __global__ void __launch_bounds__(WAVES * 64, 1) attn_rows_kernel(const AttnPara
             fetch(i + kRing);
         }
     }
+
+    if (__any(spoilt))
+        put_back<E, D, NB, KEYS>(p, core, row, vbase, seq, len, range.end, mine, [&](int i) { const int j0 = tile_of(i); return whole(j0) ? -1 : j0; });
 
     // join the wavefronts
 #pragma unroll
@@ -228,7 +229,7 @@ __global__ void __launch_bounds__(Block<E>::WAVES * 64, Block<E>::per_simd(D)) a
     __shared__ __align__(1024) char s_ring[kBlockRing * 2 * TILE];
     __shared__ int s_ids[kIdTiles * KEYS];
     __shared__ uint64_t s_tree[64];
-    __shared__ uint32_t s_bad[2][2];
+    __shared__ int s_spoilt;                              // something was taken out of a tile
     __shared__ Unit s_unit;
 
     // XCD x gets consecutive units, so that blocks of one head find its keys in their L2
@@ -251,7 +252,7 @@ __global__ void __launch_bounds__(Block<E>::WAVES * 64, Block<E>::per_simd(D)) a
     const int per = max(1, KEYS >> p.c.page_shift);
     page_ids<KEYS, THREADS>(p.c, seq, range, begin, min(n, kIdTiles), per, s_ids);
     if (p.parents && wave == 0) tree_masks(p.parents + u.first_row, u.rows, s_tree);
-    if (tid < 4) s_bad[tid >> 1][tid & 1] = 0;
+    if (tid == 0) s_spoilt = 0;
     __syncthreads();
 
     C core;
@@ -315,27 +316,21 @@ __global__ void __launch_bounds__(Block<E>::WAVES * 64, Block<E>::per_simd(D)) a
     const int see_lo = !p.window ? 0 : max(0, len + (p.parents ? 0 : wt0) - p.window + 1);
     // tiles that some row does not see all of
     auto edge = [&](int from, int to) {
-        if (tid < 2) s_bad[from & 1][tid] = 0;
         RowSees row[NB];
         sees_of(fresh(), row);
         for (int i = from; i < to; ++i) {
             arrive(i);
-            if (tid < 2) s_bad[(i + 1) & 1][tid] = 0;
-            uint64_t bad = 0;
+            bool bad = false;
 #pragma unroll
             for (int m = 0; m < MINE; ++m) bad |= take_out<G>(tile_of(i) + TILE, (wave * MINE + m) % LOADS);
-            if (bad) {
-                atomicOr(&s_bad[i & 1][0], (uint32_t)bad);
-                atomicOr(&s_bad[i & 1][1], (uint32_t)(bad >> 32));
-            }
+            if (bad) s_spoilt = 1;
             barrier();
-            bad = ((uint64_t)s_bad[i & 1][1] << 32) | s_bad[i & 1][0];
             // (a wavefront that sees nothing of the tile only keeps the others' time)
             const int j0 = tile_at(range, begin + i) * KEYS;
             if (j0 >= see_hi || (j0 + KEYS <= see_lo && j0 >= p.sinks)) continue;
             f32x4 s[NB][Q];
             scores(i, s);
-            apply_sees(s, row, j0, p.sinks, len, bad);
+            apply_sees(s, row, j0, p.sinks, len);
             soft.step(core, s, p.scale_log2);
             const uint32_t v = C::v_base(tile_of(i) + TILE);
 #pragma unroll
@@ -389,6 +384,9 @@ __global__ void __launch_bounds__(Block<E>::WAVES * 64, Block<E>::per_simd(D)) a
 
     RowSees row[NB];
     sees_of(fresh(), row);
+    if (s_spoilt)                                         // (set in front of a barrier that everybody has passed)
+        put_back<E, D, NB, KEYS>(p, core, row, vbase, seq, len, range.end, n,
+                                 [&](int i) { return i >= mid0 && i < mid1 ? -1 : tile_at(range, begin + i) * KEYS; });
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         const int r = 16 * nb + (lane & 15) + w0;

@@ -379,25 +379,30 @@ __device__ __forceinline__ void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-// Load x of a V tile in LDS: this lane's piece becomes zero if it is not finite, so that a weight of zero takes
-// it out; the bit of its key, or 0.  (Only tiles that some row does not see all of are looked through: in the
-// others what is not finite belongs in the results.)
+// Load x of a V tile in LDS: what is not finite in this lane's piece becomes zero, so that a weight of zero takes it
+// out; whether there was any.  (Only tiles that some row does not see all of are looked through: in the others what
+// is not finite belongs in the results.)
 template <typename G>
-__device__ __forceinline__ uint64_t take_out(uint32_t v, int x) {
+__device__ __forceinline__ bool take_out(uint32_t v, int x) {
     const int lane = threadIdx.x & 63;
     auto* at = (__attribute__((address_space(3))) u32x4*)(lds_char*)(size_t)(v + x * 1024 + lane * 16);
-    const u32x4 w = *at;
+    u32x4 w = *at;
     bool inf = false;
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
         inf |= (w[y] & 0x7f800000u) == 0x7f800000u;
         if constexpr (G::ES == 2) inf |= (w[y] & 0x7f80u) == 0x7f80u;
     }
-    if (!inf) return 0;
-    *at = u32x4{0, 0, 0, 0};
-    return 1ull << ((x * 64 + lane) / G::CPR);
+    if (!inf) return false;
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+        if ((w[y] & 0x7f800000u) == 0x7f800000u) w[y] &= G::ES == 2 ? 0xffffu : 0u;
+        if constexpr (G::ES == 2)
+            if ((w[y] & 0x7f80u) == 0x7f80u) w[y] &= 0xffff0000u;
+    }
+    *at = w;
+    return true;
 }
-
 // ---- the two products ----------------------------------------------------------------------------
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 // maximum / sum over the four lanes of a column (lane ^ 16, lane ^ 32)
@@ -542,6 +547,7 @@ struct Core<uint16_t, D, NB> {
     // first dim of the four that o[nb][x] .. hold: quad y of them, y < OB
     __device__ __forceinline__ static int quad_dim(int y) { return 16 * y + 4 * ((threadIdx.x & 63) >> 4); }
     __device__ __forceinline__ f32x4 quad(int nb, int y) const { return o[nb][y]; }
+    __device__ __forceinline__ void add_quad(int nb, int y, f32x4 x) { o[nb][y] += x; }
 };
 
 template <int D, int NB>
@@ -631,6 +637,14 @@ struct Core<float, D, NB> {
         if constexpr (VE == 4) return f32x4{o[nb][4 * b][x], o[nb][4 * b + 1][x], o[nb][4 * b + 2][x], o[nb][4 * b + 3][x]};
         else return f32x4{o[nb][2 * b][2 * x], o[nb][2 * b + 1][2 * x], o[nb][2 * b][2 * x + 1], o[nb][2 * b + 1][2 * x + 1]};
     }
+    __device__ __forceinline__ void add_quad(int nb, int y, f32x4 v) {
+        const int b = y / VE, x = y % VE;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (VE == 4) o[nb][4 * b + e][x] += v[e];
+            else o[nb][2 * b + (e & 1)][2 * x + (e >> 1)] += v[e];
+        }
+    }
 };
 
 // The running softmax of a wavefront's columns: m the maximum of c S so far, l this lane's share of the sum.
@@ -687,22 +701,47 @@ struct Softmax {
 };
 
 // Scores of a tile from position j0 on that some row does not see all of: what a row does not see counts for
-// nothing, and what it sees of a key whose value is not finite (`bad`) makes it NaN.
+// nothing.
 template <int NB, int Q>
-__device__ __forceinline__ void apply_sees(f32x4 (&s)[NB][Q], const RowSees (&row)[NB], int j0, int sinks, int len, uint64_t bad) {
+__device__ __forceinline__ void apply_sees(f32x4 (&s)[NB][Q], const RowSees (&row)[NB], int j0, int sinks, int len) {
     const int g4 = 4 * ((threadIdx.x & 63) >> 4);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         const uint64_t bits = sees(row[nb], j0, sinks, len) >> g4;
-        if (bad) {
-            const uint64_t spoilt = bad >> g4;
-#pragma unroll
-            for (int x = 0; x < 4 * Q; ++x)
-                if ((spoilt >> (16 * (x >> 2) + (x & 3))) & 1) s[nb][x >> 2][x & 3] = NAN;
-        }
 #pragma unroll
         for (int x = 0; x < 4 * Q; ++x)
             s[nb][x >> 2][x & 3] = (bits >> (16 * (x >> 2) + (x & 3))) & 1 ? s[nb][x >> 2][x & 3] : -INFINITY;
+    }
+}
+// What take_out took out of tiles, to the sums of the rows that see it, when these are done: a weight is above zero, so
+// what is not finite comes through as it is.  Values come from the cache again, KEYS of them from position j0_of(i) on, i < n
+// (none where that is negative).
+template <typename E, int D, int NB, int KEYS, typename F>
+__device__ __forceinline__ void put_back(const AttnParams& p, Core<E, D, NB>& core, const RowSees (&row)[NB], const char* vbase, int seq,
+                                         int len, int end, int n, F j0_of) {
+    for (int i = 0; i < n; ++i) {
+        const int j0 = j0_of(i);
+        for (int m = 0; j0 >= 0 && m < KEYS && j0 + m < end; ++m) {
+            const int pos = j0 + m, named = p.c.table[(size_t)seq * p.c.max_pages + (pos >> p.c.page_shift)];
+            const int page = (unsigned)named < (unsigned)p.c.n_pages ? named : 0;
+            const char* from = vbase + (page * p.c.page_stride + (pos & ((1 << p.c.page_shift) - 1)) * p.c.slot_stride) * 16;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const bool seen = (sees(row[nb], pos, p.sinks, len) & 1) != 0;
+#pragma unroll
+                for (int y = 0; y < Core<E, D, NB>::OB; ++y) {
+                    f32x4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int dim = Core<E, D, NB>::quad_dim(y) + e;
+                        if constexpr (sizeof(E) == 4) v[e] = ((const float*)from)[dim];
+                        else v[e] = __uint_as_float((uint32_t)((const uint16_t*)from)[dim] << 16);
+                        v[e] = seen && (__float_as_uint(v[e]) & 0x7f800000u) == 0x7f800000u ? v[e] : 0.f;
+                    }
+                    core.add_quad(nb, y, v);
+                }
+            }
+        }
     }
 }
 
