@@ -612,6 +612,16 @@ def dip_tiered_mlp_forward(mlp: TieredMlp, x, k_in: int, k_mid: int, cache_in: C
 DIP_MAX_BATCH, DIP_MAX_TREE = 1024, 64
 
 
+def _strides(t) -> tuple:
+    """Strides of a tensor, those of dimensions of one entry as if it were contiguous there (torch leaves anything)."""
+    out, inner = [], 1
+    for n, s in zip(reversed(t.shape), reversed(t.stride())):
+        s = inner if n == 1 else s
+        out.append(s)
+        inner = n * s
+    return tuple(reversed(out))
+
+
 class KvCache:
     """A paged key/value cache over caller-owned device tensors: k and v [n_layers][n_pages][n_kv_heads]
     [page_size][head_dim] (float32 or bfloat16; views with any strides of whole 16-byte pieces and a
@@ -620,9 +630,10 @@ class KvCache:
 
     def __init__(self, k, v, page_table, seq_len, page_refs):
         import torch
-        if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+        stride = _strides(k)
+        if k.dim() != 5 or k.shape != v.shape or stride != _strides(v) or k.dtype != v.dtype:
             raise TypeError("k and v must be 5-D tensors of one shape, layout and dtype")
-        if not k.is_cuda or not v.is_cuda or k.stride(4) != 1:
+        if not k.is_cuda or not v.is_cuda or stride[4] != 1:
             raise TypeError("k and v must be device tensors with unit inner stride")
         if k.dtype not in (torch.float32, torch.bfloat16):
             raise TypeError(f"unsupported cache dtype {k.dtype}")
@@ -633,7 +644,7 @@ class KvCache:
         i32 = torch.int32
         self.c = _KvCache(k.data_ptr(), v.data_ptr(), _ptr(page_table, i32), _ptr(seq_len, i32), _ptr(page_refs, i32),
                           DIP_F32 if k.dtype == torch.float32 else DIP_BF16, n_layers, n_pages, page, n_heads, dim,
-                          page_table.shape[0], page_table.shape[1], k.stride(0), k.stride(1), k.stride(2), k.stride(3))
+                          page_table.shape[0], page_table.shape[1], *stride[:4])
         self.ref = C.byref(self.c)
 
 
@@ -655,10 +666,10 @@ def _rows(t, dtype, n_rows: int, what: str):
     """(pointer, row stride in elements) of row-indexed data; everything behind the row index is contiguous."""
     if not t.is_cuda or t.dtype != dtype:
         raise TypeError(f"{what} must be a device tensor of {dtype}")
-    shape, stride = t.shape, t.stride()
+    shape, stride = t.shape, _strides(t) if 1 in t.shape else t.stride()
     if shape[0] < n_rows:
         raise TypeError(f"{what} has {shape[0]} rows of {n_rows}")
-    if stride[-1] != 1 or (len(shape) == 3 and shape[1] > 1 and stride[1] != shape[2]):
+    if stride[-1] != 1 or (len(shape) == 3 and stride[1] != shape[2]):
         raise TypeError(f"a row of {what} must be contiguous")
     return t.data_ptr(), stride[0]
 
@@ -701,16 +712,17 @@ def dip_kv_reserve(cache: KvCache, batch: Batch, granted, ws, stream=None) -> No
 def dip_kv_append(cache: KvCache, layer: int, batch: Batch, k_new, v_new, stream=None) -> None:
     """k_new, v_new: [n_rows][n_kv_heads][head_dim] for one layer, or [n_layers][n_rows][n_kv_heads][head_dim]
     for layers layer .. layer + n_layers - 1; rows may be strided (a slice of a fused projection)."""
-    if k_new.dim() not in (3, 4) or k_new.shape != v_new.shape or k_new.stride() != v_new.stride():
+    stride = _strides(k_new)
+    if k_new.dim() not in (3, 4) or k_new.shape != v_new.shape or stride != _strides(v_new):
         raise TypeError("k_new and v_new must have one shape and layout, rows x heads x dims")
     if tuple(k_new.shape[-2:]) != (cache.k.shape[2], cache.k.shape[4]):
         raise TypeError("k_new rows must be [n_kv_heads][head_dim]")
     many = k_new.dim() == 4
     k0, v0 = (k_new[0], v_new[0]) if many else (k_new, v_new)
-    kp, stride = _rows(k0, cache.k.dtype, batch.n_rows, "k_new")
+    kp, row_stride = _rows(k0, cache.k.dtype, batch.n_rows, "k_new")
     vp, _ = _rows(v0, cache.k.dtype, batch.n_rows, "v_new")
-    _check(lib.dip_kv_append(cache.ref, layer, k_new.shape[0] if many else 1, batch.ref, kp, vp, stride,
-                             k_new.stride(0) if many else 0, _stream(stream)))
+    _check(lib.dip_kv_append(cache.ref, layer, k_new.shape[0] if many else 1, batch.ref, kp, vp, row_stride,
+                             stride[0] if many else 0, _stream(stream)))
 
 
 def dip_kv_compact(cache: KvCache, batch: Batch, path, keep, stream=None) -> None:
