@@ -443,7 +443,7 @@ typedef struct dip_kv_cache {
     int32_t n_layers;
     int32_t n_pages;
     int32_t page_size;    /* slots of a page, a power of two in [1, 4096]                    */
-    int32_t n_kv_heads;
+    int32_t n_kv_heads;   /* page_size * n_kv_heads * head_dim < 2^30                        */
     int32_t head_dim;     /* a multiple of 16 bytes; the attention calls: 64, 96 or 128      */
     int32_t n_seqs;
     int32_t max_pages;    /* of one sequence; max_pages * page_size <= 2^31 - 2^25           */

@@ -543,7 +543,8 @@ int32_t check_attention(const dip_kv_cache* c, const dip_batch* b, int32_t n_q_h
     const int64_t rows = (int64_t)rows_bound(b) * (n_q_heads / c->n_kv_heads);
     if (rows >= 1 << 30) return fail(DIP_ERR_UNSUPPORTED, "attention: too many rows of one entry");
     const Plan pl = plan_attention(c, b, n_q_heads, window, sinks);
-    if (pl.blocks * 32 >= (int64_t)1 << 31) return fail(DIP_ERR_UNSUPPORTED, "attention: too many rows for one call");
+    if ((pl.grid + 8) * pl.waves * 64 >= (int64_t)1 << 32)    // threads of a launch
+        return fail(DIP_ERR_UNSUPPORTED, "attention: too many rows for one call");
     return DIP_OK;
 }
 

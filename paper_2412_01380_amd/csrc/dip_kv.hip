@@ -498,7 +498,7 @@ size_t reserve_bytes(const dip_kv_cache* c, const dip_batch* b) {
     return align_up(sizeof(CopyItem) * DIP_MAX_BATCH, 256) + align_up(sizeof(int32_t) * c->n_pages, 256) +
            align_up(reserve_items(c, b) / 8 + 8, 256);
 }
-constexpr int kMaxList = 65535 * 1024;   // sequences or pages of one call
+constexpr int kMaxList = (1 << 24) - 1;  // sequences or pages of one call: a launch has fewer than 2^32 threads
 
 int32_t check_list(const void* a, const void* b, int32_t n) {
     if (!a || !b) return fail(DIP_ERR_INVALID_ARG, "null list");
@@ -586,6 +586,7 @@ int32_t dip_kv_append(const dip_kv_cache* cache, int32_t layer, int32_t n_layers
                       const void* v_new, int64_t row_stride, int64_t new_layer_stride, void* stream) {
     int32_t st = validate_kv(cache);
     if (!st) st = validate_batch(batch, true);
+    if (!st) st = check_page_bytes(cache);
     if (st) return st;
     if (layer < 0 || n_layers < 1 || n_layers > cache->n_layers || layer > cache->n_layers - n_layers)
         return fail(DIP_ERR_INVALID_ARG, "layers %d .. %d outside the cache's %d", layer, layer + n_layers - 1, cache->n_layers);
@@ -603,9 +604,9 @@ int32_t dip_kv_append(const dip_kv_cache* cache, int32_t layer, int32_t n_layers
     p.row_stride = row_stride / per;
     p.new_layer_stride = new_layer_stride / per;
     p.layer = layer;
-    // rows of a workgroup: 16 where that leaves enough workgroups for the chip, else fewer
+    // rows of a workgroup: 16 where that leaves enough workgroups for the chip, else fewer (and their pieces fit 32 bits)
     int rows = 16;
-    while (rows > 1 && (int64_t)batch->n_rows * n_layers / rows < 1024) rows >>= 1;
+    while (rows > 1 && ((int64_t)batch->n_rows * n_layers / rows < 1024 || (int64_t)rows * p.c.n_heads * p.c.pieces > 1 << 28)) rows >>= 1;
     p.rows_per_wg = rows;
     const unsigned blocks = (unsigned)((p.b.max_rows + rows - 1) / rows);
     if (blocks > 65535) return fail(DIP_ERR_UNSUPPORTED, "max_rows is too large for one call");
@@ -616,6 +617,7 @@ int32_t dip_kv_append(const dip_kv_cache* cache, int32_t layer, int32_t n_layers
 int32_t dip_kv_compact(const dip_kv_cache* cache, const dip_batch* batch, const int32_t* path, const int32_t* keep, void* stream) {
     int32_t st = validate_kv(cache);
     if (!st) st = validate_batch(batch, true);
+    if (!st) st = check_page_bytes(cache);
     if (st) return st;
     CompactParams p = {view_of(cache), view_of(batch), path, keep, 1};
     if (path) {
