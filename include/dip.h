@@ -478,8 +478,8 @@ int32_t dip_kv_init(const dip_kv_cache* cache, void* stream);
 int32_t dip_kv_free(const dip_kv_cache* cache, const int32_t* seqs, int32_t n, void* stream);
 
 /* Sequence dst[i] becomes a copy of sequence src[i] that shares its pages (up to seq_len tokens),
- * i < n (device arrays).  The destinations are empty and distinct, and none is a source; several may
- * have one source. */
+ * i < n (device arrays).  The destinations hold no pages (as after dip_kv_init or dip_kv_free) and are
+ * distinct, and none is a source; several may have one source. */
 int32_t dip_kv_fork(const dip_kv_cache* cache, const int32_t* src, const int32_t* dst, int32_t n, void* stream);
 
 /* Copy whole pages, all layers, k and v: page src[i] to page dst[i], i < n (device arrays; the
@@ -534,7 +534,8 @@ int32_t dip_kv_compact(const dip_kv_cache* cache, const dip_batch* batch, const 
  * dip_tree_attention: parents[r] is the entry's node that drafted node t (-1: none, any other value
  * outside [0, t): the node is absent, as are the nodes below an absent one); node t stands at pos =
  * seq_len + its depth, sees the ancestors that are nodes of the tree and itself, and of the committed
- * positions j < seq_len those with  j > pos - window  or  j < sinks.
+ * positions j < seq_len those with  j > pos - window  or  j < sinks.  A window shorter than the tree does not cut its
+ * ancestors: a node that deep sees more than the same token would one at a time.
  * window 0 means no bound (sinks then change nothing).  A row that sees nothing, an absent node, and a row
  * whose scores are all -inf get zeros.  Positions that a row does not see do not matter to it, whatever they hold.
  * A value that is not finite at a position that a row sees makes that channel of the row what the sum gives
@@ -545,7 +546,8 @@ int32_t dip_kv_compact(const dip_kv_cache* cache, const dip_batch* batch, const 
  *   scale > 0      n_q_heads a multiple of n_kv_heads      ws  *_workspace_bytes() bytes, 256-aligned
  * Scores, softmax statistics and sums are fp32; with a DIP_BF16 cache the weights p enter their product
  * with v as the sum of two bf16 terms (exact to 2^-15), and the output is rounded once.  Which kernel runs is chosen
- * by max_rows and the query heads per key/value head, for all entries of a call.  The order of the sums is fixed
+ * by max_rows and the query heads per key/value head, for all entries of a call: many single tokens are faster in a
+ * call without a prompt's rows among them.  The order of the sums is fixed
  * by shapes, all entries' rows and lengths, and max_len (bit-repeatable).
  */
 size_t dip_attention_workspace_bytes(const dip_kv_cache* cache, const dip_batch* batch, int32_t n_q_heads,

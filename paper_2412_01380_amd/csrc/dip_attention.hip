@@ -5,7 +5,7 @@
 //   up to 64 rows          attn_rows_kernel: blocks of 16, 32 or 64; wavefronts stream keys of their own
 //   more                   attn_block_kernel: blocks of 64 (fp32), 128 or 256 whose wavefronts share the tiles
 // Keys are read once for all query heads of a group and all rows of a block.  With few rows what bounds the
-// call is reading them: 32 tokens of 40 heads on 10, a window of 2047, 75 us for the 332 MB of K and V (52 us
+// call is reading them: 32 tokens of 40 heads on 10, a window of 2047, 73 us for the 332 MB of K and V (52 us
 // at the rate of a plain read).  With many it is the matrix cores and, beside them, the softmax's plain
 // instructions: a maximum, two multiply-adds, an exponential, a sum, a mask and two halves of a move and a conversion
 // for every weight, whose products, P V with two terms, are 384 multiply-adds at 128 dims.
@@ -27,7 +27,7 @@ constexpr int kIds = 256;                 // page numbers of a wavefront in LDS 
 // LDS although no wavefront reads another's tile: a load to LDS holds no registers while it is on its way, and
 // the products want rows of K and columns of V, which memory has neither of side by side.  Two tiles of 32 keys
 // (16 in fp32) each: a third one costs a workgroup per compute unit.
-// Measured (bf16, 128 dims): 2 x 700 keys 10.4 us, of which 4.4 any launch takes; 8 trees of 8 nodes, 4 heads on
+// Measured (bf16, 128 dims): 2 x 700 keys 10.3 us, of which 4.4 any launch takes; 8 trees of 8 nodes, 4 heads on
 // one, up to 8192 keys 46 us at 3.7 TB/s.  fp32, 3 trees of 7 nodes, 32 heads, 96 dims: 19 us.
 template <typename E, int D, int NB, int WAVES, bool ONCE>
 __global__ void __launch_bounds__(WAVES * 64, 1) attn_rows_kernel(const AttnParams p) {
@@ -197,9 +197,9 @@ __global__ void __launch_bounds__(WAVES * 64, 1) attn_rows_kernel(const AttnPara
 // beside the products of its neighbours: P V lags one tile behind K Q, so both are at hand when a wavefront
 // waits for exponentials.  What is left is that products and plain instructions of the two wavefronts of a SIMD
 // overlap only by half (with one term: alone 485 and 515 us of a probe, together 880).
-// Measured (bf16, 128 dims, 4 heads on one): 2 prompts of up to 4096 rows, window 2047: 484 us (610 TFLOP/s, 920 with the
-// weights' second terms, of the 1152 of a large library product); 4 trees of 64 nodes over up to 49152 keys 231 us.
-// With attn_rows_kernel: 1160 and 890 us.
+// Measured (bf16, 128 dims, 4 heads on one): 2 prompts of up to 4096 rows, window 2047: 470 us (630 TFLOP/s, 950 with the
+// weights' second terms, of the 1152 of a large library product); 4 trees of 64 nodes over up to 49152 keys 226 us.
+// With attn_rows_kernel: 868 and 472 us.
 // bf16: 64 keys to a tile, eight wavefronts, one workgroup to a compute unit.
 template <typename E>
 struct Block {
@@ -208,8 +208,8 @@ struct Block {
 };
 // fp32: 16 keys, and small workgroups, several to a compute unit (its products take sixteen times as long: what
 // counts is that some wavefront of a SIMD always has one).  Against attn_rows_kernel over the same rows: 2 x 100
-// rows, 64 dims, 3000 keys 61 -> 37 us; 2048 rows x 4 heads, 128 dims 555 -> 420 us; 32 trees of 96 rows, 64 dims,
-// 2000 keys 124 -> 89 us; at 96 dims within 4 % either way (214 and 221 us at 4 x 600 rows, 1600 keys).
+// rows of 8 heads, 64 dims, 3000 keys 60 -> 37 us; 2048 rows, 4 heads on one, 128 dims 555 -> 412 us; 32 trees of 24
+// nodes, 4 heads on one, 64 dims, 2000 keys 124 -> 84 us; 4 x 600 rows, 96 dims, 1000 keys before them 214 -> 210 us.
 template <>
 struct Block<float> {
     static constexpr int WAVES = 4, SUB = 1;
@@ -409,10 +409,10 @@ __global__ void __launch_bounds__(Block<E>::WAVES * 64, Block<E>::per_simd(D)) a
     }
 }
 
-// The shares of attn_block_kernel's rows, spread over the chip: with the last workgroup of a block to join its 256
-// rows of 20 shares by itself, wide trees took 465 us instead of 390.  At least kJoinRows rows to a workgroup,
-// and no more than about kJoinGrid workgroups: each works out for itself what the blocks were cut into, 13.8 us for
-// 9984 workgroups that then find nothing cut.
+// The shares of attn_block_kernel's rows, spread over the chip: 9 us of 226 for wide trees, whose blocks have 256 rows of
+// 20 shares; a workgroup that joins all of a block by itself takes 75 us longer.  At least kJoinRows rows to a
+// workgroup, and no more than about kJoinGrid workgroups: each works out for itself what the blocks were cut into.
+// 3 x 777 rows in fp32, of which nothing is cut: 111 us; with 9984 workgroups that find so 123; without the launch 107.
 constexpr int kJoinRows = 8;
 constexpr int kJoinGrid = 1024;
 template <typename E, int D, int NB>
@@ -448,7 +448,7 @@ int reach(const dip_kv_cache* c, const dip_batch* b) {
 // Non-temporal loads of keys and values from here on (bytes of a call), where one block of rows is all that reads
 // them.  At 170 MB and more of bf16: 49.3 -> 45.9 us (8 trees of 8 nodes), 78.4 -> 74.8 (32 tokens), 224 -> 210
 // (32 tokens over 12000 keys).  Less may still be in the last-level cache (256 MB) when it is read again, and what
-// several blocks read should stay there: 39 MB 19.4 -> 20.1 us, 4 MB 10.6 -> 11.0, prompts 390 -> 398.  (Of two
+// several blocks read should stay there: 39 MB 19.4 -> 20.1 us, 4 MB 10.6 -> 11.0.  (Of two
 // kernels: asking for each load costs more than it gains, 2 to 4 %.  fp32 blocks wait for their products: 184 us and 184.)
 constexpr double kOnceBytes = 64 << 20;
 Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads, int window, int sinks) {
@@ -464,12 +464,14 @@ Plan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads, in
     pl.blocks = (int64_t)b->n_batch * c->n_kv_heads * pl.row_blocks;
     // Four wavefronts to a workgroup, as many workgroups to a compute unit as their rings of tiles leave room for;
     // where the blocks alone are more than that, two: the start and the end of one workgroup, when it streams
-    // nothing, then lie beside another's middle.
+    // nothing, then lie beside another's middle (32 tokens over up to 12000 keys 201 us, with four 262; 8 trees of 8
+    // nodes 44 us with four, 54 with two).
     const auto fit = [&](int waves) { return 256 * ((160 * 1024 - 1024) / (waves * 256 * c->head_dim + 6144)); };
     pl.waves = pl.shared ? block_waves : pl.blocks <= fit(4) ? 4 : 2;
     pl.slots = !pl.shared ? fit(pl.waves) : bf16 ? 256 : 256 * (160 * 1024 / (512 * c->head_dim + 5120));
-    // attn_block_kernel's shares are joined by a launch of its own, which costs 10 us even where there turn out to
-    // be none: with far more blocks than the chip holds at a time none are made
+    // attn_block_kernel's shares are joined by a launch of its own, which costs 4 us even where there turn out to be
+    // none: with far more blocks than the chip holds at a time none are made (2 x 4096 rows 467 us, else 471; but uncut, 4
+    // trees of 64 nodes take 1685 us, 2 x 100 rows 175 instead of 37)
     pl.cut = !pl.shared || pl.blocks < 4 * pl.slots;
     if (!pl.cut) pl.slots = 0;
     int64_t keys = reach(c, b);

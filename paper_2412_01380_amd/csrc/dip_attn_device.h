@@ -467,8 +467,8 @@ struct Core<uint16_t, D, NB> {
     }
     // The weights of KEYS keys as the second product takes them: two bf16 terms, the upper half of the fp32 number and
     // what that leaves, rounded: 2^-15 of a weight.  With one term, off by up to 2^-8 where a few keys carry a row, a
-    // call's relative error is 0.0023, with two 0.0017, which the rounding of its output alone is (prompts 396 us instead
-    // of 484, trees of 64 nodes 186 instead of 231).  What is left of a weight above zero counts as at least 2^-23 of it, so
+    // call's relative error is 0.0023, with two 0.0017, which the rounding of its output alone is (prompts 389 us instead
+    // of 479, trees of 64 nodes 180 instead of 227).  What is left of a weight above zero counts as at least 2^-23 of it, so
     // that an infinite value times either term has its sign and never meets a zero.
     struct Weights {
         bf16x8 w[NB], rest[NB];
@@ -649,7 +649,8 @@ struct Core<float, D, NB> {
 
 // The running softmax of a wavefront's columns: m the maximum of c S so far, l this lane's share of the sum.
 // m may lag behind the maximum by up to kSlack: weights up to 2^kSlack instead of 1 -- fp32 numbers, and two terms that
-// keep 15 bits of them, whatever their size -- spare the rescaling that some of 32 rows would ask for with nearly every tile.
+// keep 15 bits of them, whatever their size -- spare the rescaling that some of 32 rows would ask for with nearly every
+// tile (2 x 4096 rows 494 -> 468 us, 4 trees of 64 nodes 237 -> 225, 8 trees of 8 46.9 -> 44.2).
 constexpr float kSlack = 8.f;
 template <typename E, int D, int NB>
 struct Softmax {

@@ -7,9 +7,9 @@
 // what reserve leaves an entry with, or else it grants it nothing (lacks_room).
 //
 // A decode step is reserve (two launches), append, compact (two): all wait for memory.  A few drafts of a few
-// branches are bound by the launches themselves (2 to 7 us each; six branches of 8 rows, 32 layers: 35 us with
-// fork and free, 7 launches); 16 branches of up to 256 rows, 40 layers, 10 heads of 128, by bytes: append 229 us,
-// move 119, copy on write 49 of 414 us, against 383 us for the bytes at the rate of a plain copy (4.83 TB/s).
+// branches are bound by the launches themselves (2 to 8 us each; six branches of 8 rows, 32 layers: 35 us with
+// fork and free, 7 launches); 16 branches of up to 256 rows, 40 layers, 10 heads of 128, by bytes: append 225 us,
+// move 125, copy on write 48 of 421 us, against 383 us for the bytes at the rate of a plain copy (4.83 TB/s).
 
 #include "dip_decode_internal.h"
 
@@ -138,7 +138,8 @@ __global__ void __launch_bounds__(kThreads) kv_fork_kernel(const SeqsParams p) {
 // One workgroup: the lowest free pages go to the wanted table entries in order, which is a prefix
 // sum over both.  Bound by latency (a handful of round trips to memory: 7 us), not by its bytes.  One, because
 // several would have to agree on the order through memory; 1024 threads look at 4096 counts at a time and stop
-// once there are as many free pages as are wanted.
+// once there are as many free pages as are wanted (about 75 us where the last of 200000 pages are the only
+// free ones).
 // An "item" is a table entry that some row of the step falls into, entries in order.
 constexpr int kReserveThreads = 1024;
 struct CopyItem {
@@ -363,7 +364,7 @@ __device__ __forceinline__ bool lacks_room(const KvView& c, const int32_t* table
 }
 
 // ---- append -------------------------------------------------------------------------------
-// A thread moves 16 bytes of k and the same of v.  Bound by bytes (1.1 GB read and written in 229 us at 16
+// A thread moves 16 bytes of k and the same of v.  Bound by bytes (1.1 GB read and written in 225 us at 16
 // entries of up to 256 rows, 40 layers), small ones by latency: hence fewer rows to a workgroup then.
 struct AppendParams {
     KvView c;
@@ -413,7 +414,8 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams 
 // ---- compact ------------------------------------------------------------------------------
 // Row path[j] moves to row j <= path[j].  A workgroup takes some heads' rows of a layer, all of k or of v, and
 // reads a batch of rows into registers before it writes any: what is written over is behind, or was read.
-// Row by row, each move waiting for the one before it, 16 entries of up to 256 rows took 214 us; in batches 110.
+// Row by row, each move waiting for the one before it, 16 entries of up to 256 rows took 214 us; in batches 110, and 125
+// with the look at the pages' counts.
 // (Batches go in ascending order: a later one reads rows that no earlier one wrote, since path[j] >= j.)
 struct CompactParams {
     KvView c;
