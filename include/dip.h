@@ -515,6 +515,68 @@ int32_t dip_kv_append(const dip_kv_cache* cache, int32_t layer, int32_t n_layers
                       const void* k_new, const void* v_new, int64_t row_stride, int64_t new_layer_stride,
                       void* stream);
 
+/* ---- rows turned to their positions ---- */
+
+/* How a head is turned to position pos.  Pair i < dims / 2, (a, b), becomes
+ *     scale * (a cos t - b sin t,  a sin t + b cos t),   t = pos * freq[i];
+ * what lies behind the first `dims` dims passes through.  Angles are worked out in 64 bits and reduced to a
+ * part of a turn before their sine and cosine are taken in fp32, so that far positions are as exact as near
+ * ones; products and sums are fp32, rounded once. */
+#define DIP_ROTARY_HALF 0        /* pair i: dims i and i + dims / 2                             */
+#define DIP_ROTARY_INTERLEAVED 1 /* pair i: dims 2 i and 2 i + 1                                */
+typedef struct dip_rotary {
+    const double* freq; /* device; dims / 2 angles per position, radians                    */
+    int32_t dims;       /* even, 2 .. the head's dims, at most DIP_MAX_ROTARY_DIMS          */
+    int32_t layout;     /* DIP_ROTARY_HALF or DIP_ROTARY_INTERLEAVED                        */
+    float scale;        /* of sines and cosines; 1 but for methods that ask for more        */
+    int32_t reserved;   /* must be 0                                                        */
+} dip_rotary;
+#define DIP_MAX_ROTARY_DIMS 4096
+
+/* Angles per position, f_i = base^(-2 i / dims), and as they are scaled for contexts longer than a model
+ * was trained on. */
+#define DIP_SCALING_NONE 0
+#define DIP_SCALING_LINEAR 1 /* f_i / factor (position interpolation)                            */
+#define DIP_SCALING_BASE 2   /* base * factor^(dims / (dims - 2)) in place of base               */
+#define DIP_SCALING_PARTS 3  /* f_i (m + (1 - m) / factor), m = (turns - slow) / (fast - slow) within [0, 1],
+                                turns = original_len f_i / 2 pi: quick pairs stay, slow ones are stretched */
+#define DIP_SCALING_LIST 4   /* f_i / factors[i]                                                 */
+typedef struct dip_rotary_scaling {
+    int32_t kind;
+    int32_t reserved;       /* must be 0                                                    */
+    double factor;          /* > 0: LINEAR, BASE, PARTS                                     */
+    double slow, fast;      /* 0 <= slow < fast: PARTS                                      */
+    double original_len;    /* > 0: PARTS                                                   */
+    const double* factors;  /* host; dims / 2 entries > 0: LIST                             */
+} dip_rotary_scaling;
+
+/* freq: host, dims / 2 entries.  scaling: host, NULL for none.  Host only; nothing is enqueued. */
+int32_t dip_rotary_frequencies(int32_t dims, double base, const dip_rotary_scaling* scaling /* host */,
+                               double* freq /* host */);
+
+/*
+ * Rows turned to given positions: row r of out = row r of x at positions[r] (device; any int32, negative ones turn
+ * back).  n_rows rows of n_heads * head_dim elements (DIP_F32 or DIP_BF16; a head a multiple of 16 bytes), x_stride /
+ * out_stride elements apart (multiples of 16 bytes).  out may be x itself (equal pointers and strides), but may not overlap it in another way.
+ */
+int32_t dip_rotate_rows(const dip_rotary* rot, const void* x, int64_t x_stride, const int32_t* positions, int32_t n_rows,
+                        int32_t n_heads, int32_t head_dim, int32_t dtype, void* out, int64_t out_stride, void* stream);
+
+/*
+ * dip_kv_append for one layer, with the step's queries and keys turned on the way: keys go into the cache
+ * turned, values as they are, queries to q_out.  Row t of an entry is turned to position seq_len + t; with
+ * parents (as in dip_tree_attention; NULL: none) to seq_len + its depth, an absent node to seq_len.
+ * Which entries are passed over follows dip_kv_append; the queries of an entry that is passed over are turned all
+ * the same, those of an entry whose sequence number is out of range are not written.
+ *   q, q_out   n_rows rows of n_q_heads * head_dim elements of the cache's type, strides in elements
+ *              (multiples of 16 bytes); q_out may be q itself, and overlaps neither it in another way nor k_new
+ *              or v_new.  q and q_out NULL, n_q_heads 0: keys and values alone
+ *   k_new, v_new   as in dip_kv_append: n_kv_heads * head_dim elements at r * row_stride
+ */
+int32_t dip_kv_append_rotary(const dip_kv_cache* cache, int32_t layer, const dip_batch* batch, const int32_t* parents,
+                             const dip_rotary* rot, const void* q, int64_t q_stride, int32_t n_q_heads, void* q_out,
+                             int64_t q_out_stride, const void* k_new, const void* v_new, int64_t row_stride, void* stream);
+
 /*
  * Keep keep[b] rows of every entry (device; values are clamped to its rows; NULL: all of them) and
  * commit: row path[row_start[b] + j] of the entry moves to row j, j < keep[b], in every layer (path:

@@ -53,7 +53,10 @@ int32_t dip_gemv_launch_shape(const dip_weight* w, int32_t k, int32_t bundled, i
 #define DIP_KERNEL_ATTENTION 9    /* dip_window_attention, dip_tree_attention                   */
 #define DIP_KERNEL_VERIFY 10      /* the launches of dip_verify_tree                            */
 #define DIP_KERNEL_KV 11          /* page operations of a key/value cache                       */
-#define DIP_KERNEL_KINDS 12
+#define DIP_KERNEL_ROTARY 12      /* dip_rotate_rows, dip_kv_append_rotary                      */
+#define DIP_KERNEL_BLOCKS 13      /* bounds, choice of blocks and the attention over them       */
+#define DIP_KERNEL_SAMPLE 14      /* the launches of dip_sample                                 */
+#define DIP_KERNEL_KINDS 15
 int32_t dip_profile_enable(int32_t max_launches);
 int32_t dip_profile_read(int32_t kind, double* total_ms /* host */, int32_t* launches /* host */);
 int32_t dip_profile_disable(void);

@@ -193,3 +193,20 @@ class Pool:
                 if self.table[s][j] >= 0:
                     self.refs[self.table[s][j]] -= 1
                 self.table[s][j] = -1
+
+
+# ---- rows turned to their positions ------------------------------------------------------------------------
+def turn(x: np.ndarray, positions, freq, interleaved: bool, scale: float = 1.0) -> np.ndarray:
+    """x [rows][heads][dims] (float64): each pair a complex number, times scale * exp(i position freq)."""
+    out, half = x.copy(), len(freq)
+    first = 2 * np.arange(half) if interleaved else np.arange(half)
+    second = first + (1 if interleaved else half)
+    by = scale * np.exp(1j * np.asarray(positions, dtype=np.float64)[:, None] * np.asarray(freq)[None])
+    z = (x[..., first] + 1j * x[..., second]) * by[:, None]
+    out[..., first], out[..., second] = z.real, z.imag
+    return out
+
+
+def tree_positions(n_before: int, parents) -> List[int]:
+    """Position of each node: as far behind the sequence as it is deep; an absent node's is the root's."""
+    return [n_before + (len(a) - 1 if a else 0) for a in ancestors(parents)]

@@ -103,26 +103,6 @@ __device__ __forceinline__ uint64_t sees(const RowSees& r, int j0, int sinks, in
     return bits;
 }
 
-// The ancestors of every node of an entry's tree, itself among them (0: the node is absent), into LDS by
-// one wavefront: pointers jump 1, 2, 4 .. steps up.
-__device__ __forceinline__ void tree_masks(const int32_t* parents, int rows, uint64_t* out) {
-    const int lane = threadIdx.x & 63;
-    int up = lane < rows ? parents[lane] : -2;
-    if (up < -1 || up >= lane) up = -2;
-    uint64_t mask = 1ull << lane;
-#pragma unroll
-    for (int i = 0; i < 6; ++i) {
-        const int at = up < 0 ? lane : up;
-        const uint32_t lo = __shfl((uint32_t)mask, at), hi = __shfl((uint32_t)(mask >> 32), at);
-        const int next = __shfl(up, at);
-        if (up >= 0) {
-            mask |= ((uint64_t)hi << 32) | lo;
-            up = next;
-        }
-    }
-    out[lane] = up == -1 ? mask : 0;
-}
-
 // (Nothing from max_len on: a tile that it cuts holds other positions' keys there.)
 __device__ __forceinline__ RowSees row_sees(const AttnParams& p, int len, int t, const uint64_t* masks) {
     RowSees r;

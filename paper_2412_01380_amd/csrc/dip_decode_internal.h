@@ -58,6 +58,42 @@ __device__ __forceinline__ int entry_len(const KvView& c, int seq) {
     return min(max(c.seq_len[seq], 0), c.max_pages << c.page_shift);
 }
 
+__device__ __forceinline__ bool is_page(const KvView& c, int p) { return (unsigned)p < (unsigned)c.n_pages; }
+// Whether some row of an entry (of one or more) falls into no page or into one that another sequence holds: this
+// thread's part of the pages, true for any thread of a workgroup says that the entry has no room.
+// This may be asked while other entries give pages up: a page that two tables name came to be so by a fork, so that it
+// lies within the committed length of both, and only pages beyond that are given up meanwhile.
+template <int THREADS>
+__device__ __forceinline__ bool lacks_room(const KvView& c, const int32_t* table, int len, int rows) {
+    const int last = (len + rows - 1) >> c.page_shift;
+    bool lacks = last >= c.max_pages;
+    for (int j = (len >> c.page_shift) + threadIdx.x; j <= min(last, c.max_pages - 1); j += THREADS) {
+        const int page = table[j];
+        lacks |= !is_page(c, page) || c.refs[page] > 1;
+    }
+    return lacks;
+}
+
+// The ancestors of every node of an entry's tree, itself among them (0: the node is absent), into LDS by
+// one wavefront: pointers jump 1, 2, 4 .. steps up.
+__device__ __forceinline__ void tree_masks(const int32_t* parents, int rows, uint64_t* out) {
+    const int lane = threadIdx.x & 63;
+    int up = lane < rows ? parents[lane] : -2;
+    if (up < -1 || up >= lane) up = -2;
+    uint64_t mask = 1ull << lane;
+#pragma unroll
+    for (int i = 0; i < 6; ++i) {
+        const int at = up < 0 ? lane : up;
+        const uint32_t lo = __shfl((uint32_t)mask, at), hi = __shfl((uint32_t)(mask >> 32), at);
+        const int next = __shfl(up, at);
+        if (up >= 0) {
+            mask |= ((uint64_t)hi << 32) | lo;
+            up = next;
+        }
+    }
+    out[lane] = up == -1 ? mask : 0;
+}
+
 // ---- the last workgroup of several -------------------------------------------------------------
 // A ticket word is the tag of a launch (upper 48 bits) and the tickets drawn in it; a word with another tag
 // counts as none, so nothing has to clear it.  Whoever draws the last ticket of a word goes on with what the

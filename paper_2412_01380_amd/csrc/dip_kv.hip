@@ -87,8 +87,6 @@ namespace {
 constexpr int kThreads = 256;
 typedef unsigned int piece_t __attribute__((ext_vector_type(4)));   // 16 bytes
 
-__device__ __forceinline__ bool is_page(const KvView& c, int p) { return (unsigned)p < (unsigned)c.n_pages; }
-
 // ---- init, free, fork ---------------------------------------------------------------------
 struct InitParams {
     KvView c;
@@ -349,20 +347,6 @@ __global__ void __launch_bounds__(kThreads) kv_copy_kernel(const CopyParams p) {
     }
 }
 
-// Whether some row of an entry (of one or more) falls into no page or into one that another sequence holds: this
-// thread's part of the pages, true for any thread of a workgroup says that the entry has no room.
-// This may be asked while other entries give pages up: a page that two tables name came to be so by a fork, so that it
-// lies within the committed length of both, and only pages beyond that are given up meanwhile.
-__device__ __forceinline__ bool lacks_room(const KvView& c, const int32_t* table, int len, int rows) {
-    const int last = (len + rows - 1) >> c.page_shift;
-    bool lacks = last >= c.max_pages;
-    for (int j = (len >> c.page_shift) + threadIdx.x; j <= min(last, c.max_pages - 1); j += kThreads) {
-        const int page = table[j];
-        lacks |= !is_page(c, page) || c.refs[page] > 1;
-    }
-    return lacks;
-}
-
 // ---- append -------------------------------------------------------------------------------
 // A thread moves 16 bytes of k and the same of v.  Bound by bytes (1.1 GB read and written in 225 us at 16
 // entries of up to 256 rows, 40 layers), small ones by latency: hence fewer rows to a workgroup then.
@@ -399,7 +383,7 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendParams 
         b = __builtin_nontemporal_load((const piece_t*)p.v_new + src);
     };
     if ((int)threadIdx.x < n) load(threadIdx.x);
-    if (__syncthreads_or(lacks_room(p.c, table, len, er.rows))) return;
+    if (__syncthreads_or(lacks_room<kThreads>(p.c, table, len, er.rows))) return;
     for (int i = threadIdx.x; i < n; i += kThreads) {
         const int r = i / per_row, c = i - r * per_row;
         const int pos = len + t0 + r, page = table[pos >> p.c.page_shift];
@@ -438,7 +422,7 @@ __global__ void __launch_bounds__(kThreads) kv_move_kernel(const CompactParams p
     piece_t* base = (piece_t*)(blockIdx.z / groups ? p.c.v : p.c.k) + (int64_t)blockIdx.y * p.c.layer_stride + h0 * p.c.head_stride;
     const int len = entry_len(p.c, seq);
     const int32_t* table = p.c.table + (size_t)seq * p.c.max_pages;
-    const bool lacks = lacks_room(p.c, table, len, er.rows);
+    const bool lacks = lacks_room<kThreads>(p.c, table, len, er.rows);
     const int32_t* path = p.path + er.first;
     const int slot_mask = (1 << p.c.page_shift) - 1;
     auto place = [&](int row) {                       // (of an entry that has room)
@@ -486,7 +470,7 @@ __global__ void __launch_bounds__(kThreads) kv_commit_kernel(const CompactParams
     if (seq < 0) return;
     const int before = entry_len(p.c, seq), page = 1 << p.c.page_shift;
     int32_t* row = p.c.table + (size_t)seq * p.c.max_pages;
-    const int len = kept && !__syncthreads_or(lacks_room(p.c, row, before, er.rows)) ? before + kept : before;
+    const int len = kept && !__syncthreads_or(lacks_room<kThreads>(p.c, row, before, er.rows)) ? before + kept : before;
     const int held = (len + page - 1) >> p.c.page_shift;
     for (int j = held + threadIdx.x; j < p.c.max_pages; j += kThreads) give_up(p.c, row + j);
     if (threadIdx.x == 0) p.c.seq_len[seq] = len;

@@ -18,6 +18,8 @@ DIP_OK, DIP_ERR_INVALID_ARG, DIP_ERR_UNSUPPORTED, DIP_ERR_WORKSPACE, DIP_ERR_HIP
 DIP_F32, DIP_BF16, DIP_INT4_G128 = 0, 1, 2
 DIP_LRU, DIP_LFU = 0, 1
 DIP_GATE_PRUNING, DIP_UP_PRUNING = 1, 2
+DIP_ROTARY_HALF, DIP_ROTARY_INTERLEAVED, DIP_MAX_ROTARY_DIMS = 0, 1, 4096
+DIP_SCALING_NONE, DIP_SCALING_LINEAR, DIP_SCALING_BASE, DIP_SCALING_PARTS, DIP_SCALING_LIST = range(5)
 DIP_MAX_N = 32768
 DIP_CACHE_META_WORDS = 8
 META = {"step": 0, "resident": 1, "hits": 2, "inserted": 3, "evicted": 4, "bypassed": 5,
@@ -80,6 +82,15 @@ class _KvCache(C.Structure):
 class _Batch(C.Structure):
     _fields_ = [("seqs", C.c_void_p), ("row_start", C.c_void_p), ("n_batch", C.c_int32), ("n_rows", C.c_int32),
                 ("max_rows", C.c_int32), ("max_len", C.c_int32)]
+
+
+class _Rotary(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("dims", C.c_int32), ("layout", C.c_int32), ("scale", C.c_float), ("reserved", C.c_int32)]
+
+
+class _RotaryScaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("reserved", C.c_int32), ("factor", C.c_double), ("slow", C.c_double), ("fast", C.c_double),
+                ("original_len", C.c_double), ("factors", C.POINTER(C.c_double))]
 
 
 def _load() -> C.CDLL:
@@ -159,10 +170,13 @@ def _load() -> C.CDLL:
     L.dip_tiered_mlp_forward.restype = i32
     L.dip_tiered_mlp_forward.argtypes = [C.POINTER(_TieredMlp), vp, i32, i32, C.POINTER(_Cache),
                                          C.POINTER(_Cache), f32, vp, C.POINTER(_Debug), vp, sz, vp]
-    kv, bt = C.POINTER(_KvCache), C.POINTER(_Batch)
+    kv, bt, ro, f64 = C.POINTER(_KvCache), C.POINTER(_Batch), C.POINTER(_Rotary), C.POINTER(C.c_double)
     for name, args in {
             "dip_kv_init": [kv, vp], "dip_kv_free": [kv, vp, i32, vp], "dip_kv_fork": [kv, vp, vp, i32, vp],
             "dip_kv_copy_pages": [kv, vp, vp, i32, vp], "dip_kv_reserve": [kv, bt, vp, vp, sz, vp],
+            "dip_rotary_frequencies": [i32, C.c_double, C.POINTER(_RotaryScaling), f64],
+            "dip_rotate_rows": [ro, vp, i64, vp, i32, i32, i32, i32, vp, i64, vp],
+            "dip_kv_append_rotary": [kv, i32, bt, vp, ro, vp, i64, i32, vp, i64, vp, vp, i64, vp],
             "dip_kv_append": [kv, i32, i32, bt, vp, vp, i64, i64, vp], "dip_kv_compact": [kv, bt, vp, vp, vp],
             "dip_window_attention": [kv, i32, bt, vp, i64, i32, f32, i32, i32, vp, i64, vp, sz, vp],
             "dip_tree_attention": [kv, i32, bt, vp, vp, i64, i32, f32, i32, i32, vp, i64, vp, sz, vp],
@@ -208,7 +222,7 @@ EXPORTS = ["dip_version", "dip_last_error", "dip_ca_scores", "dip_prune_topk", "
            "dip_partial_pruning_forward_workspace_bytes", "dip_partial_pruning_forward", "dip_tier_init_workspace_bytes",
            "dip_tier_init", "dip_tiered_mlp_forward_workspace_bytes", "dip_tiered_mlp_forward",
            "dip_kv_init", "dip_kv_free", "dip_kv_fork", "dip_kv_copy_pages", "dip_kv_reserve_workspace_bytes", "dip_kv_reserve",
-           "dip_kv_append", "dip_kv_compact", "dip_attention_workspace_bytes", "dip_window_attention", "dip_tree_attention",
+           "dip_rotary_frequencies", "dip_rotate_rows", "dip_kv_append", "dip_kv_append_rotary", "dip_kv_compact", "dip_attention_workspace_bytes", "dip_window_attention", "dip_tree_attention",
            "dip_verify_tree_workspace_bytes", "dip_verify_tree", "dip_tune_gemv", "dip_gemv_launch_shape", "dip_set_fusion", "dip_fused_launch_shape", "dip_stream_read", "dip_profile_enable", "dip_profile_read",
            "dip_profile_disable"]
 
@@ -723,6 +737,77 @@ def dip_kv_append(cache: KvCache, layer: int, batch: Batch, k_new, v_new, stream
     vp, _ = _rows(v0, cache.k.dtype, batch.n_rows, "v_new")
     _check(lib.dip_kv_append(cache.ref, layer, k_new.shape[0] if many else 1, batch.ref, kp, vp, row_stride,
                              stride[0] if many else 0, _stream(stream)))
+
+
+def dip_rotary_frequencies(dims: int, base: float = 10000.0, kind: int = DIP_SCALING_NONE, factor: float = 1.0, slow: float = 1.0,
+                           fast: float = 32.0, original_len: float = 0.0, factors: Optional[Sequence[float]] = None):
+    """Angles per position of each pair: a float64 CPU tensor of dims / 2 entries."""
+    import torch
+    out = torch.empty(max(dims, 0) // 2, dtype=torch.float64)
+    if factors is not None and len(factors) < dims // 2:
+        raise TypeError(f"factors has {len(factors)} entries of {dims // 2}")
+    each = (C.c_double * len(factors))(*factors) if factors is not None else None
+    scaling = _RotaryScaling(kind, 0, factor, slow, fast, original_len, each)
+    _check(lib.dip_rotary_frequencies(dims, base, C.byref(scaling), C.cast(out.data_ptr(), C.POINTER(C.c_double))))
+    return out
+
+
+class Rotary:
+    """How heads are turned: freq, a float64 device tensor of dims / 2 angles per position (dip_rotary_frequencies(..).cuda()),
+    the layout of the pairs, and a scale of sines and cosines."""
+
+    def __init__(self, freq, layout: int = DIP_ROTARY_HALF, scale: float = 1.0):
+        import torch
+        if freq.dim() != 1:
+            raise TypeError("freq is a vector")
+        self.freq = freq
+        self.c = _Rotary(_ptr(freq, torch.float64), 2 * freq.numel(), layout, scale, 0)
+        self.ref = C.byref(self.c)
+
+
+def _heads(t, dtype, n_rows: int, what: str):
+    """_rows of [n_rows][heads][dims] data."""
+    if t.dim() != 3:
+        raise TypeError(f"{what} is [n_rows][n_heads][head_dim]")
+    return _rows(t, dtype, n_rows, what)
+
+
+def dip_rotate_rows(rot: Rotary, x, positions, out, stream=None) -> None:
+    """x, out: [n_rows][n_heads][head_dim], float32 or bfloat16, rows may be strided; out may be x."""
+    import torch
+    if x.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"unsupported dtype {x.dtype}")
+    n = x.shape[0]
+    xp, xs = _heads(x, x.dtype, n, "x")
+    if out.shape != x.shape:
+        raise TypeError("x and out must have one shape")
+    op, os_ = _heads(out, x.dtype, n, "out")
+    _check(lib.dip_rotate_rows(rot.ref, xp, xs, _ints(positions, n, "positions"), n, x.shape[1], x.shape[2],
+                               DIP_F32 if x.dtype == torch.float32 else DIP_BF16, op, os_, _stream(stream)))
+
+
+def dip_kv_append_rotary(cache: KvCache, layer: int, batch: Batch, parents, rot: Rotary, q, q_out, k_new, v_new,
+                         stream=None) -> None:
+    """q, q_out: [n_rows][n_q_heads][head_dim] (None: keys and values alone); k_new, v_new: [n_rows][n_kv_heads][head_dim];
+    all of the cache's dtype, rows may be strided (slices of a fused projection).  parents: as in dip_tree_attention, or None."""
+    n, dt = batch.n_rows, cache.k.dtype
+    if tuple(k_new.shape[1:]) != (cache.k.shape[2], cache.k.shape[4]) or k_new.shape[1:] != v_new.shape[1:]:
+        raise TypeError("k_new and v_new rows must be [n_kv_heads][head_dim]")
+    if (q is None) != (q_out is None):
+        raise TypeError("q and q_out go together")
+    kp, ks = _heads(k_new, dt, n, "k_new")
+    vp, vs = _heads(v_new, dt, n, "v_new")
+    if ks != vs and n > 1:
+        raise TypeError("k_new and v_new must have one row stride")
+    qp = qs = op = os_ = heads = 0
+    if q is not None:
+        if q.dim() != 3 or q.shape[1:] != q_out.shape[1:] or q.shape[2] != cache.k.shape[4]:
+            raise TypeError("q and q_out are [n_rows][n_q_heads][head_dim]")
+        qp, qs = _heads(q, dt, n, "q")
+        op, os_ = _heads(q_out, dt, n, "q_out")
+        heads = q.shape[1]
+    _check(lib.dip_kv_append_rotary(cache.ref, layer, batch.ref, _ints(parents, n, "parents"), rot.ref, qp or None, qs, heads,
+                                    op or None, os_, kp, vp, ks, _stream(stream)))
 
 
 def dip_kv_compact(cache: KvCache, batch: Batch, path, keep, stream=None) -> None:
