@@ -647,6 +647,37 @@ int32_t dip_verify_tree(const dip_batch* batch, const int32_t* tokens, const int
                         const float* u, const float* u_sample, int32_t max_kids, int32_t* keep, int32_t* path,
                         int32_t* token, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * From logits to tokens, and to the probabilities that dip_verify_tree takes.  Row r: the words are ordered by their
+ * logits l, the largest first, equal ones by number, and weigh w(x) = exp((l(x) - l(first)) / temperature).  Kept are
+ *     the first top_k of them (top_k <= 0: all),
+ *     of these the fewest first ones whose weights come to top_p of what all of these weigh, and one at least
+ *     (top_p >= 1 or NaN: all),
+ *     of these the ones with w >= min_p (min_p <= 0 or NaN: all; above 1 counts as 1).
+ * token[r] = the first x, in order of the words' numbers, at which the running sum of the kept weights exceeds u[r] times
+ * their sum; probs[r] = the kept weights divided by their sum, 0 elsewhere.  A temperature that is not above 0 keeps
+ * the first word alone.  A logit of -inf is never kept, NaN counts as -inf; +inf outweighs all that is finite, and several
+ * share alike.  A row of nothing but -inf gives -1 and zeros.
+ * Weights are accurate to 2^-26 + 2^-50 |l / temperature| and summed in integers or fp64, so that results do not hang on the
+ * order of sums (bit-repeatable).
+ *   logits   n_rows (at most 65535) rows of n_vocab (at most 2^24), DIP_F32 or DIP_BF16, `stride` elements apart
+ *   how      host; per-row settings, device arrays of n_rows entries; a NULL array, or NULL for all: none of it (temperature 1)
+ *   u        n_rows numbers in [0, 1); may be NULL if token is
+ *   token    n_rows, or NULL     probs    n_rows rows of n_vocab, DIP_F32 or DIP_BF16, probs_stride elements apart, or NULL;
+ *            may be logits itself (same type and stride), but may not overlap it in another way
+ *   ws       *_workspace_bytes() bytes, 256-aligned
+ */
+typedef struct dip_sampling {
+    const float* temperature; /* device */
+    const int32_t* top_k;     /* device */
+    const float* top_p;       /* device */
+    const float* min_p;       /* device */
+} dip_sampling;
+size_t dip_sample_workspace_bytes(int32_t n_rows, int32_t n_vocab);
+int32_t dip_sample(const void* logits, int64_t stride, int32_t dtype, int32_t n_rows, int32_t n_vocab,
+                   const dip_sampling* how /* host */, const float* u, int32_t* token, void* probs, int64_t probs_stride,
+                   int32_t probs_dtype, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -210,3 +210,46 @@ def turn(x: np.ndarray, positions, freq, interleaved: bool, scale: float = 1.0) 
 def tree_positions(n_before: int, parents) -> List[int]:
     """Position of each node: as far behind the sequence as it is deep; an absent node's is the root's."""
     return [n_before + (len(a) - 1 if a else 0) for a in ancestors(parents)]
+
+
+# ---- sampling ------------------------------------------------------------------------------------------------
+def sample(logits: np.ndarray, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """One row: (kept weights by word, cuts one rule after the other over a sorted list; None if nothing is above -inf).
+    The second result is the smallest distance, relative to the sum, of a weight sum or a weight from a rule's border."""
+    x = np.where(np.isnan(logits), -np.inf, logits.astype(np.float64)) + 0.0
+    out, close = np.zeros(len(x)), np.inf
+    order = np.argsort(-x, kind="stable")
+    order = order[x[order] > -np.inf]
+    if not len(order):
+        return None, close
+    if not temperature > 0:
+        out[order[0]] = 1.0
+        return out, close
+    top = x[order[0]]
+    if top == np.inf:                                 # outweighs all that is finite, at any temperature
+        w = (x[order] == top).astype(np.float64)
+    else:
+        with np.errstate(over="ignore"):
+            w = np.exp((x[order] - top) / temperature)
+    if top_k > 0:
+        order, w = order[:top_k], w[:top_k]
+    if top_p < 1:
+        sums = np.cumsum(w)
+        close = min(close, np.abs(sums[:-1] / sums[-1] - top_p).min(initial=np.inf))
+        n = int(np.searchsorted(sums, top_p * sums[-1], side="left")) + 1
+        order, w = order[:n], w[:n]
+    if min_p > 0:
+        edge = min(min_p, 1.0)
+        close = min(close, np.abs(w[w != 1.0] / edge - 1).min(initial=np.inf))
+        order, w = order[w >= edge], w[w >= edge]
+    out[order] = w
+    return out, close
+
+
+def pick(weights: np.ndarray, u: float):
+    """(the word at which the running sum passes u, its distance from a border relative to the sum)."""
+    sums = np.cumsum(weights)
+    over = np.nonzero(sums > u * sums[-1])[0]
+    at = int(over[0]) if over.size else int(np.nonzero(weights)[0][-1])
+    at_border = np.abs(sums / sums[-1] - u)[weights > 0]
+    return at, float(at_border.min())

@@ -17,6 +17,17 @@ inline int elem_bytes(int dtype) { return dtype == DIP_F32 ? 4 : 2; }
 inline int rows_bound(const dip_batch* b) { return b->max_rows < b->n_rows ? b->max_rows : b->n_rows; }
 inline int log2_of(int v) { return 31 - __builtin_clz((unsigned)v); }
 
+// Whether one of `rows` rows at x, x_width bytes each, meets one at y.
+inline bool rows_overlap(const void* x, int64_t x_stride, int64_t x_width, const void* y, int64_t y_stride, int64_t y_width, int64_t rows) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
+    const uintptr_t a_end = a + (uintptr_t)((rows - 1) * x_stride + x_width), b_end = b + (uintptr_t)((rows - 1) * y_stride + y_width);
+    if (a_end <= b || b_end <= a) return false;
+    if (x_stride != y_stride) return true;
+    // (columns of one array side by side: no row of one meets a row of the other)
+    const uintptr_t stride = (uintptr_t)x_stride, off = b >= a ? (b - a) % stride : (stride - (a - b) % stride) % stride;
+    return off < (uintptr_t)x_width || off + (uintptr_t)y_width > stride;
+}
+
 // ---- the cache as the kernels take it ------------------------------------------------------
 // Strides in 16-byte pieces; the page size is a power of two.
 struct KvView {

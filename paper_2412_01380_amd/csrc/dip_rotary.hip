@@ -235,16 +235,6 @@ int32_t validate_rotary(const dip_rotary* r, int head_dim) {
     if (reinterpret_cast<uintptr_t>(r->freq) % 8) return fail(DIP_ERR_UNSUPPORTED, "rotary: freq must be 8-byte aligned");
     return DIP_OK;
 }
-// Whether one of `rows` rows at x, x_width bytes each, meets one at y.
-bool overlap(const void* x, int64_t x_stride, int64_t x_width, const void* y, int64_t y_stride, int64_t y_width, int64_t rows) {
-    const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
-    const uintptr_t a_end = a + (uintptr_t)((rows - 1) * x_stride + x_width), b_end = b + (uintptr_t)((rows - 1) * y_stride + y_width);
-    if (a_end <= b || b_end <= a) return false;
-    if (x_stride != y_stride) return true;
-    // (columns of one array side by side: no row of one meets a row of the other)
-    const uintptr_t stride = (uintptr_t)x_stride, off = b >= a ? (b - a) % stride : (stride - (a - b) % stride) % stride;
-    return off < (uintptr_t)x_width || off + (uintptr_t)y_width > stride;
-}
 // rows of a workgroup: 16 where that leaves enough workgroups for the chip, else fewer, and no more than LDS holds angles of
 int rows_of(int64_t n_rows, int pairs) {
     int rows = kRows;
@@ -310,7 +300,7 @@ int32_t dip_rotate_rows(const dip_rotary* rot, const void* x, int64_t x_stride, 
     if (x_stride < width || out_stride < width) return fail(DIP_ERR_INVALID_ARG, "rotate_rows: strides smaller than a row");
     if (x_stride % per || out_stride % per || !aligned16(x) || !aligned16(out))
         return fail(DIP_ERR_UNSUPPORTED, "rotate_rows: rows must start on 16-byte boundaries");
-    if (!(x == out && (x_stride == out_stride || n_rows == 1)) && overlap(x, x_stride * es, width * es, out, out_stride * es, width * es, n_rows))
+    if (!(x == out && (x_stride == out_stride || n_rows == 1)) && rows_overlap(x, x_stride * es, width * es, out, out_stride * es, width * es, n_rows))
         return fail(DIP_ERR_INVALID_ARG, "rotate_rows: out overlaps x without being it");
     RotateParams p;
     p.t = {rot->freq, rot->dims / 2, rot->scale};
@@ -356,7 +346,7 @@ int32_t dip_kv_append_rotary(const dip_kv_cache* cache, int32_t layer, const dip
     if (row_stride % per || !aligned16(k_new) || !aligned16(v_new) || (n_q_heads && (q_stride % per || q_out_stride % per || !aligned16(q) || !aligned16(q_out))))
         return fail(DIP_ERR_UNSUPPORTED, "append_rotary: rows must start on 16-byte boundaries");
     const auto meets = [&](const void* x, int64_t stride, int64_t w) {
-        return overlap(x, stride * es, w * es, q_out, q_out_stride * es, q_width * es, batch->n_rows);
+        return rows_overlap(x, stride * es, w * es, q_out, q_out_stride * es, q_width * es, batch->n_rows);
     };
     if (n_q_heads && !(q == q_out && (q_stride == q_out_stride || batch->n_rows == 1)) && meets(q, q_stride, q_width))
         return fail(DIP_ERR_INVALID_ARG, "append_rotary: q_out overlaps q without being it");

@@ -93,6 +93,10 @@ class _RotaryScaling(C.Structure):
                 ("original_len", C.c_double), ("factors", C.POINTER(C.c_double))]
 
 
+class _Sampling(C.Structure):
+    _fields_ = [("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p)]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(lib_path):
         raise ImportError(
@@ -180,6 +184,7 @@ def _load() -> C.CDLL:
             "dip_kv_append": [kv, i32, i32, bt, vp, vp, i64, i64, vp], "dip_kv_compact": [kv, bt, vp, vp, vp],
             "dip_window_attention": [kv, i32, bt, vp, i64, i32, f32, i32, i32, vp, i64, vp, sz, vp],
             "dip_tree_attention": [kv, i32, bt, vp, vp, i64, i32, f32, i32, i32, vp, i64, vp, sz, vp],
+            "dip_sample": [vp, i64, i32, i32, i32, C.POINTER(_Sampling), vp, vp, vp, i64, i32, vp, sz, vp],
             "dip_verify_tree": [bt, vp, vp, vp, i64, vp, i64, i32, i32, vp, vp, i32, vp, vp, vp, vp, sz, vp]}.items():
         getattr(L, name).restype = i32
         getattr(L, name).argtypes = args
@@ -189,6 +194,8 @@ def _load() -> C.CDLL:
     L.dip_attention_workspace_bytes.argtypes = [kv, bt, i32, i32, i32]
     L.dip_verify_tree_workspace_bytes.restype = sz
     L.dip_verify_tree_workspace_bytes.argtypes = [bt, i32, i32]
+    L.dip_sample_workspace_bytes.restype = sz
+    L.dip_sample_workspace_bytes.argtypes = [i32, i32]
     L.dip_tune_gemv.restype = i32
     L.dip_tune_gemv.argtypes = [i32, i32, i32, i32]
     L.dip_gemv_launch_shape.restype = i32
@@ -223,7 +230,8 @@ EXPORTS = ["dip_version", "dip_last_error", "dip_ca_scores", "dip_prune_topk", "
            "dip_tier_init", "dip_tiered_mlp_forward_workspace_bytes", "dip_tiered_mlp_forward",
            "dip_kv_init", "dip_kv_free", "dip_kv_fork", "dip_kv_copy_pages", "dip_kv_reserve_workspace_bytes", "dip_kv_reserve",
            "dip_rotary_frequencies", "dip_rotate_rows", "dip_kv_append", "dip_kv_append_rotary", "dip_kv_compact", "dip_attention_workspace_bytes", "dip_window_attention", "dip_tree_attention",
-           "dip_verify_tree_workspace_bytes", "dip_verify_tree", "dip_tune_gemv", "dip_gemv_launch_shape", "dip_set_fusion", "dip_fused_launch_shape", "dip_stream_read", "dip_profile_enable", "dip_profile_read",
+           "dip_verify_tree_workspace_bytes", "dip_verify_tree", "dip_sample_workspace_bytes", "dip_sample",
+           "dip_tune_gemv", "dip_gemv_launch_shape", "dip_set_fusion", "dip_fused_launch_shape", "dip_stream_read", "dip_profile_enable", "dip_profile_read",
            "dip_profile_disable"]
 
 
@@ -863,6 +871,30 @@ def dip_verify_tree(batch: Batch, tokens, parents, p, q, u, u_sample, max_kids: 
                                _ptr(u_sample, torch.float32), max_kids, _ints(keep, batch.n_batch, "keep"),
                                _ints(path, n, "path"), _ints(token, batch.n_batch, "token"), _ptr(ws),
                                ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def dip_sample_workspace_bytes(n_rows: int, n_vocab: int) -> int:
+    return lib.dip_sample_workspace_bytes(n_rows, n_vocab)
+
+
+def dip_sample(logits, u, token, probs, ws, temperature=None, top_k=None, top_p=None, min_p=None, stream=None) -> None:
+    """logits [n_rows][n_vocab] float32 or bfloat16, rows may be strided; u [n_rows] float32, token [n_rows] int32 (both
+    None: no tokens); probs [n_rows][n_vocab] float32 or bfloat16, or None; temperature, top_p, min_p [n_rows] float32 and
+    top_k [n_rows] int32, or None."""
+    import torch
+    kinds = {torch.float32: DIP_F32, torch.bfloat16: DIP_BF16}
+    if logits.dim() != 2 or logits.dtype not in kinds or (probs is not None and (probs.shape != logits.shape or probs.dtype not in kinds)):
+        raise TypeError("logits and probs are [n_rows][n_vocab], float32 or bfloat16")
+    n = logits.shape[0]
+    for name, t in (("u", u), ("temperature", temperature), ("top_p", top_p), ("min_p", min_p)):
+        if t is not None and t.numel() < n:
+            raise TypeError(f"{name} has {t.numel()} entries of {n}")
+    f32 = torch.float32
+    lp, ls = _rows(logits, logits.dtype, n, "logits")
+    pp, ps = _rows(probs, probs.dtype, n, "probs") if probs is not None else (None, 0)
+    how = _Sampling(_ptr(temperature, f32), _ints(top_k, n, "top_k"), _ptr(top_p, f32), _ptr(min_p, f32))
+    _check(lib.dip_sample(lp, ls, kinds[logits.dtype], n, logits.shape[1], C.byref(how), _ptr(u, f32), _ints(token, n, "token"), pp, ps,
+                          kinds[probs.dtype] if probs is not None else 0, _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
 
 
 def dip_tune_gemv(lanes_per_row: int = 0, waves: int = 0, ksplit: int = 0, unroll: int = 0) -> None:
