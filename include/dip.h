@@ -621,6 +621,60 @@ int32_t dip_tree_attention(const dip_kv_cache* cache, int32_t layer, const dip_b
                            const void* q, int64_t q_stride, int32_t n_q_heads, float scale, int32_t window,
                            int32_t sinks, void* out, int64_t out_stride, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- blocks of a long context ----
+ * Attention that reads, of each row's past, a few blocks chosen by the row itself.  A block is `block` positions from a
+ * multiple of `block` on: a power of two from 16 to the page size.  Of a sequence with `len` committed positions (the first
+ * max_len of them) are read
+ *     [0, front),       front = sinks, rounded up to whole blocks (and no more than tail),
+ *     the chosen blocks of [front, tail),
+ *     [tail, len),      tail = min(len - recent, the end of its last complete page), rounded down to whole blocks, >= 0,
+ * and the step's own rows, as in dip_window_attention (up to the row itself) or dip_tree_attention (a node's ancestors).
+ * So blocks are chosen from complete pages alone, whose positions no step changes.
+ */
+
+/* Bounds of the keys of every block, owned by the caller: of the cache's type, contiguous, 16-byte aligned,
+ *     [n_layers][n_pages][n_kv_heads][page_size / block][2][head_dim],
+ * the smallest number of each channel, then the largest (NaN not counted, an infinity as the largest finite number of its
+ * sign; 0 and 0 where there is none).  They belong to the page, whichever sequences share it. */
+size_t dip_block_bounds_bytes(const dip_kv_cache* cache, int32_t block);
+
+/*
+ * Work out the bounds of layers layer .. layer + n_layers - 1 for the complete pages of the n listed sequences (device
+ * array, at most 65535; numbers out of range are skipped) that hold some of their last `back` committed positions (0: all of them).
+ * To be called when positions were committed, with back as many as that (at least); pages copied by dip_kv_copy_pages take
+ * theirs by a call like this too.
+ */
+int32_t dip_kv_block_bounds(const dip_kv_cache* cache, int32_t layer, int32_t n_layers, const int32_t* seqs, int32_t n,
+                            int32_t back, int32_t block, void* bounds, void* stream);
+
+/*
+ * Choose blocks for every row and key/value head: of the blocks in [front, tail) the n_select (or all, if there are no more) with
+ * the largest
+ *     score = max over the query heads of the group of  sum_d max(q_d lo_d, q_d hi_d),
+ * an upper bound of q . k over the block's keys; equal scores, the lower block first.  Sums are fp64, rounded
+ * once to fp32; a sum that is NaN counts as -inf.
+ *   q        as in dip_window_attention
+ *   blocks   [n_rows][n_kv_heads][n_select], ascending, then -1; rows of an entry whose sequence is out of range: -1
+ *   n_select 1 .. DIP_MAX_SELECT        sinks, recent >= 0        ws  *_workspace_bytes() bytes, 256-aligned
+ */
+#define DIP_MAX_SELECT 4096
+size_t dip_select_blocks_workspace_bytes(const dip_kv_cache* cache, const dip_batch* batch, int32_t n_q_heads, int32_t block);
+int32_t dip_select_blocks(const dip_kv_cache* cache, int32_t layer, const dip_batch* batch, const void* q, int64_t q_stride,
+                          int32_t n_q_heads, int32_t block, const void* bounds, int32_t n_select, int32_t sinks,
+                          int32_t recent, int32_t* blocks, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Attention over what the blocks leave: arguments, softmax, rounding and what is not finite as in dip_window_attention (parents
+ * NULL) or dip_tree_attention.  blocks: as dip_select_blocks writes them, or of the caller's own making: ascending, unused
+ * entries, -1, at the end; an entry outside [front, tail) or not above the one before it is passed over.
+ */
+size_t dip_block_attention_workspace_bytes(const dip_kv_cache* cache, const dip_batch* batch, int32_t n_q_heads, int32_t block,
+                                           int32_t n_select, int32_t sinks, int32_t recent);
+int32_t dip_block_attention(const dip_kv_cache* cache, int32_t layer, const dip_batch* batch, const int32_t* parents,
+                            const int32_t* blocks, int32_t n_select, int32_t block, const void* q, int64_t q_stride,
+                            int32_t n_q_heads, float scale, int32_t sinks, int32_t recent, void* out, int64_t out_stride, void* ws,
+                            size_t ws_bytes, void* stream);
+
 /*
  * Verification of drafted trees (entries and parents as in dip_tree_attention, at most DIP_MAX_TREE
  * nodes).  Node t carries tokens[r]; p[r] is the target's distribution behind node t and q[r] the one

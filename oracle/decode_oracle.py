@@ -253,3 +253,45 @@ def pick(weights: np.ndarray, u: float):
     at = int(over[0]) if over.size else int(np.nonzero(weights)[0][-1])
     at_border = np.abs(sums / sums[-1] - u)[weights > 0]
     return at, float(at_border.min())
+
+
+# ---- blocks of a long context ----------------------------------------------------------------------------------
+def block_parts(n: int, page: int, block: int, sinks: int, recent: int):
+    """(front, tail): positions [0, front) and [tail, n) are always read, blocks are chosen between."""
+    tail = min(max(n - recent, 0), n - n % page) // block * block
+    return min(-(-sinks // block) * block, tail), tail
+
+
+def block_bounds(k: np.ndarray, most: float):
+    """Keys of a block [positions][D] -> (lo, hi); NaN not counted, infinities as +-most, 0 where there is nothing."""
+    lo, hi = np.zeros(k.shape[1]), np.zeros(k.shape[1])
+    for d in range(k.shape[1]):
+        x = k[:, d][~np.isnan(k[:, d])]
+        if x.size:
+            lo[d], hi[d] = max(min(x.min(), most), -most), max(min(x.max(), most), -most)
+    return lo, hi
+
+
+def choose_blocks(q: np.ndarray, lo: np.ndarray, hi: np.ndarray, first: int, n_select: int) -> List[int]:
+    """q [heads of a group][D], lo and hi [blocks][D]: the numbers (from `first` on) of the chosen ones, ascending."""
+    score = np.full(len(lo), -np.inf)
+    for h in q:
+        with np.errstate(invalid="ignore", over="ignore"):
+            s = (np.maximum(h, 0) * hi + np.minimum(h, 0) * lo).sum(1)
+        score = np.maximum(score, np.where(np.isnan(s), -np.inf, s))
+    with np.errstate(over="ignore"):
+        order = np.argsort(-score.astype(np.float32), kind="stable")[:n_select]
+    return sorted(first + int(b) for b in order)
+
+
+def block_visible(n: int, rows: int, front: int, tail: int, block: int, chosen, parents=None) -> np.ndarray:
+    """bool [rows][n + rows]; chosen: the blocks of each row."""
+    sees = visible(n, rows, 0, 0, parents)
+    for t in range(rows):
+        read = np.zeros(n + rows, dtype=bool)
+        read[:front] = True
+        read[tail:] = True
+        for b in chosen[t]:
+            read[b * block:(b + 1) * block] = True
+        sees[t] &= read
+    return sees

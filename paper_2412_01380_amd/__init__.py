@@ -27,5 +27,6 @@ from .libdip import (  # noqa: F401
     DIP_ROTARY_HALF, DIP_ROTARY_INTERLEAVED, DIP_MAX_ROTARY_DIMS, DIP_SCALING_NONE, DIP_SCALING_LINEAR, DIP_SCALING_BASE,
     DIP_SCALING_PARTS, DIP_SCALING_LIST, Rotary, dip_rotary_frequencies, dip_rotate_rows, dip_kv_append_rotary,
     dip_window_attention, dip_tree_attention, dip_verify_tree, dip_verify_tree_workspace_bytes,
-    dip_sample, dip_sample_workspace_bytes,
+    dip_sample, dip_sample_workspace_bytes, DIP_MAX_SELECT, dip_block_bounds_bytes, dip_kv_block_bounds,
+    dip_select_blocks, dip_select_blocks_workspace_bytes, dip_block_attention, dip_block_attention_workspace_bytes,
 )

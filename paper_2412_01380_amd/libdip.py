@@ -184,6 +184,9 @@ def _load() -> C.CDLL:
             "dip_kv_append": [kv, i32, i32, bt, vp, vp, i64, i64, vp], "dip_kv_compact": [kv, bt, vp, vp, vp],
             "dip_window_attention": [kv, i32, bt, vp, i64, i32, f32, i32, i32, vp, i64, vp, sz, vp],
             "dip_tree_attention": [kv, i32, bt, vp, vp, i64, i32, f32, i32, i32, vp, i64, vp, sz, vp],
+            "dip_kv_block_bounds": [kv, i32, i32, vp, i32, i32, i32, vp, vp],
+            "dip_select_blocks": [kv, i32, bt, vp, i64, i32, i32, vp, i32, i32, i32, vp, vp, sz, vp],
+            "dip_block_attention": [kv, i32, bt, vp, vp, i32, i32, vp, i64, i32, f32, i32, i32, vp, i64, vp, sz, vp],
             "dip_sample": [vp, i64, i32, i32, i32, C.POINTER(_Sampling), vp, vp, vp, i64, i32, vp, sz, vp],
             "dip_verify_tree": [bt, vp, vp, vp, i64, vp, i64, i32, i32, vp, vp, i32, vp, vp, vp, vp, sz, vp]}.items():
         getattr(L, name).restype = i32
@@ -194,6 +197,10 @@ def _load() -> C.CDLL:
     L.dip_attention_workspace_bytes.argtypes = [kv, bt, i32, i32, i32]
     L.dip_verify_tree_workspace_bytes.restype = sz
     L.dip_verify_tree_workspace_bytes.argtypes = [bt, i32, i32]
+    for name, args in {"dip_block_bounds_bytes": [kv, i32], "dip_select_blocks_workspace_bytes": [kv, bt, i32, i32],
+                       "dip_block_attention_workspace_bytes": [kv, bt, i32, i32, i32, i32, i32]}.items():
+        getattr(L, name).restype = sz
+        getattr(L, name).argtypes = args
     L.dip_sample_workspace_bytes.restype = sz
     L.dip_sample_workspace_bytes.argtypes = [i32, i32]
     L.dip_tune_gemv.restype = i32
@@ -231,6 +238,8 @@ EXPORTS = ["dip_version", "dip_last_error", "dip_ca_scores", "dip_prune_topk", "
            "dip_kv_init", "dip_kv_free", "dip_kv_fork", "dip_kv_copy_pages", "dip_kv_reserve_workspace_bytes", "dip_kv_reserve",
            "dip_rotary_frequencies", "dip_rotate_rows", "dip_kv_append", "dip_kv_append_rotary", "dip_kv_compact", "dip_attention_workspace_bytes", "dip_window_attention", "dip_tree_attention",
            "dip_verify_tree_workspace_bytes", "dip_verify_tree", "dip_sample_workspace_bytes", "dip_sample",
+           "dip_block_bounds_bytes", "dip_kv_block_bounds", "dip_select_blocks_workspace_bytes", "dip_select_blocks",
+           "dip_block_attention_workspace_bytes", "dip_block_attention",
            "dip_tune_gemv", "dip_gemv_launch_shape", "dip_set_fusion", "dip_fused_launch_shape", "dip_stream_read", "dip_profile_enable", "dip_profile_read",
            "dip_profile_disable"]
 
@@ -631,7 +640,7 @@ def dip_tiered_mlp_forward(mlp: TieredMlp, x, k_in: int, k_mid: int, cache_in: C
         _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
 
 
-DIP_MAX_BATCH, DIP_MAX_TREE = 1024, 64
+DIP_MAX_BATCH, DIP_MAX_TREE, DIP_MAX_SELECT = 1024, 64, 4096
 
 
 def _strides(t) -> tuple:
@@ -848,6 +857,63 @@ def dip_tree_attention(cache: KvCache, layer: int, batch: Batch, parents, q, sca
     _check(lib.dip_tree_attention(cache.ref, layer, batch.ref, _ints(parents, batch.n_rows, "parents"), qp, qs, q.shape[1],
                                   scale, window, sinks, op, os_, _ptr(ws), ws.numel() * ws.element_size(),
                                   _stream(stream)))
+
+
+def dip_block_bounds_bytes(cache: KvCache, block: int) -> int:
+    return lib.dip_block_bounds_bytes(cache.ref, block)
+
+
+def _block_of(cache: KvCache, bounds) -> int:
+    n_layers, n_pages, n_heads, page, dim = cache.k.shape
+    b = page // bounds.shape[3] if bounds.dim() == 6 and bounds.shape[3] else 0
+    if bounds.dim() != 6 or tuple(bounds.shape) != (n_layers, n_pages, n_heads, page // b if b else -1, 2, dim) or bounds.dtype != cache.k.dtype:
+        raise TypeError("bounds is [n_layers][n_pages][n_kv_heads][page_size / block][2][head_dim] of the cache's dtype")
+    return b
+
+
+def dip_kv_block_bounds(cache: KvCache, layer: int, n_layers: int, seqs, back: int, bounds, stream=None) -> None:
+    """bounds: [n_layers of the cache][n_pages][n_kv_heads][page_size / block][2][head_dim] of the cache's dtype."""
+    _check(lib.dip_kv_block_bounds(cache.ref, layer, n_layers, _ints(seqs, 1, "seqs"), seqs.numel(), back, _block_of(cache, bounds),
+                                   _ptr(bounds), _stream(stream)))
+
+
+def dip_select_blocks_workspace_bytes(cache: KvCache, batch: Batch, n_q_heads: int, block: int) -> int:
+    return lib.dip_select_blocks_workspace_bytes(cache.ref, batch.ref, n_q_heads, block)
+
+
+def _chosen(cache: KvCache, batch: Batch, blocks):
+    import torch
+    if blocks.dim() != 3 or blocks.shape[0] < batch.n_rows or blocks.shape[1] != cache.k.shape[2]:
+        raise TypeError("blocks is [n_rows][n_kv_heads][n_select]")
+    return _ptr(blocks, torch.int32)
+
+
+def _query_rows(cache: KvCache, batch: Batch, q):
+    if q.dim() != 3 or q.shape[2] != cache.k.shape[4]:
+        raise TypeError("q is [n_rows][n_q_heads][head_dim]")
+    return _rows(q, cache.k.dtype, batch.n_rows, "q")
+
+
+def dip_select_blocks(cache: KvCache, layer: int, batch: Batch, q, bounds, sinks: int, recent: int, blocks, ws, stream=None) -> None:
+    """q: [n_rows][n_q_heads][head_dim] of the cache's dtype, rows may be strided; bounds as in dip_kv_block_bounds; blocks:
+    [n_rows][n_kv_heads][n_select] int32, written."""
+    qp, qs = _query_rows(cache, batch, q)
+    _check(lib.dip_select_blocks(cache.ref, layer, batch.ref, qp, qs, q.shape[1], _block_of(cache, bounds), _ptr(bounds), blocks.shape[-1],
+                                 sinks, recent, _chosen(cache, batch, blocks), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def dip_block_attention_workspace_bytes(cache: KvCache, batch: Batch, n_q_heads: int, block: int, n_select: int, sinks: int = 0,
+                                        recent: int = 0) -> int:
+    return lib.dip_block_attention_workspace_bytes(cache.ref, batch.ref, n_q_heads, block, n_select, sinks, recent)
+
+
+def dip_block_attention(cache: KvCache, layer: int, batch: Batch, parents, blocks, block: int, q, scale: float, sinks: int, recent: int,
+                        out, ws, stream=None) -> None:
+    """blocks: [n_rows][n_kv_heads][n_select] int32; q, out as in dip_window_attention; parents as in dip_tree_attention, or None."""
+    qp, qs, op, os_ = _attention_rows(cache, batch, q, out)
+    _check(lib.dip_block_attention(cache.ref, layer, batch.ref, _ints(parents, batch.n_rows, "parents"), _chosen(cache, batch, blocks),
+                                   blocks.shape[-1], block, qp, qs, q.shape[1], scale, sinks, recent, op, os_, _ptr(ws),
+                                   ws.numel() * ws.element_size(), _stream(stream)))
 
 
 def dip_verify_tree_workspace_bytes(batch: Batch, n_vocab: int, max_kids: int) -> int:
