@@ -3,17 +3,20 @@
 // The kept words are the first ones in order of (logit, number), so every rule is a cut in one order: behind the top_k-th word,
 // behind the word at which the weights pass top_p of their sum, in front of the first word below min_p.  A cut is a logit and
 // a number among the words that have it.  It is found without sorting:
-//   sample_scan_kernel   a workgroup per chunk of a row: its maximum, and a histogram of count and weight over bins an eighth
-//                        of a nat wide, aligned to a grid that all chunks share (bin = floor(8 l / T)); the row's last
-//                        workgroup adds the histograms up and says which bins the cut lies in -- or, where no rule
-//                        applies, draws
-//   sample_cut_kernel    the words in these bins (a few in a hundred) go into a list; the row's last workgroup narrows
-//                        the cut down to a logit by histograms of 1024 key ranges over the list, and draws
-//   sample_probs_kernel  the probabilities
-// A weight is exp(-bin / 8) times a factor in (0.88, 1], which is held as an integer in units of 2^-30: sums over a bin are
-// integer sums, the same in any order, and 2^-27 accurate relative to the weight itself however small it is.  8 l / T and its place
-// in its bin are fp64 (2^-50 |l / T| more): of an fp32 quotient 2^-24 is lost, which at 30 nats is a weight off by 2 in 10^6.
+//   sample_scan_kernel     a workgroup per chunk of a row: its maximum, and a histogram of count and weight over bins an eighth
+//                          of a nat wide, aligned to a grid that all chunks share
+//   sample_row_kernel      a workgroup per row adds the histograms up and says which bins, and so which logits, the cut lies
+//                          in -- or, where no rule applies, draws
+//   sample_collect_kernel  the words with these logits (a few in a hundred) go into a list
+//   sample_cut_kernel      a workgroup per row narrows the cut down over the list, to a word, and draws
+//   sample_probs_kernel    the probabilities
+// A word's place is an integer: D = top - rint(8 2^23 l / T), in fp64, is how far below a grid line above the maximum it
+// lies, in units of 2^-23 of a bin.  Its bin is D >> 23, and its weight exp(-bin / 8) times a factor in (0.88, 1] that follows
+// from the other bits and is held in units of 2^-30.  So sums over a bin are integer sums, the same in any order, and 2^-26
+// accurate relative to the weight itself however small it is, and two chunks agree on every word's bin.  (Of an fp32 l / T 2^-24 is
+// lost, which at 30 nats is a weight off by 2 in 10^6.)
 
+#include <cfloat>
 #include <cmath>
 
 #include "dip_vocab_device.h"
@@ -21,17 +24,19 @@
 namespace dip {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;             // of the kernels over chunks
+constexpr int kRowThreads = 512;          // of the kernels that have a workgroup per row
 constexpr int kTile = kThreads * kPer;
-constexpr int kTiles = 2;                 // of a chunk, in registers
-constexpr int kChunk = kTiles * kTile;
-constexpr int kMaxChunks = (1 << 24) / kChunk;
+constexpr int kMaxTiles = 2;              // of a chunk, in registers
+constexpr int kMaxChunks = (1 << 24) / (kMaxTiles * kTile);
 constexpr int kBins = 512;                // the last one: all that lies 64 nats and more below the maximum
 constexpr int kRest = kBins - 1;
+constexpr int kPlaceBits = 23;            // of a place within a bin
 constexpr int kList = 8192;               // words of a row's list; where more qualify the row itself is gone through again
 constexpr int kRanges = 1024;             // key ranges of a step of narrowing down
-constexpr uint32_t kOne = 1u << 30;       // weight 1 within a bin
-constexpr int kCountShift = 44;           // a histogram word: count, weight
+constexpr int kFew = 64;                  // words that a wavefront puts in order
+constexpr float kOne = 0x1p30f;           // weight 1 within a bin
+constexpr int kCountShift = 45;           // a histogram word: count, weight
 constexpr uint64_t kWeightMask = (1ull << kCountShift) - 1;
 constexpr uint32_t kNothing = 0x007fffffu;    // key of -inf
 
@@ -45,64 +50,76 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k ^ ((int32_t)k < 0 ? 0x80000000u : 0xffffffffu)); }
 
-__device__ __forceinline__ bool infinite(double x) { return x == (double)INFINITY; }
-// 8 x / T (inv8 = 8 / T, 0 for an infinite temperature)
-__device__ __forceinline__ double scaled(float x, double inv8) { return x == INFINITY ? (double)INFINITY : (double)x * inv8; }
-
-// Where a word above -inf lies below `top`, the grid line of a maximum, and its weight within the bin.
+// rate = 8 2^23 / T, 0 for an infinite temperature; top: the grid line above a maximum (+inf where the maximum is).  A maximum
+// on a grid line has bin 1.
+__device__ __forceinline__ double place(float x, double rate) { return rint((double)x * rate); }
+__device__ __forceinline__ double top_of(float best, double rate) {
+    if (best == INFINITY) return (double)INFINITY;
+    return (floor(place(best, rate) * 0x1p-23) + 1.0) * 0x1p23;
+}
+// how far a finite word lies below a finite top, at most 2^32 - 1
+__device__ __forceinline__ uint32_t below(float x, double rate, double top) { return (uint32_t)fmin(top - place(x, rate), 4294967295.0); }
+// its weight within its bin, in units of 2^-30: 1 + (exp(t) - 1) by the series of the latter, of which the first term left
+// out is 1e-10
+__device__ __forceinline__ uint32_t weight_at(uint32_t d) {
+    const float t = (float)(d & ((1u << kPlaceBits) - 1)) * -0x1p-26f;
+    float q = fmaf(t, kOne / 720.f, kOne / 120.f);
+    q = fmaf(t, q, kOne / 24.f);
+    q = fmaf(t, q, kOne / 6.f);
+    q = fmaf(t, q, kOne / 2.f);
+    q = fmaf(t, q, kOne);
+    return (1u << 30) + (uint32_t)(int32_t)(q * t);
+}
 struct Place {
     int bin;
     uint32_t weight;
 };
-__device__ __forceinline__ Place place_of(float x, double inv8, double top) {
-    if (infinite(top)) return x == INFINITY ? Place{0, kOne} : Place{kRest, 0};
-    const double z = scaled(x, inv8), line = floor(z), below = top - line;
-    if (!(below < (double)kRest)) return {kRest, 0};
-    // exp((part - 1) / 8) - 1, by its series: the first term left out is 1e-10
-    const float t = ((float)(z - line) - 1.f) * 0.125f;
-    float q = fmaf(t, 1.f / 720.f, 1.f / 120.f);
-    q = fmaf(t, q, 1.f / 24.f);
-    q = fmaf(t, q, 1.f / 6.f);
-    q = fmaf(t, q, 0.5f);
-    q = fmaf(t, q, 1.f);
-    q *= t;
-    return {(int)below, (uint32_t)((int)kOne + (int)rintf(q * (float)kOne))};
+// of a word above -inf
+__device__ __forceinline__ Place place_of(float x, double rate, double top) {
+    if (top == (double)INFINITY) return x == INFINITY ? Place{0, 1u << 30} : Place{kRest, 0};
+    const uint32_t d = below(x, rate, top);
+    return {(int)(d >> kPlaceBits), weight_at(d)};
 }
 // what bins weigh: exp(-bin / 8) for weights in units of 2^-30, nothing behind the last
 __device__ __forceinline__ void bin_scales(double* out) {
-    for (int b = threadIdx.x; b < kBins; b += kThreads) out[b] = b == kRest ? 0.0 : exp(-0.125 * b) * 0x1p-30;
+    for (int b = threadIdx.x; b < kBins; b += kRowThreads) out[b] = b == kRest ? 0.0 : exp(-0.125 * b) * 0x1p-30;
+}
+// bins that a chunk's top lies below the row's
+__device__ __forceinline__ int bins_below(double chunk_top, double row_top) {
+    if (row_top == (double)INFINITY) return chunk_top == (double)INFINITY ? 0 : kRest;
+    return (int)fmin((row_top - chunk_top) * 0x1p-23, (double)kRest);
 }
 
 // ---- workspace -----------------------------------------------------------------------------------------
 struct alignas(32) Chunk {
-    double top;               // grid line of its maximum
-    double weight;            // of its words, in units of exp((top + 1) / 8)
-    uint64_t max_at;          // key of the maximum, ~number of the first word that has it
-    uint64_t count;           // words above -inf
+    double top;               // of its maximum, -inf: no words
+    double weight;            // of its words, in units of exp(top / 8)
+    float best;
+    int32_t first;            // of a greedy row: the first word that has it
 };
 struct alignas(128) Row {
     double top;
-    double inv8;
-    double total;             // of the kept words, in units of exp((top + 1) / 8)
+    double rate;
+    double total;             // of the kept words, in units of exp(top / 8)
     double part;              // top_p's share
     uint32_t key;             // kept: a larger key, or this one and a number up to
     int32_t at;
     int32_t state;
     int32_t greedy;
-    int32_t lo, hi;           // bins that the cut lies in
+    int32_t lo;               // the first bin that the cut may lie in, and the keys of these bins
+    uint32_t least, most;
     int32_t k;                // words up to top_k's cut, 0: no such rule
     int32_t by_part;          // top_p cuts
     uint32_t min_key;         // min_p's cut, 0: no such rule
-    int32_t listed;           // words in these bins: in the list, or too many for it
+    int32_t listed;           // words with these keys: in the list, or too many for it
     uint32_t n;               // words in the list so far
-    uint32_t least, most;     // their keys
     float best;               // the largest logit
 };
 
 struct SampleParams {
     const char* logits;
     int64_t stride;           // bytes
-    int n_vocab, chunks;
+    int n_rows, n_vocab, chunks, chunk;
     const float* temperature; // these four: nullable
     const int32_t* top_k;
     const float* top_p;
@@ -115,23 +132,43 @@ struct SampleParams {
     uint64_t* hist;           // [row][chunk][kBins]
     Row* rows;
     uint64_t* list;           // [row][kList]: key, number
-    uint64_t* tickets;        // a word per row, kTicketStride apart; another of the second kernel behind them
-    uint64_t epoch;
 };
 
-__device__ __forceinline__ void put64(void* to, uint64_t x) { __hip_atomic_store((uint64_t*)to, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ uint64_t get64(const void* from) { return __hip_atomic_load((const uint64_t*)from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ uint32_t get32(const uint32_t* from) { return __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// a row's settings
+struct How {
+    float T;
+    int k;                    // 0: all
+    float part, least;        // 1 and more: all; 0: all
+    bool greedy, cuts;
+    double rate;
+};
+__device__ __forceinline__ How how_of(const SampleParams& p, int row) {
+    How h;
+    h.T = p.temperature ? p.temperature[row] : 1.f;
+    h.greedy = !(h.T > 0.f);
+    h.rate = h.greedy ? 0.0 : 0x1p26 / (double)h.T;
+    const int k = p.top_k ? p.top_k[row] : 0;
+    h.k = k > 0 && k < p.n_vocab ? k : 0;
+    const float part = p.top_p ? p.top_p[row] : 1.f, least = p.min_p ? p.min_p[row] : 0.f;
+    h.part = part < 1.f ? fmaxf(part, 0.f) : 1.f;
+    h.least = isinf(h.T) || !(least > 0.f) ? 0.f : fminf(least, 1.f);
+    h.cuts = !h.greedy && (h.k || h.part < 1.f || h.least > 0.f);
+    return h;
+}
 
+// kPer words from x on, -inf from `end` on and in place of NaN
 template <typename E>
 __device__ __forceinline__ void load_logits(const char* row, int x, int end, float (&f)[kPer]) {
     load_entries<E>(row, x, end, f);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) f[i] = x + i < end && f[i] == f[i] ? f[i] : -INFINITY;
+    for (int i = 0; i < kPer; ++i) f[i] = fmaxf(f[i], -INFINITY);
+    if (x + kPer > end)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) f[i] = x + i < end ? f[i] : -INFINITY;
 }
 
-// exclusive sum over the workgroup, in order of the threads; *total: of all
-template <typename T>
+// exclusive sum over a workgroup, in order of the threads; *total: of all
+template <int THREADS, typename T>
 __device__ __forceinline__ T block_before(T x, T* waves, T* total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     T upto = x;
@@ -145,409 +182,563 @@ __device__ __forceinline__ T block_before(T x, T* waves, T* total) {
     __syncthreads();
     T before = upto - x, all = 0;
 #pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) {
+    for (int w = 0; w < THREADS / 64; ++w) {
         if (w < wave) before += waves[w];
         all += waves[w];
     }
     *total = all;
     return before;
 }
-__device__ __forceinline__ uint64_t block_max(uint64_t x, uint64_t* waves) {
+template <int THREADS>
+__device__ __forceinline__ float block_max(float x, float* waves) {
 #pragma unroll
-    for (int off = 32; off; off >>= 1) {
-        const uint64_t y = __shfl_xor((unsigned long long)x, off);
-        x = y > x ? y : x;
-    }
+    for (int off = 32; off; off >>= 1) x = fmaxf(x, __shfl_xor(x, off));
     __syncthreads();
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = x;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) x = waves[w] > x ? waves[w] : x;
+    for (int w = 0; w < THREADS / 64; ++w) x = fmaxf(x, waves[w]);
     return x;
 }
 
-struct Shared {
-    double scale[kBins];
-    double chunk[kMaxChunks];             // weights of the chunks' kept words
-    union {
-        struct {
-            uint32_t count[kRanges];
-            unsigned long long weight[kRanges];
-        } range;
-        struct {
-            double weight[kBins];
-            uint32_t count[kBins];
-            int below[kMaxChunks];        // grid lines that a chunk's maximum lies below the row's
-        } row;
-        unsigned long long fixed[kMaxChunks];     // chunk weights of the listed words
-    };
-    double waves_d[kThreads / 64];
-    uint64_t waves_u[kThreads / 64];
-    uint32_t waves_i[kThreads / 64];
-    double target;
-    double total;
-    uint64_t found;
-    int at, last, flag;
-    double got_weight;
-    uint32_t got_count, got_key, got_here;
-    double got_each;
-};
+// ---- chunks: grid (chunks, rows) ------------------------------------------------------------------------
+template <typename E, int TILES>
+__global__ void __launch_bounds__(kThreads) sample_scan_kernel(const SampleParams p) {
+    __shared__ unsigned long long s_hist[kBins];
+    __shared__ float s_max[kThreads / 64];
+    __shared__ double s_sum[kThreads / 64];
+    __shared__ int s_first;
+    const int row = blockIdx.y, chunk = blockIdx.x, tid = threadIdx.x;
+    const int begin = chunk * (TILES * kTile), end = min(p.n_vocab, begin + TILES * kTile);
+    float f[TILES][kPer];
+    float best = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) load_logits<E>(p.logits + row * p.stride, begin + t * kTile + tid * kPer, end, f[t]);
+    const How how = how_of(p, row);
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) best = fmaxf(best, f[t][i]);
+    for (int b = tid; b < kBins; b += kThreads) s_hist[b] = 0;
+    if (tid == 0) s_first = 0x7fffffff;
+    best = block_max<kThreads>(best, s_max);
+    const double top = best > -INFINITY ? top_of(best, how.rate) : -(double)INFINITY;
+    Chunk* sum = p.sums + (size_t)row * p.chunks + chunk;
+    if (tid == 0) {
+        sum->top = top;
+        sum->best = best;
+    }
+    if (how.greedy) {
+        int first = 0x7fffffff;
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (f[t][i] == best) first = min(first, begin + t * kTile + tid * kPer + i);
+        if (first != 0x7fffffff) atomicMin(&s_first, first);
+        __syncthreads();
+        if (tid == 0) sum->first = s_first;
+        return;
+    }
+    if (best == INFINITY) {
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (f[t][i] > -INFINITY) {
+                    const Place pl = place_of(f[t][i], how.rate, top);
+                    atomicAdd(&s_hist[pl.bin], (1ull << kCountShift) | pl.weight);
+                }
+    } else if (best > -INFINITY) {
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (f[t][i] > -INFINITY) {
+                    const uint32_t d = below(f[t][i], how.rate, top);
+                    atomicAdd(&s_hist[d >> kPlaceBits], (1ull << kCountShift) | weight_at(d));
+                }
+    }
+    __syncthreads();
+    if (how.cuts) {
+        uint64_t* out = p.hist + ((size_t)row * p.chunks + chunk) * kBins;
+        for (int b = tid; b < kBins; b += kThreads) out[b] = s_hist[b];
+    } else {
+        double weight = 0.0, all;
+        for (int b = tid; b < kRest; b += kThreads)
+            if (const uint64_t h = s_hist[b]) weight += (double)(h & kWeightMask) * (exp(-0.125 * b) * 0x1p-30);
+        block_before<kThreads>(weight, s_sum, &all);
+        if (tid == 0) sum->weight = all;
+    }
+}
+
+// The least of what the threads found, ascending with them (in LDS), by the first one of a wavefront that found anything;
+// likewise the most, by the last one.  (512 atomics on one word take 3 us.)
+__device__ __forceinline__ void to_least(int* least, bool found, int x) {
+    const uint64_t mask = __ballot(found);
+    if (mask && (int)(threadIdx.x & 63) == __ffsll((unsigned long long)mask) - 1) atomicMin(least, x);
+}
+__device__ __forceinline__ void to_most(int* most, bool found, int x) {
+    const uint64_t mask = __ballot(found);
+    if (mask && (int)(threadIdx.x & 63) == 63 - __clzll((long long)mask)) atomicMax(most, x);
+}
 
 // ---- the draw -----------------------------------------------------------------------------------------------
-// s.chunk holds what each chunk's kept words weigh; kept: a key above `key`, or `key` and a number up to `at`.
-// Returns the sum of all; the token is thread 0's to write.
-template <typename E>
-__device__ double draw(const SampleParams& p, int row, double top, double inv8, uint32_t key, int at, Shared& s) {
-    const int tid = threadIdx.x;
+struct Draw {
+    double scale[kBins];
+    double chunk[kMaxChunks];             // weights of the chunks' kept words
+    double waves[kRowThreads / 64];
+    double target;
+    int at, last;
+};
+// The place of the first of the threads' weights, in order, at which their running sum exceeds the target; where rounding leaves
+// none, of the last weight above 0; -1: there is none.  weight(i), i < n: the thread's own, at place first + i, `before` in front of them.
+template <typename F>
+__device__ __forceinline__ int first_past(F weight, int n, int first, double before, double target, Draw& s) {
+    if (threadIdx.x == 0) s.at = 0x7fffffff, s.last = -1;
     __syncthreads();
-    // running sums over the chunks, contiguous ones to a thread
-    const int per = (p.chunks + kThreads - 1) / kThreads;
+    int past = 0x7fffffff, some = -1;
+    for (int i = 0; i < n; ++i) {
+        const double w = weight(i);
+        before += w;
+        if (!(w > 0.0)) continue;
+        some = first + i;
+        if (before > target) past = min(past, first + i);
+    }
+    to_least(&s.at, past != 0x7fffffff, past);
+    to_most(&s.last, some >= 0, some);
+    __syncthreads();
+    return s.at != 0x7fffffff ? s.at : s.last;
+}
+// kept: a key above `key`, or `key` and a number up to `at`.  Returns the sum of all; the token is thread 0's to write.
+template <typename E>
+__device__ __forceinline__ double draw(const SampleParams& p, int row, double top, double rate, uint32_t key, int at, Draw& s) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    __syncthreads();
+    // the chunk, contiguous ones to a thread
+    const int per = (p.chunks + kRowThreads - 1) / kRowThreads, c0 = min(tid * per, p.chunks), n = min(p.chunks, c0 + per) - c0;
     double mine = 0.0;
-    for (int c = tid * per; c < min(p.chunks, (tid + 1) * per); ++c) mine += s.chunk[c];
+    for (int i = 0; i < n; ++i) mine += s.chunk[c0 + i];
     double total;
-    const double before = block_before(mine, s.waves_d, &total);
+    const double before = block_before<kRowThreads>(mine, s.waves, &total);
     if (!p.token) return total;
     const double target = (double)p.u[row] * total;
-    if (tid == 0) s.at = 0x7fffffff, s.last = -1, s.target = 0.0;
-    __syncthreads();
-    double run = before;
-    int first = 0x7fffffff, some = -1;
-    for (int c = tid * per; c < min(p.chunks, (tid + 1) * per); ++c) {
-        run += s.chunk[c];
-        if (s.chunk[c] > 0.0) {
-            some = c;
-            if (run > target) first = min(first, c);
-        }
-    }
-    if (first != 0x7fffffff) atomicMin(&s.at, first);
-    if (some >= 0) atomicMax(&s.last, some);
-    __syncthreads();
-    // (rounding may leave no chunk past the target: then the last one that holds anything)
-    const int c = s.at != 0x7fffffff ? s.at : s.last;
+    const int c = first_past([&](int i) { return s.chunk[c0 + i]; }, n, c0, before, target, s);
     if (c < 0) {
         if (tid == 0) p.token[row] = -1;
         return total;
     }
-    if (tid == c / per) {
+    if (c >= c0 && c < c0 + n) {
         double sum = before;
-        for (int i = tid * per; i < c; ++i) sum += s.chunk[i];
+        for (int i = c0; i < c; ++i) sum += s.chunk[i];
         s.target = target - sum;
     }
-    __syncthreads();
-    const double left = s.target;
-    if (tid == 0) s.at = 0x7fffffff, s.last = -1;
-    __syncthreads();
+    // in it the thread's words, contiguous ones
     const char* logits = p.logits + row * p.stride;
-    double ahead = 0.0;
-    for (int x0 = c * kChunk; x0 < min((c + 1) * kChunk, p.n_vocab); x0 += kTile) {
-        const int x = x0 + tid * kPer;
-        float f[kPer];
-        load_logits<E>(logits, x, p.n_vocab, f);
-        double w[kPer], sum = 0.0;
-        int some_word = -1;
+    const int begin = c * p.chunk, end = min(begin + p.chunk, p.n_vocab), words = p.chunk / kRowThreads;     // 8, 16 or 32
+    const float cut = of_key(key);                        // (of_key(kNothing) is -inf)
+    auto weight_of = [&](float x, int number) {
+        if (!(x > cut || (x == cut && number <= at)) || x == -INFINITY) return 0.0;
+        const Place pl = place_of(x, rate, top);
+        return (double)pl.weight * s.scale[pl.bin];
+    };
+    const int x = begin + tid * words;
+    float f[kMaxTiles * kTile / kRowThreads / kPer][kPer];
+    double sum = 0.0;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const uint32_t k = key_of(f[i]);
-            w[i] = 0.0;
-            if (f[i] > -INFINITY && (k > key || (k == key && x + i <= at))) {
-                const Place pl = place_of(f[i], inv8, top);
-                w[i] = (double)pl.weight * s.scale[pl.bin];
-                if (w[i] > 0.0) some_word = x + i;
-            }
-            sum += w[i];
-        }
-        double tile;
-        double run_sum = ahead + block_before(sum, s.waves_d, &tile);
-        int found = 0x7fffffff;
+    for (int t = 0; t < kMaxTiles * kTile / kRowThreads / kPer; ++t)
+        if (t * kPer < words) load_logits<E>(logits, x + t * kPer, min(end, x + words), f[t]);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            run_sum += w[i];
-            if (w[i] > 0.0 && run_sum > left) found = min(found, x + i);
-        }
-        if (found != 0x7fffffff) atomicMin(&s.at, found);
-        if (some_word >= 0) atomicMax(&s.last, some_word);
-        ahead += tile;
-        __syncthreads();
-        if (s.at != 0x7fffffff) break;
+    for (int t = 0; t < kMaxTiles * kTile / kRowThreads / kPer; ++t)
+        if (t * kPer < words)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) sum += weight_of(f[t][i], x + t * kPer + i);
+    double all;
+    const double ahead = block_before<kRowThreads>(sum, s.waves, &all);
+    const int thread = max(0, first_past([&](int) { return sum; }, 1, tid, ahead, s.target, s));
+    __syncthreads();
+    if (tid == thread) s.target -= ahead;
+    __syncthreads();
+    // and the word, a lane each
+    if (tid < 64) {
+        const int number = begin + thread * words + lane;
+        double w = 0.0;
+        if (lane < words && number < end) w = weight_of(fmaxf(entry_at<E>(logits, number), -INFINITY), number);
+        const double upto = running(w);
+        const uint64_t past = __ballot(w > 0.0 && upto > s.target), some = __ballot(w > 0.0);
+        const int first = past ? __ffsll((unsigned long long)past) - 1 : some ? 63 - __clzll((long long)some) : -1;
+        if (lane == 0) p.token[row] = first >= 0 ? number + first : -1;
     }
-    if (tid == 0) p.token[row] = s.at != 0x7fffffff ? s.at : s.last;
     return total;
 }
 
-// ---- chunks, and what a row is to be cut at: grid (chunks, rows) ------------------------------------------------
+// ---- what a row is to be cut at: grid (rows) --------------------------------------------------------------------
+// The smallest key whose word lies in one of the first `bins` bins below a finite top, by one wavefront: 64 candidates at a
+// time (a word's place falls as its key rises).
+__device__ __forceinline__ uint32_t least_key(double rate, double top, int bins) {
+    uint32_t from = kNothing + 1;         // the answer is `from` or more ...
+    const int lane = threadIdx.x & 63;
+    for (int shift = 26;; shift -= 6) {   // ... and less than from + 64 << shift
+        shift = max(shift, 0);
+        const uint64_t key = (uint64_t)from + ((uint64_t)lane << shift);
+        const bool in = key > 0xff7fffffull || below(of_key((uint32_t)key), rate, top) >> kPlaceBits < (uint32_t)bins;
+        const uint64_t mask = __ballot(in);
+        const int first = mask ? __ffsll((unsigned long long)mask) - 1 : 64;
+        if (shift == 0) return first ? from + first : from;
+        from += first ? (uint32_t)(first - 1) << shift : 0;
+        if (!first) return from;
+    }
+}
+
 template <typename E>
-__global__ void __launch_bounds__(kThreads) sample_scan_kernel(const SampleParams p) {
-    __shared__ Shared s;
-    __shared__ unsigned long long s_hist[kBins];
-    const int row = blockIdx.y, chunk = blockIdx.x, tid = threadIdx.x;
-    const float T = p.temperature ? p.temperature[row] : 1.f;
-    const bool greedy = !(T > 0.f);
-    const double inv8 = greedy ? 0.0 : 8.0 / (double)T;
-    const int k = p.top_k ? p.top_k[row] : 0;
-    const float part = p.top_p ? p.top_p[row] : 1.f;
-    float least = p.min_p ? p.min_p[row] : 0.f;
-    least = isinf(T) || !(least > 0.f) ? 0.f : fminf(least, 1.f);
-    const bool cuts = !greedy && ((k > 0 && k < p.n_vocab) || part < 1.f || least > 0.f);
-    uint64_t* ticket = p.tickets + (size_t)row * kTicketStride;
-    if (tid == 0) ticket_open(ticket, p.epoch);
-
-    float f[kTiles][kPer];
-    uint64_t best = 0;
-    uint32_t n = 0;
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-        const int x = chunk * kChunk + t * kTile + tid * kPer;
-        load_logits<E>(p.logits + row * p.stride, x, min(p.n_vocab, (chunk + 1) * kChunk), f[t]);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const bool is = f[t][i] > -INFINITY;
-            n += is;
-            const uint64_t at = is ? ((uint64_t)key_of(f[t][i]) << 32) | (uint32_t)~(x + i) : 0;
-            best = at > best ? at : best;
-        }
-    }
-    bin_scales(s.scale);
-    for (int b = tid; b < kBins; b += kThreads) s_hist[b] = 0;
-    best = block_max(best, s.waves_u);
-    uint32_t count;
-    block_before(n, s.waves_i, &count);
-    const double top = best ? floor(scaled(of_key((uint32_t)(best >> 32)), inv8)) : -(double)INFINITY;
-    double weight = 0.0;
-    if (!greedy && best) {
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (f[t][i] > -INFINITY) {
-                    const Place pl = place_of(f[t][i], inv8, top);
-                    atomicAdd(&s_hist[pl.bin], (1ull << kCountShift) | pl.weight);
-                }
-        __syncthreads();
-        for (int b = tid; b < kBins; b += kThreads) weight += (double)(s_hist[b] & kWeightMask) * s.scale[b];
-        double all;
-        block_before(weight, s.waves_d, &all);
-        weight = all;
-    }
-    if (cuts) {
-        uint64_t* out = p.hist + ((size_t)row * p.chunks + chunk) * kBins;
-        for (int b = tid; b < kBins; b += kThreads) put64(out + b, s_hist[b]);
-    }
-    Chunk* sum = p.sums + (size_t)row * p.chunks + chunk;
-    if (tid == 0) {
-        put((double*)&sum->top, top);
-        put((double*)&sum->weight, weight);
-        put64(&sum->max_at, best);
-        put64(&sum->count, count);
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) s.flag = ticket_last(ticket, p.epoch, p.chunks);
-    __syncthreads();
-    if (!s.flag) return;
-
-    // ---- the row ----
+__global__ void __launch_bounds__(kRowThreads) sample_row_kernel(const SampleParams p) {
+    __shared__ Draw s;
+    __shared__ double s_weight[kBins];
+    __shared__ uint32_t s_count[kBins];
+    __shared__ int s_below[kMaxChunks];
+    __shared__ float s_max[kRowThreads / 64];
+    __shared__ uint32_t s_waves[kRowThreads / 64];
+    __shared__ int s_range[2];
+    const int row = blockIdx.x, tid = threadIdx.x;
+    const How how = how_of(p, row);
     const Chunk* sums = p.sums + (size_t)row * p.chunks;
-    uint64_t first = 0;
-    uint32_t words = 0;
-    for (int c = tid; c < p.chunks; c += kThreads) {
-        const uint64_t at = get64(&sums[c].max_at);
-        first = at > first ? at : first;
-        words += (uint32_t)get64(&sums[c].count);
-    }
-    first = block_max(first, s.waves_u);
-    uint32_t n_words;
-    block_before(words, s.waves_i, &n_words);
     Row* r = p.rows + row;
-    if (first == 0 || greedy) {
+    float best = -INFINITY;
+    for (int c = tid; c < p.chunks; c += kRowThreads) best = fmaxf(best, sums[c].best);
+    best = block_max<kRowThreads>(best, s_max);
+    if (best == -INFINITY || how.greedy) {
+        if (tid == 0) s_range[0] = 0x7fffffff;
+        __syncthreads();
+        if (best > -INFINITY)
+            for (int c = tid; c < p.chunks; c += kRowThreads)
+                if (sums[c].best == best) atomicMin(&s_range[0], sums[c].first);
+        __syncthreads();
         if (tid == 0) {
-            r->state = first ? kDone : kEmpty;
+            r->state = best > -INFINITY ? kDone : kEmpty;
             r->greedy = 1;
-            r->key = (uint32_t)(first >> 32);
-            r->at = (int)~(uint32_t)first;
+            r->key = key_of(best);
+            r->at = s_range[0];
             r->total = 1.0;
-            r->top = r->inv8 = 0.0;
-            if (p.token) p.token[row] = first ? (int)~(uint32_t)first : -1;
+            r->top = r->rate = 0.0;
+            if (p.token) p.token[row] = best > -INFINITY ? s_range[0] : -1;
         }
         return;
     }
-    const float best_logit = of_key((uint32_t)(first >> 32));
-    const double row_top = floor(scaled(best_logit, inv8));
-    for (int c = tid; c < p.chunks; c += kThreads) {
-        const double below = infinite(row_top) ? (infinite(get(&sums[c].top)) ? 0.0 : (double)kRest) : row_top - get(&sums[c].top);
-        const int off = below < (double)kRest ? (int)below : kRest;
-        s.row.below[c] = off;
-        s.chunk[c] = off == kRest ? 0.0 : get(&sums[c].weight) * (s.scale[off] * 0x1p30);
-    }
+    const double top = top_of(best, how.rate);
+    bin_scales(s.scale);
     if (tid == 0) {
         r->state = kDone;
         r->greedy = 0;
-        r->best = best_logit;
-        r->top = row_top;
-        r->inv8 = inv8;
+        r->best = best;
+        r->top = top;
+        r->rate = how.rate;
         r->key = kNothing;
         r->at = -1;
     }
     __syncthreads();
-    if (!cuts) {
-        const double total = draw<E>(p, row, row_top, inv8, kNothing, -1, s);
+    for (int c = tid; c < p.chunks; c += kRowThreads) {
+        const int off = bins_below(sums[c].top, top);
+        s_below[c] = off;
+        s.chunk[c] = off == kRest || how.cuts ? 0.0 : sums[c].weight * (s.scale[off] * 0x1p30);
+    }
+    __syncthreads();
+    if (!how.cuts) {
+        const double total = draw<E>(p, row, top, how.rate, kNothing, -1, s);
         if (tid == 0) r->total = total;
         return;
     }
 
     // counts and weights of the row's bins, and their running sums
     const uint64_t* hist = p.hist + (size_t)row * p.chunks * kBins;
-    constexpr int PER = kBins / kThreads;
-    uint32_t cnt[PER], cnt_sum = 0;
+    constexpr int PER = kBins / kRowThreads;
+    uint32_t cnt[PER], cnt_sum = 0, rest = 0;
     double wgt[PER], wgt_sum = 0.0;
+    uint64_t w[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) cnt[i] = 0, w[i] = 0;
+    constexpr int FLIGHT = 16;            // chunks on their way at a time
+    for (int c0 = 0; c0 < p.chunks; c0 += FLIGHT) {
+        uint64_t h[FLIGHT][PER];
+#pragma unroll
+        for (int c = 0; c < FLIGHT; ++c) {
+            const int off = c0 + c < p.chunks ? s_below[c0 + c] : kBins;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {               // (a chunk whose maximum lies lower: its bins are shifted)
+                const int b = tid * PER + i;
+                h[c][i] = b >= off && (off == 0 || b < kRest) ? hist[(size_t)(c0 + c) * kBins + b - off] : 0;
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < FLIGHT; ++c)
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                cnt[i] += (uint32_t)(h[c][i] >> kCountShift);
+                w[i] += h[c][i] & kWeightMask;
+            }
+    }
+    // what is shifted out of them
+    for (int c = tid / 64; c < p.chunks; c += kRowThreads / 64)
+        for (int b = kBins - 1 - (tid & 63); s_below[c] && b >= max(0, kRest - s_below[c]); b -= 64) rest += (uint32_t)(hist[(size_t)c * kBins + b] >> kCountShift);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int b = tid * PER + i;
-        cnt[i] = 0;
-        uint64_t w = 0;
-        for (int c = 0; c < p.chunks && b < kRest; ++c) {
-            const int lb = b - s.row.below[c];
-            if (lb < 0) continue;
-            const uint64_t h = get64(hist + (size_t)c * kBins + lb);
-            cnt[i] += (uint32_t)(h >> kCountShift);
-            w += h & kWeightMask;
-        }
-        wgt[i] = (double)w * s.scale[b];
+        wgt[i] = (double)w[i] * s.scale[tid * PER + i];
         cnt_sum += cnt[i];
         wgt_sum += wgt[i];
     }
-    uint32_t known;
-    uint32_t cnt_before = block_before(cnt_sum, s.waves_i, &known);
-    if (tid == kThreads - 1) cnt[PER - 1] = n_words - known;
+    uint32_t known, more;
+    uint32_t cnt_before = block_before<kRowThreads>(cnt_sum, s_waves, &known);
+    block_before<kRowThreads>(rest, s_waves, &more);
+    const uint32_t n_words = known + more;
+    if (tid == kRowThreads - 1) cnt[PER - 1] += more;
     double total;
-    double wgt_before = block_before(wgt_sum, s.waves_d, &total);
+    double wgt_before = block_before<kRowThreads>(wgt_sum, s.waves, &total);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int b = tid * PER + i;
-        s.row.count[b] = cnt_before += cnt[i];
-        s.row.weight[b] = wgt_before += wgt[i];
+        s_count[b] = cnt_before += cnt[i];
+        s_weight[b] = wgt_before += wgt[i];
     }
     __syncthreads();
-    if (tid == 0) {
-        // (in order, by one thread: a binary search each)
+    if (tid < 64) {
+        // the first bin at which the running sums satisfy a rule: every lane looks at eight neighbouring ones
         auto bin_of = [&](auto past) {
-            int lo = 0, hi = kRest;
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (past(mid)) hi = mid;
-                else lo = mid + 1;
-            }
-            return lo;
+            int first = kRest;
+            for (int i = kBins / 64 - 1; i >= 0; --i)
+                if (past(tid * (kBins / 64) + i)) first = tid * (kBins / 64) + i;
+            const uint64_t mask = __ballot(past(tid * (kBins / 64) + kBins / 64 - 1));
+            const int lane = mask ? __ffsll((unsigned long long)mask) - 1 : 63;
+            return __shfl(first, lane);
         };
-        auto count_to = [&](int b) { return b < 0 ? 0u : s.row.count[b]; };
-        auto weight_to = [&](int b) { return b < 0 ? 0.0 : s.row.weight[b]; };
-        bool by_k = k > 0 && (uint32_t)k < n_words, by_part = part < 1.f;
+        auto count_to = [&](int b) { return b < 0 ? 0u : s_count[b]; };
+        auto weight_to = [&](int b) { return b < 0 ? 0.0 : s_weight[b]; };
+        bool by_k = how.k && (uint32_t)how.k < n_words, by_part = how.part < 1.f;
         int lo = kBins, hi = -1, bin_k = kRest;
-        if (by_k) lo = hi = bin_k = bin_of([&](int b) { return count_to(b) >= (uint32_t)k; });
+        if (by_k) lo = hi = bin_k = bin_of([&](int b) { return s_count[b] >= (uint32_t)how.k; });
         if (by_part) {
-            const double share = part > 0.f ? (double)part : 0.0;
-            const double from = share * (by_k ? weight_to(bin_k - 1) : total), to = share * (by_k ? weight_to(bin_k) : total);
-            lo = min(bin_k, bin_of([&](int b) { return weight_to(b) >= from && count_to(b) > 0; }));
-            hi = by_k ? bin_k : min(bin_k, bin_of([&](int b) { return weight_to(b) >= to && count_to(b) > 0; }));
+            const double from = (double)how.part * (by_k ? weight_to(bin_k - 1) : total), to = (double)how.part * (by_k ? weight_to(bin_k) : total);
+            lo = min(bin_k, bin_of([&](int b) { return s_weight[b] >= from && s_count[b] > 0; }));
+            hi = by_k ? bin_k : min(bin_k, bin_of([&](int b) { return s_weight[b] >= to && s_count[b] > 0; }));
         }
         uint32_t min_key = 0;
-        if (least > 0.f) {
-            const double c = least < 1.f ? (double)best_logit + (double)T * log((double)least) : (double)best_logit;
+        if (how.least > 0.f) {
+            const double c = how.least < 1.f ? (double)best + (double)how.T * log((double)how.least) : (double)best;
             float at = (float)c;
             if ((double)at < c) at = of_key(key_of(at) + 1);
             if (at > -INFINITY) {
                 min_key = key_of(at);
-                const double below = infinite(row_top) ? (at == INFINITY ? 0.0 : (double)kRest) : row_top - floor(scaled(at, inv8));
-                const int b = below < (double)kRest ? (int)below : kRest;
+                const int b = place_of(at, how.rate, top).bin;
                 if (b < lo) {
                     lo = hi = b;
                     by_k = by_part = false;
                 }
             }
         }
-        if (lo > hi) {                        // nothing cuts this row after all
-            s.flag = 0;
-        } else {
-            s.flag = 1;
-            r->state = kCut;
-            r->part = part > 0.f ? (double)part : 0.0;
-            r->lo = lo;
-            r->hi = hi;
-            r->k = by_k ? k : 0;
-            r->by_part = by_part;
-            r->min_key = min_key;
-            r->listed = (int)(count_to(hi) - count_to(lo - 1));
-            r->total = total;
-            r->n = 0;
-            r->least = 0xffffffffu;
-            r->most = 0;
+        if (lo <= hi) {
+            // the keys that these bins hold
+            uint32_t least = kNothing + 1, most = 0xff800000u;
+            if (top != (double)INFINITY) {
+                if (hi < kRest) least = least_key(how.rate, top, hi + 1);
+                most = lo > 0 ? least_key(how.rate, top, lo) - 1 : 0xff7fffffu;
+            } else if (hi == 0) {
+                least = most;
+            } else if (lo == kRest) {
+                most = 0xff7fffffu;
+            }
+            if (tid == 0) {
+                r->state = kCut;
+                r->part = (double)how.part;
+                r->lo = lo;
+                r->least = least;
+                r->most = most;
+                r->k = by_k ? how.k : 0;
+                r->by_part = by_part;
+                r->min_key = min_key;
+                r->listed = (int)(count_to(hi) - count_to(lo - 1));
+                r->total = total;
+                r->n = 0;
+            }
         }
+        if (tid == 0) s_range[0] = lo <= hi;
     }
     __syncthreads();
-    if (!s.flag) {
-        total = draw<E>(p, row, row_top, inv8, kNothing, -1, s);
-        if (tid == 0) r->total = total;
+    if (s_range[0]) return;
+    // nothing cuts this row after all
+    for (int c = tid >> 6; c < p.chunks; c += kRowThreads / 64) {
+        double sum = 0.0;
+        for (int b = tid & 63; b < kRest - s_below[c]; b += 64) sum += (double)(hist[(size_t)c * kBins + b] & kWeightMask) * s.scale[b + s_below[c]];
+        sum = wave_sum(sum);
+        if ((tid & 63) == 0) s.chunk[c] = sum;
     }
+    __syncthreads();
+    total = draw<E>(p, row, top, how.rate, kNothing, -1, s);
+    if (tid == 0) r->total = total;
 }
 
-// ---- the cut: grid (chunks, rows) -------------------------------------------------------------------------------
-// f(x, number) of every word that lies in the row's bins lo .. hi, by the threads of a workgroup
+// ---- words that the cut lies among: grid (chunks, rows) -----------------------------------------------------------
+template <typename E, int TILES>
+__global__ void __launch_bounds__(kThreads) sample_collect_kernel(const SampleParams p) {
+    __shared__ uint32_t s_waves[kThreads / 64];
+    __shared__ uint32_t s_at;
+    const int row = blockIdx.y, tid = threadIdx.x;
+    Row* r = p.rows + row;
+    if (r->state != kCut || r->listed > kList) return;
+    const float least = of_key(r->least), most = of_key(r->most);
+    const int begin = blockIdx.x * (TILES * kTile), end = min(p.n_vocab, begin + TILES * kTile);
+    const float best = p.sums[(size_t)row * p.chunks + blockIdx.x].best;
+    if (best < least) return;
+    float f[TILES][kPer];
+    uint64_t hits = 0;                    // a bit per word
+    static_assert(kMaxTiles * kPer <= 64, "a bit per word");
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+        load_logits<E>(p.logits + row * p.stride, begin + t * kTile + tid * kPer, end, f[t]);
+        uint32_t mask = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) mask |= f[t][i] >= least && f[t][i] <= most ? 1u << i : 0u;
+        hits |= (uint64_t)mask << (t * kPer);
+    }
+    uint32_t all;
+    const uint32_t before = block_before<kThreads>((uint32_t)__popcll(hits), s_waves, &all);
+    if (!all) return;
+    if (tid == 0) s_at = atomicAdd(&r->n, all);
+    __syncthreads();
+    uint32_t at = s_at + before;
+    uint64_t* list = p.list + (size_t)row * kList;
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (hits >> (t * kPer + i) & 1) {
+                if (at < (uint32_t)kList) list[at] = ((uint64_t)key_of(f[t][i]) << 32) | (uint32_t)(begin + t * kTile + tid * kPer + i);
+                ++at;
+            }
+}
+
+// ---- the cut: grid (rows) --------------------------------------------------------------------------------------------
+struct Cut {
+    Draw d;
+    union {
+        struct {
+            uint32_t count[kRanges];
+            unsigned long long weight[kRanges];
+        } range;
+        unsigned long long fixed[kMaxChunks];     // chunk weights of the listed words
+    };
+    uint64_t few[kFew];
+    uint64_t waves_u[kRowThreads / 64];
+    uint32_t waves_i[kRowThreads / 64];
+    int at, last;
+    uint32_t n_few, key;
+    uint32_t count, here;
+    double weight, each;
+};
+struct Listed {
+    int row, n;
+    bool listed;
+    double rate, top;
+    int lo;
+    uint32_t least, most;
+};
+// f(key, number) of every word whose key lies among those that the cut may have, by the threads of a workgroup
 template <typename E, typename F>
-__device__ __forceinline__ void each_word(const SampleParams& p, const Row& r, int row, bool listed, int n, F f) {
-    if (listed) {
-        const uint64_t* list = p.list + (size_t)row * kList;
-        for (int i = threadIdx.x; i < n; i += kThreads) {
-            const uint64_t e = get64(list + i);
-            f(of_key((uint32_t)(e >> 32)), (int)(uint32_t)e);
+__device__ __forceinline__ void each_word(const SampleParams& p, const Listed& l, F f) {
+    constexpr int FLIGHT = 8;
+    if (l.listed) {
+        const uint64_t* list = p.list + (size_t)l.row * kList;
+        for (int i0 = threadIdx.x; i0 < l.n; i0 += FLIGHT * kRowThreads) {
+            uint64_t e[FLIGHT];
+#pragma unroll
+            for (int i = 0; i < FLIGHT; ++i) e[i] = list[min(i0 + i * kRowThreads, l.n - 1)];
+#pragma unroll
+            for (int i = 0; i < FLIGHT; ++i)
+                if (i0 + i * kRowThreads < l.n) f((uint32_t)(e[i] >> 32), (int)(uint32_t)e[i]);
         }
     } else {
-        constexpr int FLIGHT = 8;
-        const char* logits = p.logits + row * p.stride;
-        for (int x0 = threadIdx.x; x0 < p.n_vocab; x0 += FLIGHT * kThreads) {
+        const char* logits = p.logits + l.row * p.stride;
+        for (int x0 = threadIdx.x; x0 < p.n_vocab; x0 += FLIGHT * kRowThreads) {
             float v[FLIGHT];
 #pragma unroll
-            for (int i = 0; i < FLIGHT; ++i) v[i] = entry_at<E>(logits, min(x0 + i * kThreads, p.n_vocab - 1));
+            for (int i = 0; i < FLIGHT; ++i) v[i] = entry_at<E>(logits, min(x0 + i * kRowThreads, p.n_vocab - 1));
 #pragma unroll
             for (int i = 0; i < FLIGHT; ++i) {
-                const int x = x0 + i * kThreads;
-                if (x >= p.n_vocab || !(v[i] > -INFINITY)) continue;
-                const int b = place_of(v[i], r.inv8, r.top).bin;
-                if (b >= r.lo && b <= r.hi) f(v[i], x);
+                const uint32_t k = key_of(fmaxf(v[i], -INFINITY));
+                if (x0 + i * kRowThreads < p.n_vocab && k >= l.least && k <= l.most) f(k, x0 + i * kRowThreads);
             }
         }
     }
 }
-
-// A listed word's weight as an integer, in units of exp((top - lo + 1) / 8) 2^-38: 2^24 of them fit 64 bits.
-__device__ __forceinline__ uint64_t fixed_weight(const Row& r, const Shared& s, float x) {
-    const Place pl = place_of(x, r.inv8, r.top);
-    return pl.bin == kRest ? 0 : (uint64_t)((double)pl.weight * (s.scale[max(pl.bin - r.lo, 0)] * 0x1p38) + 0.5);
+// A listed word's weight as an integer, in units of exp(-lo / 8) 2^-38: 2^24 of them fit 64 bits.
+__device__ __forceinline__ uint64_t fixed_weight(const Listed& l, const Cut& s, uint32_t key) {
+    const Place pl = place_of(of_key(key), l.rate, l.top);
+    return pl.bin == kRest ? 0 : (uint64_t)((double)pl.weight * (s.d.scale[max(pl.bin - l.lo, 0)] * 0x1p38) + 0.5);
 }
 
-// The logit at which the listed words, in order, first come to `need` words or to `need` in weight: in s.got_key, the
-// words and the weight in front of it in got_count and got_weight, how many have it in got_here, what one of them
-// weighs in got_each.
-template <typename E, bool WEIGHT>
-__device__ void narrow(const SampleParams& p, const Row& r, int row, bool listed, int n, uint32_t least, uint32_t most, double need, Shared& s) {
+// The number of the m-th word (from 1) of those with a key in [least, most], in order of their numbers; their key in s.key.
+template <typename E>
+__device__ __forceinline__ int nth(const SampleParams& p, const Listed& l, uint32_t least, uint32_t most, uint32_t m, Cut& s) {
     const int tid = threadIdx.x;
-    constexpr int PER = kRanges / kThreads;
-    uint32_t count = 0;
+    constexpr int PER = kRanges / kRowThreads;
+    uint32_t lo = 0, skipped = 0;
+    for (int shift = max(0, 32 - __clz(p.n_vocab) - 10);; shift = max(0, shift - 10)) {
+        __syncthreads();
+        for (int i = tid; i < kRanges; i += kRowThreads) s.range.count[i] = 0;
+        if (tid == 0) s.at = kRanges - 1;
+        __syncthreads();
+        each_word<E>(p, l, [&](uint32_t k, int number) {
+            const uint32_t at = ((uint32_t)number - lo) >> shift;
+            if (k < least || k > most || (uint32_t)number < lo || at >= kRanges) return;
+            atomicAdd(&s.range.count[at], 1u);
+            s.key = k;
+        });
+        __syncthreads();
+        uint32_t mine = 0, all;
+        for (int i = 0; i < PER; ++i) mine += s.range.count[tid * PER + i];
+        const uint32_t before = block_before<kRowThreads>(mine, s.waves_i, &all);
+        uint32_t run = skipped + before;
+        int found = kRanges;
+        for (int i = 0; i < PER; ++i) {
+            run += s.range.count[tid * PER + i];
+            if (run >= m) found = min(found, tid * PER + i);
+        }
+        to_least(&s.at, found < kRanges, found);
+        __syncthreads();
+        const int at = s.at;
+        if (tid == at / PER) {
+            uint32_t c = skipped + before;
+            for (int i = tid * PER; i < at; ++i) c += s.range.count[i];
+            s.count = c;
+        }
+        __syncthreads();
+        skipped = s.count;
+        lo += (uint32_t)at << shift;
+        if (shift == 0) return (int)lo;
+    }
+}
+
+// The word at which the listed ones, in order, first come to `need` words or to `need` in weight: its key in s.key, its
+// number in s.at, and what all up to it weigh in s.weight.  Words behind (end_key, end_at) are not looked at.
+template <typename E, bool WEIGHT>
+__device__ __forceinline__ void find(const SampleParams& p, const Listed& l, uint32_t end_key, int end_at, double need, Cut& s) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    constexpr int PER = kRanges / kRowThreads;
+    uint32_t least = end_key > l.least ? end_key : l.least, most = l.most, count = 0;
     double weight = 0.0;
+    auto ends = [&](uint32_t k, int number) { return k == end_key && number > end_at; };
     for (;;) {
         const uint32_t span = most - least;
         const int bits = span ? 32 - __clz((int)span) : 1, shift = max(0, bits - 10);
         __syncthreads();
-        for (int i = tid; i < kRanges; i += kThreads) {
+        for (int i = tid; i < kRanges; i += kRowThreads) {
             s.range.count[i] = 0;
             s.range.weight[i] = 0;
         }
-        if (tid == 0) s.at = kRanges, s.last = 0;
+        if (tid == 0) s.at = kRanges, s.last = 0, s.n_few = 0;
         __syncthreads();
-        each_word<E>(p, r, row, listed, n, [&](float x, int) {
-            const uint32_t k = key_of(x);
-            if (k < least || k > most) return;
+        each_word<E>(p, l, [&](uint32_t k, int number) {
+            if (k < least || k > most || ends(k, number)) return;
             const uint32_t at = (most - k) >> shift;
             atomicAdd(&s.range.count[at], 1u);
-            atomicAdd(&s.range.weight[at], (unsigned long long)fixed_weight(r, s, x));
+            atomicAdd(&s.range.weight[at], (unsigned long long)fixed_weight(l, s, k));
         });
         __syncthreads();
         uint32_t c_mine = 0, c_all;
@@ -556,10 +747,10 @@ __device__ void narrow(const SampleParams& p, const Row& r, int row, bool listed
             c_mine += s.range.count[tid * PER + i];
             w_mine += s.range.weight[tid * PER + i];
         }
-        uint32_t c_run = block_before(c_mine, s.waves_i, &c_all);
-        uint64_t w_run = block_before(w_mine, s.waves_u, &w_all);
-        const uint32_t c_before = c_run;
-        const uint64_t w_before = w_run;
+        const uint32_t c_before = block_before<kRowThreads>(c_mine, s.waves_i, &c_all);
+        const uint64_t w_before = block_before<kRowThreads>(w_mine, s.waves_u, &w_all);
+        uint32_t c_run = c_before;
+        uint64_t w_run = w_before;
         int found = kRanges, some = 0;
         for (int i = 0; i < PER; ++i) {
             const int at = tid * PER + i;
@@ -570,8 +761,8 @@ __device__ void narrow(const SampleParams& p, const Row& r, int row, bool listed
             const double have = WEIGHT ? weight + (double)w_run : (double)(count + c_run);
             if (have >= need) found = min(found, at);
         }
-        if (found < kRanges) atomicMin(&s.at, found);
-        if (some) atomicMax(&s.last, some);
+        to_least(&s.at, found < kRanges, found);
+        to_most(&s.last, some > 0, some);
         __syncthreads();
         // (rounding may leave the last one short of the need)
         const int at = s.at < kRanges ? s.at : s.last;
@@ -582,179 +773,121 @@ __device__ void narrow(const SampleParams& p, const Row& r, int row, bool listed
                 c += s.range.count[i];
                 w += s.range.weight[i];
             }
-            s.got_count = count + c;
-            s.got_weight = weight + (double)w;
-            s.got_here = s.range.count[at];
-            s.got_each = s.range.count[at] ? (double)s.range.weight[at] / (double)s.range.count[at] : 0.0;
+            s.count = count + c;
+            s.weight = weight + (double)w;
+            s.here = s.range.count[at];
+            s.each = s.range.count[at] ? (double)s.range.weight[at] / (double)s.range.count[at] : 0.0;
         }
         __syncthreads();
-        count = s.got_count;
-        weight = s.got_weight;
-        const uint32_t top = most - ((uint32_t)at << shift);
-        if (shift == 0) {
-            if (tid == 0) s.got_key = top;
+        count = s.count;
+        weight = s.weight;
+        const uint32_t here = s.here, high = most - ((uint32_t)at << shift), width = (1u << shift) - 1;
+        least = high - least > width ? high - width : least;
+        most = high;
+        if (here == 0) {                                  // (no listed word: nothing is cut)
+            if (tid == 0) s.key = kNothing, s.at = 0x7fffffff;
             __syncthreads();
             return;
         }
-        const uint32_t width = (1u << shift) - 1;
-        least = top - least > width ? top - width : least;
-        most = top;
+        if (here <= (uint32_t)kFew) {
+            each_word<E>(p, l, [&](uint32_t k, int number) {
+                if (k < least || k > most || ends(k, number)) return;
+                s.few[atomicAdd(&s.n_few, 1u)] = ((uint64_t)k << 32) | (uint32_t)~number;
+            });
+            __syncthreads();
+            if (tid < 64) {                               // every lane a word: what lies in front of it
+                const uint64_t mine = lane < (int)here ? s.few[lane] : 0;
+                const uint64_t w = lane < (int)here ? fixed_weight(l, s, (uint32_t)(mine >> 32)) : 0;
+                uint32_t c = 1;
+                uint64_t upto = w;
+                for (int j = 0; j < (int)here; ++j) {
+                    const uint64_t other = s.few[j];
+                    const uint64_t ow = __shfl((unsigned long long)w, j);
+                    if (other > mine) {
+                        ++c;
+                        upto += ow;
+                    }
+                }
+                const double have = WEIGHT ? weight + (double)upto : (double)(count + c);
+                // the first that comes to the need, or the last
+                const uint64_t past = __ballot(lane < (int)here && have >= need);
+                uint32_t rank = lane < (int)here && (past == 0 || (past >> lane & 1)) ? c : past ? 65u : 0u;
+                for (int off = 32; off; off >>= 1) {
+                    const uint32_t y = __shfl_xor(rank, off);
+                    rank = past ? min(rank, y) : max(rank, y);
+                }
+                if (lane < (int)here && c == rank) {
+                    s.key = (uint32_t)(mine >> 32);
+                    s.at = (int)~(uint32_t)mine;
+                    s.weight = weight + (double)upto;
+                }
+            }
+            __syncthreads();
+            return;
+        }
+        // one logit that many words have: a range is no wider than the distance of two
+        if (shift <= (sizeof(E) == 2 ? 15 : 0)) {
+            double more = WEIGHT ? (s.each > 0.0 ? ceil((need - weight) / s.each) : 1.0) : need - (double)count;
+            more = fmin(fmax(more, 1.0), (double)here);
+            const double all = weight + more * s.each;
+            const int number = nth<E>(p, l, least, most, (uint32_t)more, s);
+            __syncthreads();
+            if (tid == 0) {
+                s.at = number;
+                s.weight = all;
+            }
+            __syncthreads();
+            return;
+        }
     }
 }
 
-// The number of the m-th word (from 1) among the listed ones with a key, in order of their numbers.
 template <typename E>
-__device__ int nth(const SampleParams& p, const Row& r, int row, bool listed, int n, uint32_t key, uint32_t m, Shared& s) {
-    const int tid = threadIdx.x;
-    constexpr int PER = kRanges / kThreads;
-    uint32_t lo = 0, skipped = 0;
-    for (int shift = 14; shift >= 0; shift -= shift > 10 ? 10 : 4) {  // numbers of 24 bits: by 10, 10 and 4 of them
-        __syncthreads();
-        for (int i = tid; i < kRanges; i += kThreads) s.range.count[i] = 0;
-        if (tid == 0) s.at = kRanges - 1;
-        __syncthreads();
-        each_word<E>(p, r, row, listed, n, [&](float x, int number) {
-            const uint32_t at = ((uint32_t)number - lo) >> shift;
-            if (key_of(x) == key && (uint32_t)number >= lo && at < kRanges) atomicAdd(&s.range.count[at], 1u);
-        });
-        __syncthreads();
-        uint32_t mine = 0, all;
-        for (int i = 0; i < PER; ++i) mine += s.range.count[tid * PER + i];
-        const uint32_t before = block_before(mine, s.waves_i, &all);
-        uint32_t run = skipped + before;
-        int found = kRanges;
-        for (int i = 0; i < PER; ++i) {
-            run += s.range.count[tid * PER + i];
-            if (run >= m) found = min(found, tid * PER + i);
-        }
-        if (found < kRanges) atomicMin(&s.at, found);
-        __syncthreads();
-        const int at = s.at;
-        if (tid == at / PER) {
-            uint32_t c = skipped + before;
-            for (int i = tid * PER; i < at; ++i) c += s.range.count[i];
-            s.got_count = c;
-        }
-        __syncthreads();
-        skipped = s.got_count;
-        lo += (uint32_t)at << shift;
-        if (shift == 0) break;
-    }
-    return (int)lo;
-}
-
-template <typename E>
-__global__ void __launch_bounds__(kThreads) sample_cut_kernel(const SampleParams p) {
-    __shared__ Shared s;
-    const int row = blockIdx.y, chunk = blockIdx.x, tid = threadIdx.x;
+__global__ void __launch_bounds__(kRowThreads) sample_cut_kernel(const SampleParams p) {
+    __shared__ Cut s;
+    const int row = blockIdx.x, tid = threadIdx.x;
     Row* rp = p.rows + row;
     if (rp->state != kCut) return;
     const Row r = *rp;
-    uint64_t* ticket = p.tickets + (size_t)(gridDim.y + row) * kTicketStride;
-    if (tid == 0) ticket_open(ticket, p.epoch);
-    const bool listed = r.listed <= kList;
-    float f[kTiles][kPer];
-    uint32_t hits = 0, mine = 0, least = 0xffffffffu, most = 0;      // (a bit of hits per word)
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-        const int x = chunk * kChunk + t * kTile + tid * kPer;
-        load_logits<E>(p.logits + row * p.stride, x, min(p.n_vocab, (chunk + 1) * kChunk), f[t]);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            if (!(f[t][i] > -INFINITY)) continue;
-            const int b = place_of(f[t][i], r.inv8, r.top).bin;
-            if (b < r.lo || b > r.hi) continue;
-            hits |= 1u << (t * kPer + i);
-            ++mine;
-            const uint32_t k = key_of(f[t][i]);
-            least = min(least, k);
-            most = max(most, k);
-        }
-    }
-    static_assert(kTiles * kPer <= 32, "a bit per word");
-    uint32_t all;
-    const uint32_t before = block_before(mine, s.waves_i, &all);
-    const uint32_t top_key = (uint32_t)block_max(most, s.waves_u), low_key = ~(uint32_t)block_max((uint32_t)~least, s.waves_u);
-    if (tid == 0 && all) {
-        s.got_count = atomicAdd(&rp->n, all);
-        atomicMin(&rp->least, low_key);
-        atomicMax(&rp->most, top_key);
-    }
+    const Listed l = {row, min((int)r.n, kList), r.listed <= kList, r.rate, r.top, r.lo, r.least, r.most};
+    bin_scales(s.d.scale);
     __syncthreads();
-    if (all && listed) {
-        uint32_t at = s.got_count + before;
-        uint64_t* list = p.list + (size_t)row * kList;
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (hits >> (t * kPer + i) & 1) {
-                    if (at < (uint32_t)kList) put64(list + at, ((uint64_t)key_of(f[t][i]) << 32) | (uint32_t)(chunk * kChunk + t * kTile + tid * kPer + i));
-                    ++at;
-                }
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) s.flag = ticket_last(ticket, p.epoch, p.chunks);
-    __syncthreads();
-    if (!s.flag) return;
-
-    // ---- the row ----
-    const int n = (int)min(get32(&rp->n), (uint32_t)kList);
-    const uint32_t all_least = get32(&rp->least), all_most = get32(&rp->most);
-    bin_scales(s.scale);
-    __syncthreads();
-    // the chunks' words above the bins that the cut lies in
+    // the chunks' words above the bins that the cut lies in, a wavefront per chunk
     const Chunk* sums = p.sums + (size_t)row * p.chunks;
     const uint64_t* hist = p.hist + (size_t)row * p.chunks * kBins;
-    for (int c = tid; c < p.chunks; c += kThreads) s.chunk[c] = 0.0;
-    __syncthreads();
-    double above = 0.0;
-    uint32_t above_n = 0;
-    for (int c = tid >> 6; c < p.chunks; c += kThreads / 64) {        // a wavefront per chunk
-        const double below = infinite(r.top) ? (infinite(sums[c].top) ? 0.0 : (double)kRest) : r.top - sums[c].top;
+    double above = 0.0, above_all;
+    uint32_t above_n = 0, above_count;
+    for (int c = tid >> 6; c < p.chunks; c += kRowThreads / 64) {
+        const int off = bins_below(sums[c].top, r.top);
         double w = 0.0;
-        if (below < (double)kRest)
-            for (int b = (int)below + (tid & 63); b < r.lo; b += 64) {
-                const uint64_t h = hist[(size_t)c * kBins + b - (int)below];
-                w += (double)(h & kWeightMask) * s.scale[b];
-                above_n += (uint32_t)(h >> kCountShift);
-            }
+        for (int b = tid & 63; b < r.lo - off; b += 64) {
+            const uint64_t h = hist[(size_t)c * kBins + b];
+            w += (double)(h & kWeightMask) * s.d.scale[b + off];
+            above_n += (uint32_t)(h >> kCountShift);
+        }
         w = wave_sum(w);
         if ((tid & 63) == 0) {
-            s.chunk[c] = w;
+            s.d.chunk[c] = w;
             above += w;
         }
     }
-    double above_all;
-    block_before(above, s.waves_d, &above_all);
-    uint32_t above_count;
-    block_before(above_n, s.waves_i, &above_count);
-    // weights of listed words are counted in `unit`s
-    const double unit = s.scale[min(r.lo, kRest - 1)] * 0x1p-8;       // (exp(-lo / 8) 2^-38)
+    block_before<kRowThreads>(above, s.d.waves, &above_all);
+    block_before<kRowThreads>(above_n, s.waves_i, &above_count);
+    // weights of listed words are counted in units
+    const double unit = s.d.scale[min(r.lo, kRest - 1)] * 0x1p-8;     // (exp(-lo / 8) 2^-38)
     double total = r.total;
     uint32_t key = kNothing;
-    int at = -1;
+    int at = 0x7fffffff;
     if (r.k) {
-        const uint32_t need = (uint32_t)r.k - above_count;
-        narrow<E, false>(p, r, row, listed, n, all_least, all_most, (double)need, s);
-        key = s.got_key;
-        const uint32_t ties = need - s.got_count, here = s.got_here;
-        total = above_all + (s.got_weight + (double)ties * s.got_each) * unit;
-        at = ties < here && !r.by_part ? nth<E>(p, r, row, listed, n, key, ties, s) : 0x7fffffff;
-        if (r.by_part) at = (int)ties;        // (so far a count: the other cut lies in front of this one)
+        find<E, false>(p, l, key, at, (double)((uint32_t)r.k - above_count), s);
+        key = s.key;
+        at = s.at;
+        total = above_all + s.weight * unit;
     }
     if (r.by_part) {
-        const double need = (r.part * total - above_all) / unit;
-        const uint32_t key_k = key;
-        const int ties_k = at;
-        narrow<E, true>(p, r, row, listed, n, r.k ? key_k : all_least, all_most, need, s);
-        key = s.got_key;
-        const uint32_t here = r.k && key == key_k ? (uint32_t)ties_k : s.got_here;
-        double more = s.got_each > 0.0 ? ceil((need - s.got_weight) / s.got_each) : 1.0;
-        more = more < 1.0 ? 1.0 : more;
-        const uint32_t ties = more < (double)here ? (uint32_t)more : here;
-        at = ties < s.got_here ? nth<E>(p, r, row, listed, n, key, ties, s) : 0x7fffffff;
+        find<E, true>(p, l, key, at, (r.part * total - above_all) / unit, s);
+        key = s.key;
+        at = s.at;
     }
     if (r.min_key > key) {
         key = r.min_key;
@@ -762,15 +895,14 @@ __global__ void __launch_bounds__(kThreads) sample_cut_kernel(const SampleParams
     }
     // the kept ones among the listed
     __syncthreads();
-    for (int c = tid; c < p.chunks; c += kThreads) s.fixed[c] = 0;
+    for (int c = tid; c < p.chunks; c += kRowThreads) s.fixed[c] = 0;
     __syncthreads();
-    each_word<E>(p, r, row, listed, n, [&](float x, int number) {
-        const uint32_t k = key_of(x);
-        if (k > key || (k == key && number <= at)) atomicAdd(&s.fixed[number / kChunk], (unsigned long long)fixed_weight(r, s, x));
+    each_word<E>(p, l, [&](uint32_t k, int number) {
+        if (k > key || (k == key && number <= at)) atomicAdd(&s.fixed[number / p.chunk], (unsigned long long)fixed_weight(l, s, k));
     });
     __syncthreads();
-    for (int c = tid; c < p.chunks; c += kThreads) s.chunk[c] += (double)s.fixed[c] * unit;
-    total = draw<E>(p, row, r.top, r.inv8, key, at, s);
+    for (int c = tid; c < p.chunks; c += kRowThreads) s.d.chunk[c] += (double)s.fixed[c] * unit;
+    total = draw<E>(p, row, r.top, r.rate, key, at, s.d);
     if (tid == 0) {
         rp->total = total;
         rp->key = key;
@@ -779,7 +911,7 @@ __global__ void __launch_bounds__(kThreads) sample_cut_kernel(const SampleParams
     }
 }
 
-// ---- probabilities: grid (chunks, rows) ----------------------------------------------------------------------------
+// ---- probabilities: grid (tiles, rows) ----------------------------------------------------------------------------
 template <typename E, typename O>
 __global__ void __launch_bounds__(kThreads) sample_probs_kernel(const SampleParams p) {
     const int row = blockIdx.y;
@@ -788,56 +920,64 @@ __global__ void __launch_bounds__(kThreads) sample_probs_kernel(const SamplePara
     const bool greedy = rp->greedy;
     const uint32_t key = rp->key;
     // weights relative to the largest logit's: differences of logits are exact, of 8 l / T they are not where T is next to nothing
-    const double top = rp->top, inv8 = rp->inv8, best = (double)rp->best, step = inv8 * (0.125 * 1.44269504088896340736);
-    const float each = (float)(greedy || state == kEmpty ? 1.0 : (double)place_of(rp->best, inv8, top).weight * 0x1p-30 / rp->total);
-    const int end = min(p.n_vocab, (int)(blockIdx.x + 1) * kChunk);
+    const double top = rp->top, rate = rp->rate, best = (double)rp->best, step = rate * (0x1p-26 * 1.44269504088896340736);
+    const int x = (blockIdx.x * kThreads + threadIdx.x) * kPer;
+    if (x >= p.n_vocab) return;
+    float f[kPer];
+    load_logits<E>(p.logits + row * p.stride, x, p.n_vocab, f);
+    uint32_t kept = 0;
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-        const int x = blockIdx.x * kChunk + t * kTile + threadIdx.x * kPer;
-        if (x >= end) break;
-        float f[kPer];
-        load_logits<E>(p.logits + row * p.stride, x, end, f);
+    for (int i = 0; i < kPer; ++i) {
+        const uint32_t k = key_of(f[i]);
+        kept |= f[i] > -INFINITY && (k > key || (k == key && x + i <= at)) ? 1u << i : 0u;
+    }
+    if (state == kEmpty) kept = 0;
+    if (__any(kept != 0)) {
+        const Place first = place_of(rp->best, rate, top);
+        const float each = (float)(greedy ? 1.0 : (double)first.weight * (first.bin ? 0.88249690258459540286 : 1.0) * 0x1p-30 / rp->total);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const uint32_t k = key_of(f[i]);
-            const bool kept = state != kEmpty && f[i] > -INFINITY && (k > key || (k == key && x + i <= at));
-            float y = 0.f;
-            if (kept) {
-                if (greedy) y = 1.f;
-                else if (infinite(top)) y = f[i] == INFINITY ? each : 0.f;
-                else {                        // 2^(whole + part)
-                    const double z = ((double)f[i] - best) * step, whole = floor(z);
-                    y = whole < -400.0 ? 0.f : ldexpf(__builtin_amdgcn_exp2f((float)(z - whole)) * each, (int)whole);
-                }
+            float y;
+            if (greedy) y = 1.f;
+            else if (top == (double)INFINITY) y = f[i] == INFINITY ? each : 0.f;
+            else {                        // 2^(whole + part)
+                const double z = ((double)f[i] - best) * step, whole = floor(fmax(z, -400.0));
+                y = ldexpf(__builtin_amdgcn_exp2f((float)(z - whole)) * each, (int)whole);
             }
-            f[i] = y;
+            f[i] = kept >> i & 1 ? y : 0.f;
         }
-        struct __attribute__((packed, aligned(sizeof(O)))) Any { O w[16 / sizeof(O)]; };
-        O* out = (O*)(p.probs + row * p.probs_stride) + x;
-        constexpr int N = 16 / sizeof(O);
-        if (x + kPer <= end) {
+    } else {
 #pragma unroll
-            for (int y = 0; y < kPer / N; ++y) {
-                Any a;
+        for (int i = 0; i < kPer; ++i) f[i] = 0.f;
+    }
+    struct __attribute__((packed, aligned(sizeof(O)))) Any { O w[16 / sizeof(O)]; };
+    O* out = (O*)(p.probs + row * p.probs_stride) + x;
+    constexpr int N = 16 / sizeof(O);
+    if (x + kPer <= p.n_vocab) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) a.w[i] = (O)f[y * N + i];
-                *(Any*)(out + y * N) = a;
-            }
-        } else {
+        for (int y = 0; y < kPer / N; ++y) {
+            Any a;
 #pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (x + i < end) out[i] = (O)f[i];
+            for (int i = 0; i < N; ++i) a.w[i] = (O)f[y * N + i];
+            *(Any*)(out + y * N) = a;
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (x + i < p.n_vocab) out[i] = (O)f[i];
     }
 }
 
 struct SamplePlan {
-    int chunks;
-    size_t off_hist, off_rows, off_list, off_tickets, total;
+    int tiles, chunks;
+    size_t off_hist, off_rows, off_list, total;
 };
 SamplePlan plan_sample(int n_rows, int n_vocab) {
     SamplePlan pl;
-    pl.chunks = (n_vocab + kChunk - 1) / kChunk;
+    const int64_t tiles = (n_vocab + kTile - 1) / kTile;
+    pl.tiles = kMaxTiles;
+    while (pl.tiles > 1 && n_rows * ((tiles + pl.tiles - 1) / pl.tiles) < 1024 && tiles / (pl.tiles / 2) < kMaxChunks) pl.tiles /= 2;
+    pl.chunks = (int)((tiles + pl.tiles - 1) / pl.tiles);
     size_t o = 0;
     auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
     const size_t parts = (size_t)n_rows * pl.chunks;
@@ -845,7 +985,6 @@ SamplePlan plan_sample(int n_rows, int n_vocab) {
     pl.off_hist = take(sizeof(uint64_t) * kBins * parts);
     pl.off_rows = take(sizeof(Row) * n_rows);
     pl.off_list = take(sizeof(uint64_t) * kList * n_rows);
-    pl.off_tickets = take(sizeof(uint64_t) * kTicketStride * 2 * n_rows);
     pl.total = o;
     return pl;
 }
@@ -857,15 +996,17 @@ int32_t check_sample(int n_rows, int n_vocab) {
 }
 
 template <typename E>
-int32_t launch_sample(SampleParams& p, int n_rows, bool cuts, int probs_dtype, hipStream_t stream) {
-    const dim3 grid(p.chunks, n_rows), block(kThreads);
-    p.epoch = next_epoch();
-    int32_t st = check_hip(launch_timed(sample_scan_kernel<E>, grid, block, stream, DIP_KERNEL_SAMPLE, p), "sample_scan launch");
-    if (!st && cuts) st = check_hip(launch_timed(sample_cut_kernel<E>, grid, block, stream, DIP_KERNEL_SAMPLE, p), "sample_cut launch");
-    if (st || !p.probs) return st;
-    return check_hip(probs_dtype == DIP_F32 ? launch_timed(sample_probs_kernel<E, float>, grid, block, stream, DIP_KERNEL_SAMPLE, p)
-                                            : launch_timed(sample_probs_kernel<E, __bf16>, grid, block, stream, DIP_KERNEL_SAMPLE, p),
-                     "sample_probs launch");
+int32_t launch_sample(const SampleParams& p, const SamplePlan& pl, bool cuts, int probs_dtype, hipStream_t stream) {
+    const dim3 chunks(p.chunks, p.n_rows), rows(p.n_rows), tiles((p.n_vocab + kTile - 1) / kTile, p.n_rows), wide(kThreads), tall(kRowThreads);
+    const auto go = [&](auto kernel, dim3 grid, dim3 block, const char* what) { return check_hip(launch_timed(kernel, grid, block, stream, DIP_KERNEL_SAMPLE, p), what); };
+    int32_t st = go(pl.tiles == 2 ? sample_scan_kernel<E, 2> : sample_scan_kernel<E, 1>, chunks, wide, "sample_scan launch");
+    if (!st) st = go(sample_row_kernel<E>, rows, tall, "sample_row launch");
+    if (!st && cuts)
+        st = go(pl.tiles == 2 ? sample_collect_kernel<E, 2> : sample_collect_kernel<E, 1>, chunks, wide,
+                "sample_collect launch");
+    if (!st && cuts) st = go(sample_cut_kernel<E>, rows, tall, "sample_cut launch");
+    if (!st && p.probs) st = go(probs_dtype == DIP_F32 ? sample_probs_kernel<E, float> : sample_probs_kernel<E, __bf16>, tiles, wide, "sample_probs launch");
+    return st;
 }
 
 }  // namespace
@@ -904,8 +1045,10 @@ int32_t dip_sample(const void* logits, int64_t stride, int32_t dtype, int32_t n_
     SampleParams p;
     p.logits = (const char*)logits;
     p.stride = stride * es;
+    p.n_rows = n_rows;
     p.n_vocab = n_vocab;
     p.chunks = pl.chunks;
+    p.chunk = pl.tiles * kTile;
     p.temperature = how ? how->temperature : nullptr;
     p.top_k = how ? how->top_k : nullptr;
     p.top_p = how ? how->top_p : nullptr;
@@ -918,10 +1061,9 @@ int32_t dip_sample(const void* logits, int64_t stride, int32_t dtype, int32_t n_
     p.hist = (uint64_t*)(base + pl.off_hist);
     p.rows = (Row*)(base + pl.off_rows);
     p.list = (uint64_t*)(base + pl.off_list);
-    p.tickets = (uint64_t*)(base + pl.off_tickets);
     const bool cuts = p.top_k || p.top_p || p.min_p;
-    return dtype == DIP_F32 ? launch_sample<float>(p, n_rows, cuts, probs_dtype, (hipStream_t)stream)
-                            : launch_sample<uint16_t>(p, n_rows, cuts, probs_dtype, (hipStream_t)stream);
+    return dtype == DIP_F32 ? launch_sample<float>(p, pl, cuts, probs_dtype, (hipStream_t)stream)
+                            : launch_sample<uint16_t>(p, pl, cuts, probs_dtype, (hipStream_t)stream);
 }
 
 }  // extern "C"
