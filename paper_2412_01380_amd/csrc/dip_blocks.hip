@@ -2,14 +2,15 @@
 // (dip_select_blocks), and the attention itself (dip_block_attention).
 //
 // A block's smallest and largest key, channel by channel, bound q . k for all its keys: sum_d max(q_d lo_d, q_d hi_d).  With
-// q+ = max(q, 0), q- = max(-q, 0) this is q+ . hi - q- . lo.  Which blocks are read hangs on the order of these sums, so
-// that they are taken in fp64, where another order of adding moves them by 1e-16 and not by a block's rank.
+// q+ = max(q, 0), q- = max(-q, 0) this is q+ . hi - q- . lo.  Which blocks are read must not hang on the order in which a sum
+// is taken: the choice is that of the sums in fp64, where another order moves them by 1e-16 and not by a block's rank.
 
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
 
 #include "dip_attn_device.h"
+#include "dip_vocab_device.h"
 
 namespace dip {
 namespace blocks {
@@ -110,7 +111,13 @@ __global__ void __launch_bounds__(kThreads) block_bounds_kernel(const BoundsPara
     }
 }
 
-// ---- scores: grid (chunks of blocks, key/value heads, entries) --------------------------------------------------------------
+// ---- scores: grid (parts, key/value heads, entries) --------------------------------------------------------------
+// In fp32 on the matrix cores: [blocks x 2 D] times [2 D x columns], the bounds hi and lo times q+ and -q- of 16 columns (rows of the
+// entry times the heads of the group).  A lane loads 16 bytes of a block's bounds, 16 blocks and 64 bytes of each at a time, straight
+// into the product's operands, and they serve all columns: the call waits for memory (16 tokens over up to 64k positions, blocks of
+// 32: 92 MB).  In fp64 without the matrix cores it took 44 us, and 24 for trees.
+// The same sums with |hi| + |lo| and |q|, T, bound what rounding does to a score: half of its products are zero, the others are D
+// roundings of 2^-23 T at most, in whatever order they are added up.  The choice settles in fp64 what lies nearer to its border than that.
 struct ChoiceParams {
     KvView c;
     BatchView b;
@@ -118,8 +125,10 @@ struct ChoiceParams {
     int64_t q_stride;         // bytes
     const char* bounds;       // at the layer
     float* scores;            // [row][head][most]
+    float4* stats;            // [entry][head][part]: least and most score, error bound (inf: none known)
     int32_t* out;             // [row][head][n_select]
-    int most;                 // blocks of a sequence that there may be
+    int most;                 // blocks of a sequence that there may be, a multiple of 4
+    int parts;                // workgroups that share an entry's blocks of a head
     int group;
     int block_shift;
     int n_select, sinks, recent, max_len;
@@ -132,106 +141,170 @@ __device__ __forceinline__ Middle middle_of(const ChoiceParams& p, int len) {
     const Parts x = parts_of(min(len, p.max_len), p.c.page_shift, p.block_shift, p.sinks, p.recent);
     return {x.front >> p.block_shift, (x.tail - x.front) >> p.block_shift};
 }
-
-// Lanes of a block: each holds 16 bytes of its bounds' channels.
-template <typename E, int D>
-struct Lanes {
-    static constexpr int PIECES = D * sizeof(E) / 16, L = PIECES <= 8 ? 8 : PIECES <= 16 ? 16 : 32;
-};
-// sum over L neighbouring lanes, in the last of them
-template <int L>
-__device__ __forceinline__ double sum_of_lanes(double x) {
-    const auto moved = [&](auto ctrl) {
-        const uint64_t b = __double_as_longlong(x);
-        const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, decltype(ctrl)::value, 0xf, 0xf, true);
-        const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(b >> 32), decltype(ctrl)::value, 0xf, 0xf, true);
-        return __longlong_as_double(((uint64_t)hi << 32) | lo);
-    };
-    x += moved(std::integral_constant<int, 0x111>());     // row_shr 1, 2, 4, 8
-    x += moved(std::integral_constant<int, 0x112>());
-    x += moved(std::integral_constant<int, 0x114>());
-    if constexpr (L >= 16) x += moved(std::integral_constant<int, 0x118>());
-    if constexpr (L == 32) x += __shfl_up(x, 16);
-    return x;
+// a block's bounds of a head
+__device__ __forceinline__ const char* bounds_of(const ChoiceParams& p, const int32_t* table, int head, int b) {
+    const int per_shift = p.c.page_shift - p.block_shift;
+    const int named = table[b >> per_shift], page = is_page(p.c, named) ? named : 0;
+    const int64_t at = (((int64_t)page * p.c.n_heads + head) << per_shift) + (b & ((1 << per_shift) - 1));
+    return p.bounds + at * 2 * p.c.pieces * 16;
 }
 
-constexpr int kBlocks = 4;                // of a group of lanes, in registers
-constexpr int kHeads = 2;                 // query heads at a time
+constexpr int kChunk = kThreads / 64 * 16;               // blocks at a time, 16 of a wavefront
+// one 16-byte piece of 16 blocks times the same of 16 columns
+template <typename E>
+__device__ __forceinline__ f32x4 product(u32x4 a, u32x4 b, f32x4 c) {
+    if constexpr (sizeof(E) == 2) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(attn::bf16x8, a), __builtin_bit_cast(attn::bf16x8, b), c, 0, 0, 0);
+    } else {
+        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
+        return c;
+    }
+}
+// numbers above 0, below 0, and without their signs
+template <typename E>
+__device__ __forceinline__ void split(u32x4 x, u32x4& up, u32x4& down, u32x4& size) {
+    constexpr uint32_t SIGN = sizeof(E) == 2 ? 0x80008000u : 0x80000000u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t below = sizeof(E) == 2 ? ((x[i] >> 15) & 0x00010001u) * 0xffffu : (uint32_t)((int32_t)x[i] >> 31);
+        up[i] = x[i] & ~below;
+        down[i] = x[i] & below;
+        size[i] = x[i] & ~SIGN;
+    }
+}
+template <typename E>
+__device__ __forceinline__ u32x4 sizes(u32x4 x) {
+    u32x4 up, down, size;
+    split<E>(x, up, down, size);
+    return size;
+}
+template <typename E>
+__device__ __forceinline__ float largest(u32x4 size) {
+    uint32_t m = 0;                                       // (numbers without signs are in order of their bits)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = sizeof(E) == 2 ? max(m, max(size[i] & 0xffff0000u, size[i] << 16)) : max(m, size[i]);
+    return __uint_as_float(m);
+}
+
 template <typename E, int D>
-__global__ void __launch_bounds__(kThreads) block_scores_kernel(const ChoiceParams p) {
-    typedef Lanes<E, D> X;
-    constexpr int N = 16 / sizeof(E), GROUPS = kThreads / X::L, CHUNK = GROUPS * kBlocks;
-    const int e = blockIdx.z, head = blockIdx.y, lane = threadIdx.x % X::L, g = threadIdx.x / X::L;
+__global__ void __launch_bounds__(kThreads, sizeof(E) == 2 ? 4 : 3) block_scores_kernel(const ChoiceParams p) {
+    constexpr int ES = sizeof(E), STEPS = D * ES / 64, PIECES = D * ES / 16, WAVES = kThreads / 64;
+    __shared__ float s_tile[WAVES][16][20];               // [column][block]
+    __shared__ float s_stat[3][WAVES];
+    const int e = blockIdx.z, head = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const EntryRows er = entry_rows(p.b, e);
     const int seq = entry_seq(p.b, p.c, e);
     if (seq < 0 || er.rows == 0) return;
     const Middle m = middle_of(p, entry_len(p.c, seq));
-    const int b0 = blockIdx.x * CHUNK;
-    if (b0 >= m.n || m.n <= p.n_select) return;           // (all of them are chosen)
+    if ((int)blockIdx.x * kChunk >= m.n || m.n <= p.n_select) return;     // (all of them are chosen)
     const int32_t* table = p.c.table + (size_t)seq * p.c.max_pages;
-    const int per_shift = p.c.page_shift - p.block_shift;
-    const bool has = lane < X::PIECES;
-    u32x4 lo[kBlocks], hi[kBlocks];
+    const int n = lane & 15, g = lane >> 4;
+    float least = INFINITY, most = -INFINITY, error = 0.f;
+    const int side = p.group < 16 ? 16 / p.group : 1;     // rows side by side in the columns
+    const auto block_at = [&](int c) { return m.first + min(c * kChunk + wave * 16 + n, m.n - 1); };
+    u32x4 lo[STEPS], hi[STEPS], x[STEPS];
+    const auto load = [&](const char* at) {
+        const u32x4* from = (const u32x4*)at + g;
 #pragma unroll
-    for (int i = 0; i < kBlocks; ++i) {
-        const int b = m.first + min(b0 + i * GROUPS + g, m.n - 1);
-        const int named = table[b >> per_shift], page = is_page(p.c, named) ? named : 0;
-        const int64_t at = (((int64_t)page * p.c.n_heads + head) << per_shift) + (b & ((1 << per_shift) - 1));
-        const u32x4* from = (const u32x4*)p.bounds + at * 2 * X::PIECES + (has ? lane : 0);
-        lo[i] = from[0];
-        hi[i] = from[X::PIECES];
+        for (int s = 0; s < STEPS; ++s) lo[s] = from[4 * s];
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) hi[s] = from[PIECES + 4 * s];
+    };
+    // the queries of column n: row t0 + r, head h of the group
+    const auto load_q = [&](int t0, int h0) {
+        const int r = p.group < 16 ? n / p.group : 0, h = p.group < 16 ? n - r * p.group : h0 + n;
+        const bool has = r < side && t0 + r < er.rows && h < p.group;
+        const u32x4* q = (const u32x4*)(p.q + (int64_t)(er.first + t0 + (has ? r : 0)) * p.q_stride + (int64_t)(head * p.group + (has ? h : 0)) * (D * ES)) + g;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            x[s] = q[4 * s];
+            if (!has) x[s] = u32x4{0, 0, 0, 0};
+        }
+    };
+    const bool once = er.rows <= side && p.group <= 16;   // one set of columns: it stays in registers
+    load(bounds_of(p, table, head, block_at(blockIdx.x)));
+    if (once) load_q(0, 0);
+    const char* next = bounds_of(p, table, head, block_at(blockIdx.x + gridDim.x));
+    for (int c = blockIdx.x; c * kChunk < m.n; c += gridDim.x) {
+        const int b0 = c * kChunk + wave * 16;
+        for (int t0 = 0; t0 < er.rows; t0 += side) {
+            float best[4];                                // of (row, block) lane + 64 i of side x 16
+#pragma unroll
+            for (int i = 0; i < 4; ++i) best[i] = -INFINITY;
+            for (int h0 = 0; h0 < p.group; h0 += 16) {
+                if (!once) load_q(t0, h0);
+                f32x4 sum = {0, 0, 0, 0}, bound = {0, 0, 0, 0};
+                float q_most = 0.f;
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) {
+                    u32x4 up, down, size;
+                    split<E>(x[s], up, down, size);
+                    q_most = fmaxf(q_most, largest<E>(size));
+                    sum = product<E>(hi[s], up, sum);
+                    bound = product<E>(sizes<E>(hi[s]), size, bound);
+                    sum = product<E>(lo[s], down, sum);
+                    bound = product<E>(sizes<E>(lo[s]), size, bound);
+                }
+                // (should products flush what is below the normal numbers, each of them is off by the query times 2^-126)
+                error = fmaxf(error, q_most <= FLT_MAX ? q_most * 0x1p-117f : INFINITY);
+                float tall = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tall = tall <= FLT_MAX && bound[i] <= FLT_MAX ? fmaxf(tall, bound[i]) : INFINITY;
+                error = fmaxf(error, tall * ((D + 8) * 0x1p-23f));
+                if (t0 + side >= er.rows && h0 + 16 >= p.group && (c + (int)gridDim.x) * kChunk < m.n) {
+                    load(next);                           // (the chunk's last product is done with them)
+                    next = bounds_of(p, table, head, block_at(c + 2 * (int)gridDim.x));
+                }
+                *(f32x4*)&s_tile[wave][n][4 * g] = sum;
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                const int heads = min(16, p.group - h0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int y = lane + 64 * i, row = y >> 4;
+                    if (row >= side) continue;
+                    for (int k = 0; k < heads; ++k) best[i] = fmaxf(best[i], s_tile[wave][row * p.group + k][y & 15]);
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int y = lane + 64 * i, row = t0 + (y >> 4), b = b0 + (y & 15);
+                if ((y >> 4) >= side || row >= er.rows || b >= m.n) continue;
+                p.scores[((size_t)(er.first + row) * p.c.n_heads + head) * p.most + b] = best[i];
+                least = fminf(least, best[i]);
+                most = fmaxf(most, best[i]);
+            }
+        }
     }
-    for (int t = 0; t < er.rows; ++t) {
-        const char* q = p.q + (int64_t)(er.first + t) * p.q_stride + (int64_t)head * p.group * (D * (int)sizeof(E));
-        double best[kBlocks];
 #pragma unroll
-        for (int i = 0; i < kBlocks; ++i) best[i] = -(double)INFINITY;
-        for (int h = 0; h < p.group; h += kHeads) {
-            double up[kHeads][N], down[kHeads][N];        // q+, q-
-#pragma unroll
-            for (int y = 0; y < kHeads; ++y) {
-                float f[N];
-                // (an odd group's last head twice)
-                widen<E>(*(const u32x4*)(q + min(h + y, p.group - 1) * (D * (int)sizeof(E)) + (has ? lane : 0) * 16), f);
-#pragma unroll
-                for (int d = 0; d < N; ++d) {
-                    up[y][d] = !has ? 0.0 : f[d] > 0.f || f[d] != f[d] ? (double)f[d] : 0.0;
-                    down[y][d] = has && f[d] < 0.f ? (double)f[d] : 0.0;      // (-q-)
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kBlocks; ++i) {
-                float l[N], u[N];
-                widen<E>(lo[i], l);
-                widen<E>(hi[i], u);
-                double s[kHeads];
-#pragma unroll
-                for (int y = 0; y < kHeads; ++y) s[y] = 0.0;
-#pragma unroll
-                for (int d = 0; d < N; ++d)
-#pragma unroll
-                    for (int y = 0; y < kHeads; ++y) s[y] = fma(down[y][d], (double)l[d], fma(up[y][d], (double)u[d], s[y]));
-#pragma unroll
-                for (int y = 0; y < kHeads; ++y) {
-                    const double all = sum_of_lanes<X::L>(s[y]);
-                    best[i] = all > best[i] ? all : best[i];
-                }
-            }
+    for (int off = 32; off; off >>= 1) {
+        least = fminf(least, __shfl_xor(least, off));
+        most = fmaxf(most, __shfl_xor(most, off));
+        error = fmaxf(error, __shfl_xor(error, off));
+    }
+    if (lane == 0) {
+        s_stat[0][wave] = least;
+        s_stat[1][wave] = most;
+        s_stat[2][wave] = error;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < WAVES; ++w) {
+            least = fminf(least, s_stat[0][w]);
+            most = fmaxf(most, s_stat[1][w]);
+            error = fmaxf(error, s_stat[2][w]);
         }
-        if (lane == X::L - 1) {
-            float* out = p.scores + ((size_t)(er.first + t) * p.c.n_heads + head) * p.most;
-#pragma unroll
-            for (int i = 0; i < kBlocks; ++i) {
-                const int b = b0 + i * GROUPS + g;
-                if (b < m.n) out[b] = (float)best[i];
-            }
-        }
+        p.stats[((size_t)e * p.c.n_heads + head) * p.parts + blockIdx.x] = make_float4(least, most, error, 0.f);
     }
 }
 
 // ---- the choice: grid (rows of an entry, key/value heads, entries) ------------------------------------------------------------
-// The n_select largest of a row's scores, equal ones in order: a radix selection of their keys, 11, 11 and 10 bits, and
-// a pass that writes the chosen ones in order.
+// One histogram of the fp32 scores finds the range that the border lies in.  What lies above it by more than three times the
+// error is chosen, what lies below it by as much is not, and the few between are scored again in fp64 (unless all of them
+// are wanted) and ranked, equal ones by number.  Where that leaves more than kNear, or no error bound is known (queries that are
+// not finite, scores beyond fp32), all are scored in fp64 and selected by the digits of their keys.
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);
     return u ^ ((int32_t)u < 0 ? 0xffffffffu : 0x80000000u);
@@ -256,13 +329,87 @@ __device__ __forceinline__ int block_before(int x, int* waves, int* total) {
     *total = all;
     return before;
 }
-constexpr int kDigits = 2048;
-constexpr int kItems = 8;                 // neighbouring scores of a thread in the last pass
+// A block's score in fp64, rounded once, by a wavefront.
+template <typename E>
+__device__ __forceinline__ float exact_score(const ChoiceParams& p, const int32_t* table, const char* q, int head, int b) {
+    const int lane = threadIdx.x & 63, dims = p.c.pieces * (16 / (int)sizeof(E));      // (at most 128)
+    const char* at = bounds_of(p, table, head, b);
+    const auto number = [](const char* from, int i) {
+        if constexpr (sizeof(E) == 4) return ((const float*)from)[i];
+        else return __uint_as_float((uint32_t)((const uint16_t*)from)[i] << 16);
+    };
+    float lo[2], hi[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int d = min(lane + 64 * i, dims - 1);
+        lo[i] = number(at, d);
+        hi[i] = number(at, dims + d);
+    }
+    constexpr int HEADS = 4;
+    double best = -(double)INFINITY;
+    for (int h0 = 0; h0 < p.group; h0 += HEADS) {
+        float x[HEADS][2];
+#pragma unroll
+        for (int h = 0; h < HEADS; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) x[h][i] = lane + 64 * i < dims ? number(q, min(h0 + h, p.group - 1) * dims + lane + 64 * i) : 0.f;
+#pragma unroll
+        for (int h = 0; h < HEADS; ++h) {
+            double s = 0.0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) s += lane + 64 * i < dims ? (double)x[h][i] * (double)(x[h][i] > 0.f ? hi[i] : lo[i]) : 0.0;
+            s = wave_sum(s);
+            best = s > best ? s : best;                   // (a sum that is NaN is none)
+        }
+    }
+    return (float)best;
+}
+
+constexpr int kDigits = 1024;
+constexpr int kItems = 16;                // neighbouring scores of a thread
+constexpr int kNear = 128;
+// kItems scores from i0 on, of n (a row of scores is whole 16 bytes)
+__device__ __forceinline__ void load_scores(const float* scores, int i0, int n, float (&x)[kItems]) {
+#pragma unroll
+    for (int i = 0; i < kItems; i += 4) {
+        const f32x4 y = i0 + i < n ? *(const f32x4*)(scores + i0 + i) : f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[i + k] = y[k];
+    }
+}
+struct ChoiceShared {
+    int hist[kDigits];
+    int waves[kThreads / 64];
+    float stat[3][kThreads / 64];
+    int digit, before;
+    int n_near, n_sure;
+    int near[kNear];
+    float near_score[kNear];
+    int near_taken[kNear];
+};
+// the first place in hist, from `n` of them, at which their running sum comes to `need`: s.digit, and the sum in front of it s.before
+__device__ __forceinline__ void first_to(ChoiceShared& s, int n, int need) {
+    const int per = n / kThreads, tid = threadIdx.x;
+    int mine = 0, total, each[kDigits / kThreads];
+#pragma unroll
+    for (int i = 0; i < kDigits / kThreads; ++i) mine += each[i] = i < per ? s.hist[tid * per + i] : 0;
+    int before = block_before(mine, s.waves, &total);
+    if (before < need && before + mine >= need)
+#pragma unroll
+        for (int i = 0; i < kDigits / kThreads; ++i) {
+            const int x = each[i];
+            if (before < need && before + x >= need) {
+                s.digit = tid * per + i;
+                s.before = before;
+            }
+            before += x;
+        }
+    __syncthreads();
+}
+template <typename E>
 __global__ void __launch_bounds__(kThreads) block_choice_kernel(const ChoiceParams p) {
-    __shared__ int s_hist[kDigits];
-    __shared__ int s_waves[kThreads / 64];
-    __shared__ int s_digit, s_left;
-    const int e = blockIdx.z, head = blockIdx.y, tid = threadIdx.x;
+    __shared__ ChoiceShared s;
+    const int e = blockIdx.z, head = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
     const EntryRows er = entry_rows(p.b, e);
     if ((int)blockIdx.x >= er.rows) return;
     const size_t row = (size_t)(er.first + blockIdx.x) * p.c.n_heads + head;
@@ -273,62 +420,151 @@ __global__ void __launch_bounds__(kThreads) block_choice_kernel(const ChoicePara
         for (int i = tid; i < p.n_select; i += kThreads) out[i] = i < m.n ? m.first + i : -1;
         return;
     }
-    const float* scores = p.scores + row * p.most;
-    // the key that the last chosen one has, and how many of those that have it
-    uint32_t prefix = 0;
-    int left = p.n_select;
-    for (int shift = 21; shift >= 0; shift -= shift == 21 ? 11 : 10) {
-        const int bits = shift == 0 ? 10 : 11, digits = 1 << bits;
-        for (int i = tid; i < digits; i += kThreads) s_hist[i] = 0;
-        __syncthreads();
-        for (int i = tid; i < m.n; i += kThreads) {
-            const uint32_t k = key_of(scores[i]);
-            if ((uint64_t)(k ^ prefix) >> (shift + bits) == 0) atomicAdd(&s_hist[k >> shift & (digits - 1)], 1);
+    float* scores = p.scores + row * p.most;
+    const int32_t* table = p.c.table + (size_t)seq * p.c.max_pages;
+    const char* q = p.q + (int64_t)(er.first + blockIdx.x) * p.q_stride + (int64_t)head * p.group * p.c.pieces * 16;
+
+    float least = INFINITY, most = -INFINITY, error = 0.f;
+    const float4* stats = p.stats + ((size_t)e * p.c.n_heads + head) * p.parts;
+    for (int c = tid; c < p.parts && (int64_t)c * kChunk < m.n; c += kThreads) {
+        const float4 x = stats[c];
+        least = fminf(least, x.x);
+        most = fmaxf(most, x.y);
+        error = fmaxf(error, x.z);
+    }
+#pragma unroll
+    for (int off = 32; off; off >>= 1) {
+        least = fminf(least, __shfl_xor(least, off));
+        most = fmaxf(most, __shfl_xor(most, off));
+        error = fmaxf(error, __shfl_xor(error, off));
+    }
+    if (lane == 0) {
+        s.stat[0][tid >> 6] = least;
+        s.stat[1][tid >> 6] = most;
+        s.stat[2][tid >> 6] = error;
+    }
+    for (int i = tid; i < kDigits; i += kThreads) s.hist[i] = 0;
+    if (tid == 0) s.n_near = s.n_sure = 0;
+    __syncthreads();
+    for (int w = 0; w < kThreads / 64; ++w) {
+        least = fminf(least, s.stat[0][w]);
+        most = fmaxf(most, s.stat[1][w]);
+        error = fmaxf(error, s.stat[2][w]);
+    }
+    const float span = most - least;
+    bool known = error <= FLT_MAX && span <= FLT_MAX && span >= 0.f;
+    float above = 0.f, under = 0.f;                       // chosen: above `above`; not chosen: below `under`
+    int need = 0;                                         // of those between
+    if (known) {
+        // ranges from the largest score down
+        const float per = span > 0.f ? (kDigits - 1) / span : 0.f, width = span / (kDigits - 1);
+        known = per <= FLT_MAX;
+        for (int i0 = tid * kItems; i0 < m.n; i0 += kThreads * kItems) {
+            float x[kItems];
+            load_scores(scores, i0, m.n, x);
+#pragma unroll
+            for (int i = 0; i < kItems; ++i)
+                if (i0 + i < m.n) atomicAdd(&s.hist[min(kDigits - 1, (int)((most - x[i]) * per))], 1);
         }
         __syncthreads();
-        // from the largest digit down: the one in which `left` are reached
-        const int per = digits / kThreads;
-        int mine = 0, total;
-        for (int i = 0; i < per; ++i) mine += s_hist[digits - 1 - (tid * per + i)];
-        int before = block_before(mine, s_waves, &total);
-        if (before < left && before + mine >= left)
-            for (int i = 0; i < per; ++i) {
-                const int d = digits - 1 - (tid * per + i), n = s_hist[d];
-                if (before < left && before + n >= left) {
-                    s_digit = d;
-                    s_left = left - before;
-                }
-                before += n;
+        first_to(s, kDigits, p.n_select);
+        // (the range's limits, and what rounding leaves of them)
+        const float slack = 3.f * error + span * 0x1p-18f;
+        above = most - (float)s.digit * width + slack;
+        under = most - (float)(s.digit + 1) * width - slack;
+        int sure = 0;
+        for (int i0 = tid * kItems; i0 < m.n; i0 += kThreads * kItems) {
+            float x[kItems];
+            load_scores(scores, i0, m.n, x);
+#pragma unroll
+            for (int i = 0; i < kItems; ++i) {
+                if (i0 + i >= m.n) continue;
+                sure += x[i] > above;
+                if (x[i] > above || x[i] < under) continue;
+                const int at = atomicAdd(&s.n_near, 1);
+                if (at < kNear) s.near[at] = i0 + i;
             }
+        }
+#pragma unroll
+        for (int off = 32; off; off >>= 1) sure += __shfl_xor(sure, off);
+        if (lane == 0 && sure) atomicAdd(&s.n_sure, sure);
         __syncthreads();
-        prefix |= (uint32_t)s_digit << shift;
-        left = s_left;
+        need = p.n_select - s.n_sure;
+        if (s.n_near > kNear && s.n_near != need) known = false;
+    }
+    const int near = s.n_near;
+    if (known && near != need) {
+        for (int i = tid >> 6; i < near; i += kThreads / 64) {
+            const float x = exact_score<E>(p, table, q, head, m.first + s.near[i]);
+            if (lane == 0) s.near_score[i] = x;
+        }
+        __syncthreads();
+        if (tid < near) {
+            const uint32_t mine = key_of(s.near_score[tid]);
+            int ahead = 0;
+            for (int i = 0; i < near; ++i) {
+                const uint32_t k = key_of(s.near_score[i]);
+                ahead += k > mine || (k == mine && s.near[i] < s.near[tid]);
+            }
+            s.near_taken[tid] = ahead < need;
+        }
         __syncthreads();
     }
+    uint32_t prefix = 0;
+    int left = p.n_select;
+    if (!known) {
+        // all of them in fp64; the key that the last chosen one has, and how many of those that have it
+        for (int i = tid >> 6; i < m.n; i += kThreads / 64) {
+            const float x = exact_score<E>(p, table, q, head, m.first + i);
+            if (lane == 0) scores[i] = x;
+        }
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            constexpr int bits = 8, digits = 1 << bits;
+            __syncthreads();
+            for (int i = tid; i < digits; i += kThreads) s.hist[i] = 0;
+            __syncthreads();
+            for (int i = tid; i < m.n; i += kThreads) {
+                const uint32_t k = key_of(scores[i]);
+                if ((uint64_t)(k ^ prefix) >> (shift + bits) == 0) atomicAdd(&s.hist[digits - 1 - (k >> shift & (digits - 1))], 1);
+            }
+            __syncthreads();
+            first_to(s, digits, left);                    // from the largest digit down
+            prefix |= (uint32_t)(digits - 1 - s.digit) << shift;
+            left -= s.before;
+        }
+    }
+    // the chosen ones, in order
     int given = 0, ties = 0;
     for (int i0 = 0; i0 < m.n; i0 += kThreads * kItems) {
-        uint32_t k[kItems];
-        int more = 0, same = 0;
+        uint32_t take = 0, tie = 0;
+        float x[kItems];
+        load_scores(scores, i0 + tid * kItems, m.n, x);
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
             const int at = i0 + tid * kItems + i;
-            k[i] = at < m.n ? key_of(scores[at]) : 0;
-            more += at < m.n && k[i] > prefix;
-            same += at < m.n && k[i] == prefix;
+            if (at >= m.n) continue;
+            if (!known) {
+                const uint32_t k = key_of(x[i]);
+                take |= k > prefix ? 1u << i : 0u;
+                tie |= k == prefix ? 1u << i : 0u;
+            } else if (x[i] > above) {
+                take |= 1u << i;
+            } else if (x[i] >= under) {
+                bool in = near == need;
+                for (int y = 0; !in && y < near; ++y) in = s.near[y] == at && s.near_taken[y];
+                take |= in ? 1u << i : 0u;
+            }
         }
-        int all_more, all_same;
-        const int more_before = block_before(more, s_waves, &all_more);
-        const int same_before = ties + block_before(same, s_waves, &all_same);
-        // of the ties in front of this thread's, `left` at most were taken
-        int to = given + more_before + min(same_before, left) - min(ties, left), tie = same_before;
-#pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-            const int at = i0 + tid * kItems + i;
-            if (at >= m.n || k[i] < prefix) continue;
-            if (k[i] > prefix || tie++ < left) out[to++] = m.first + at;
+        int all, same;
+        if (!known) {                                     // (uniform)
+            int before = ties + block_before(__popc(tie), s.waves, &same);
+            for (uint32_t rest = tie; rest; rest &= rest - 1)
+                if (before++ < left) take |= rest & -rest;
+            ties += same;
         }
-        given += all_more + min(ties + all_same, left) - min(ties, left);
-        ties += all_same;
+        int to = given + block_before(__popc(take), s.waves, &all);
+        for (uint32_t rest = take; rest; rest &= rest - 1) out[to++] = m.first + i0 + tid * kItems + __ffs((int)rest) - 1;
+        given += all;
     }
 }
 
@@ -627,18 +863,28 @@ size_t layer_bounds(const dip_kv_cache* c, int32_t block) {
     return (size_t)c->n_pages * c->n_kv_heads * (c->page_size / block) * 2 * c->head_dim * elem_bytes(c->dtype);
 }
 // most blocks that a row may choose from
-int64_t most_blocks(const dip_kv_cache* c, const dip_batch* b, int32_t block) { return reach(c, b) / block; }
+int64_t most_blocks(const dip_kv_cache* c, const dip_batch* b, int32_t block) { return (reach(c, b) / block + 3) / 4 * 4; }
 
 template <typename E>
-hipError_t launch_scores(const ChoiceParams& p, int head_dim, int n_batch, hipStream_t stream) {
-    const auto go = [&](auto dim) {
-        constexpr int D = decltype(dim)::value, CHUNK = kThreads / Lanes<E, D>::L * kBlocks;
-        return launch_timed(block_scores_kernel<E, D>, dim3((p.most + CHUNK - 1) / CHUNK, p.c.n_heads, n_batch), dim3(kThreads), stream,
-                            DIP_KERNEL_BLOCKS, p);
+hipError_t launch_choice(const ChoiceParams& p, int head_dim, int n_batch, hipStream_t stream) {
+    const auto scores = [&](auto dim) {
+        return launch_timed(block_scores_kernel<E, decltype(dim)::value>, dim3(p.parts, p.c.n_heads, n_batch), dim3(kThreads), stream, DIP_KERNEL_BLOCKS, p);
     };
-    if (head_dim == 64) return go(std::integral_constant<int, 64>());
-    if (head_dim == 96) return go(std::integral_constant<int, 96>());
-    return go(std::integral_constant<int, 128>());
+    if (p.most > p.n_select) {
+        const hipError_t err = head_dim == 64 ? scores(std::integral_constant<int, 64>()) : head_dim == 96 ? scores(std::integral_constant<int, 96>())
+                                                                                                 : scores(std::integral_constant<int, 128>());
+        if (err != hipSuccess) return err;
+    }
+    return launch_timed(block_choice_kernel<E>, dim3(p.b.max_rows, p.c.n_heads, n_batch), dim3(kThreads), stream, DIP_KERNEL_BLOCKS, p);
+}
+// Workgroups of block_scores_kernel that share an entry and head: about kScoreGrid in all
+constexpr int kScoreGrid = 1280;
+int parts_of(const dip_kv_cache* c, const dip_batch* b, int32_t block) {
+    const int64_t chunks = (most_blocks(c, b, block) + kChunk - 1) / kChunk, fair = kScoreGrid / ((int64_t)c->n_kv_heads * b->n_batch);
+    return (int)std::max<int64_t>(1, std::min(chunks, fair));
+}
+size_t score_bytes(const dip_kv_cache* c, const dip_batch* b, int32_t block) {
+    return align_up((size_t)b->n_rows * c->n_kv_heads * most_blocks(c, b, block) * sizeof(float), 256);
 }
 
 struct AttnPlan {
@@ -733,7 +979,7 @@ int32_t dip_kv_block_bounds(const dip_kv_cache* cache, int32_t layer, int32_t n_
 
 size_t dip_select_blocks_workspace_bytes(const dip_kv_cache* cache, const dip_batch* batch, int32_t n_q_heads, int32_t block) {
     if (check_rows(cache, batch, n_q_heads, block)) return 0;
-    const size_t n = (size_t)batch->n_rows * cache->n_kv_heads * most_blocks(cache, batch, block) * sizeof(float);
+    const size_t n = score_bytes(cache, batch, block) + (size_t)batch->n_batch * cache->n_kv_heads * parts_of(cache, batch, block) * sizeof(float4);
     return n < 256 ? 256 : align_up(n, 256);
 }
 
@@ -756,7 +1002,9 @@ int32_t dip_select_blocks(const dip_kv_cache* cache, int32_t layer, const dip_ba
     p.q_stride = q_stride * elem_bytes(cache->dtype);
     p.bounds = (const char*)bounds + layer_bounds(cache, block) * layer;
     p.scores = (float*)ws;
+    p.stats = (float4*)((char*)ws + score_bytes(cache, batch, block));
     p.out = blocks;
+    p.parts = parts_of(cache, batch, block);
     p.most = (int)most_blocks(cache, batch, block);
     p.group = n_q_heads / cache->n_kv_heads;
     p.block_shift = log2_of(block);
@@ -764,14 +1012,9 @@ int32_t dip_select_blocks(const dip_kv_cache* cache, int32_t layer, const dip_ba
     p.sinks = sinks;
     p.recent = recent;
     p.max_len = reach(cache, batch);
-    if (p.most > n_select) {
-        st = check_hip(cache->dtype == DIP_F32 ? launch_scores<float>(p, cache->head_dim, batch->n_batch, (hipStream_t)stream)
-                                               : launch_scores<uint16_t>(p, cache->head_dim, batch->n_batch, (hipStream_t)stream),
-                       "block_scores launch");
-        if (st) return st;
-    }
-    return check_hip(launch_timed(block_choice_kernel, dim3(p.b.max_rows, cache->n_kv_heads, batch->n_batch), dim3(kThreads),
-                                  (hipStream_t)stream, DIP_KERNEL_BLOCKS, p), "block_choice launch");
+    return check_hip(cache->dtype == DIP_F32 ? launch_choice<float>(p, cache->head_dim, batch->n_batch, (hipStream_t)stream)
+                                             : launch_choice<uint16_t>(p, cache->head_dim, batch->n_batch, (hipStream_t)stream),
+                     "select_blocks launch");
 }
 
 size_t dip_block_attention_workspace_bytes(const dip_kv_cache* cache, const dip_batch* batch, int32_t n_q_heads, int32_t block,
