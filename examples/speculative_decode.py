@@ -1,17 +1,18 @@
 #!/usr/bin/env python3
 """Speculative decoding with pruned layers, end to end: a small random-weight decoder whose MLPs run as
-DIP batches, whose attention reads a paged cache with a sliding window and sinks, and whose drafts are trees
-that are verified against its own probabilities.
+DIP batches, whose attention reads a paged cache with a sliding window and sinks, or blocks of it that every row
+chooses for itself, and whose drafts are trees that are verified against its own probabilities.
 
-    python examples/speculative_decode.py [--tokens N] [--greedy] [--branches 2]
+    python examples/speculative_decode.py [--tokens N] [--greedy] [--branches 2] [--blocks 8]
 
 One step of the loop, for all sequences together:
     draft     a tree per sequence, at most 8 nodes of both together -- what dip_swiglu_mlp_forward_batched takes
     reserve   room for the nodes in the cache                     dip_kv_reserve
-    layers    append keys and values, attend, MLP                 dip_kv_append, dip_tree_attention,
-                                                                  dip_swiglu_mlp_forward_batched
-    verify    which nodes stand, and the next token               dip_verify_tree
-    compact   keep their rows, give back the rest                 dip_kv_compact
+    layers    append keys and values, turned to their positions,  dip_kv_append_rotary,
+              attend, MLP                                         dip_tree_attention (or dip_select_blocks and
+                                                                  dip_block_attention), dip_swiglu_mlp_forward_batched
+    verify    the probabilities, which nodes stand, next token    dip_sample, dip_verify_tree
+    compact   keep their rows, give back the rest                 dip_kv_compact (and dip_kv_block_bounds)
 The projections are torch products: the library has none.
 """
 import argparse
@@ -40,12 +41,13 @@ class Decoder:
     """Pre-norm decoder layers in fp32 with a bf16 or fp32 cache; d_model is heads * head_dim."""
 
     def __init__(self, layers=2, heads=8, kv_heads=2, head_dim=64, d_ff=1536, vocab=512, keep=0.5, window=64, sinks=4,
-                 dtype=torch.bfloat16, n_seqs=2, max_tokens=512, page=16, seed=0):
+                 dtype=torch.bfloat16, n_seqs=2, max_tokens=512, page=16, seed=0, blocks=0, recent=32):
         g = torch.Generator(device="cuda").manual_seed(seed)
         d = heads * head_dim
         normal = lambda *s, scale=1.0: torch.randn(s, generator=g, device="cuda") * scale
         self.heads, self.kv_heads, self.dim, self.d, self.vocab = heads, kv_heads, head_dim, d, vocab
         self.window, self.sinks, self.dtype = window, sinks, dtype
+        self.blocks, self.recent, self.page = blocks, recent, page     # blocks: pages that a row chooses (0: the window)
         self.k_in, self.k_mid = max(1, int(keep * d)), max(1, int(keep * d_ff))
         self.emb = normal(vocab, d)
         # what a token leads to on its own: a fixed successor, more or less
@@ -58,6 +60,8 @@ class Decoder:
         kv = lambda: torch.empty(layers, pages, kv_heads, page, head_dim, dtype=dtype, device="cuda")
         self.cache = D.KvCache(kv(), kv(), ints([[0] * (max_tokens // page)] * n_seqs), ints([0] * n_seqs), ints([0] * pages))
         D.dip_kv_init(self.cache)
+        self.rot = D.Rotary(D.dip_rotary_frequencies(head_dim).cuda(), D.DIP_ROTARY_HALF)
+        self.bounds = torch.zeros(layers, pages, kv_heads, 1, 2, head_dim, dtype=dtype, device="cuda")
         self.seqs, self.lens = ints(list(range(n_seqs))), [0] * n_seqs
         self.mlp_ws = workspace(max(D.dip_swiglu_mlp_forward_batched_workspace_bytes(self.mlps[0], b, self.k_in, self.k_mid)
                                     for b in range(1, ROWS + 1)))
@@ -79,14 +83,22 @@ class Decoder:
         n, hd = batch.n_rows, self.heads * self.dim
         x = self.emb[tokens.long()]
         norm = lambda y: torch.nn.functional.rms_norm(y, (self.d,))
-        ws = workspace(D.dip_attention_workspace_bytes(self.cache, batch, self.heads, self.window, self.sinks))
+        if self.blocks:
+            ws = workspace(max(D.dip_select_blocks_workspace_bytes(self.cache, batch, self.heads, self.page),
+                               D.dip_block_attention_workspace_bytes(self.cache, batch, self.heads, self.page, self.blocks, self.sinks,
+                                                                     self.recent)))
+            chosen = torch.empty(n, self.kv_heads, self.blocks, dtype=torch.int32, device="cuda")
+        else:
+            ws = workspace(D.dip_attention_workspace_bytes(self.cache, batch, self.heads, self.window, self.sinks))
         for layer, (w_qkv, w_o, mlp) in enumerate(zip(self.qkv, self.proj, self.mlps)):
             fused = (norm(x) @ w_qkv).to(self.dtype)         # q, k and v side by side: the calls take strided rows
-            q = fused[:, :hd].unflatten(1, (self.heads, self.dim))
             k, v = fused[:, hd:].unflatten(1, (2, self.kv_heads, self.dim)).unbind(1)
-            D.dip_kv_append(self.cache, layer, batch, k, v)
-            a = torch.empty(n, self.heads, self.dim, dtype=self.dtype, device="cuda")
-            if parents is None:
+            q, a = (torch.empty(n, self.heads, self.dim, dtype=self.dtype, device="cuda") for _ in range(2))
+            D.dip_kv_append_rotary(self.cache, layer, batch, parents, self.rot, fused[:, :hd].unflatten(1, (self.heads, self.dim)), q, k, v)
+            if self.blocks:
+                D.dip_select_blocks(self.cache, layer, batch, q, self.bounds, self.sinks, self.recent, chosen, ws)
+                D.dip_block_attention(self.cache, layer, batch, parents, chosen, self.page, q, self.dim ** -0.5, self.sinks, self.recent, a, ws)
+            elif parents is None:
                 D.dip_window_attention(self.cache, layer, batch, q, self.dim ** -0.5, self.window, self.sinks, a, ws)
             else:
                 D.dip_tree_attention(self.cache, layer, batch, parents, q, self.dim ** -0.5, self.window, self.sinks, a, ws)
@@ -99,15 +111,25 @@ class Decoder:
             x = x + y
         return norm(x) @ self.unemb.t() * (9.0 / self.d)
 
+    def commit(self, batch, path=None, keep=None):
+        """Keep rows of a step, and work out the bounds of the pages that they filled."""
+        D.dip_kv_compact(self.cache, batch, path, keep)
+        if self.blocks:
+            D.dip_kv_block_bounds(self.cache, 0, len(self.mlps), self.seqs, batch.c.max_rows, self.bounds)
+
     def draft_logits(self, token):
         """The drafter: the model without its layers."""
         return torch.nn.functional.rms_norm(self.emb[token], (self.d,)) @ self.unemb.t() * (9.0 / self.d)
 
 
-def probabilities(logits, greedy):
-    if greedy:
-        return torch.nn.functional.one_hot(logits.argmax(-1), logits.shape[-1]).float()
-    return torch.softmax(logits, -1)
+def probabilities(logits, greedy, top_p=0.95):
+    """What tokens are drawn from, for the target and the drafter alike."""
+    rows = logits.view(-1, logits.shape[-1])
+    probs = torch.empty_like(rows)
+    each = lambda x: torch.full((len(rows),), x, device="cuda")
+    D.dip_sample(rows, None, None, probs, workspace(D.dip_sample_workspace_bytes(*rows.shape)), temperature=each(0.0 if greedy else 1.0),
+                 top_p=each(top_p))
+    return probs.view_as(logits)
 
 
 def generate(model, prompts, n_tokens, nodes=4, branches=1, greedy=False, seed=0):
@@ -122,7 +144,7 @@ def generate(model, prompts, n_tokens, nodes=4, branches=1, greedy=False, seed=0
     batch = model.batch(rows)
     model.reserve(batch)
     model.forward(batch, ints([t for p in prompts for t in p[:-1]]))
-    D.dip_kv_compact(model.cache, batch, None, None)
+    model.commit(batch)
     model.lens = [n + r for n, r in zip(model.lens, rows)]
     out, steps = [list(p) for p in prompts], 0
     parents = [-1] + [(t - 1) // branches for t in range(1, nodes)]
@@ -146,7 +168,7 @@ def generate(model, prompts, n_tokens, nodes=4, branches=1, greedy=False, seed=0
         kids = max(1, branches)
         ws = workspace(D.dip_verify_tree_workspace_bytes(batch, model.vocab, kids))
         D.dip_verify_tree(batch, tok, par, p, torch.stack(q), uniform(B * nodes), uniform(B), kids, keep, path, token, ws)
-        D.dip_kv_compact(model.cache, batch, path, keep)
+        model.commit(batch, path, keep)
         steps += 1
         for i, (n, x) in enumerate(zip(keep.tolist(), token.tolist())):
             out[i] += [tokens[i * nodes + t] for t in path[i * nodes + 1:i * nodes + n].tolist()] + [x]
@@ -160,10 +182,11 @@ def main():
     ap.add_argument("--nodes", type=int, default=4)
     ap.add_argument("--branches", type=int, default=1)
     ap.add_argument("--greedy", action="store_true")
+    ap.add_argument("--blocks", type=int, default=0, help="pages that a row chooses, in place of the window")
     a = ap.parse_args()
     prompts = [[1, 2, 3, 4, 5, 6, 7], [100, 90, 80]]
-    one, one_steps = generate(Decoder(), prompts, a.tokens, nodes=1, greedy=a.greedy)
-    out, steps = generate(Decoder(), prompts, a.tokens, a.nodes, a.branches, a.greedy)
+    one, one_steps = generate(Decoder(blocks=a.blocks), prompts, a.tokens, nodes=1, greedy=a.greedy)
+    out, steps = generate(Decoder(blocks=a.blocks), prompts, a.tokens, a.nodes, a.branches, a.greedy)
     made = sum(len(o) for o in out) - sum(len(p) for p in prompts)
     print(f"{made} tokens in {steps} steps of {len(prompts)} x {a.nodes} rows: {made / steps / len(prompts):.2f} tokens a step "
           f"and sequence (one token at a time: {one_steps} steps)")

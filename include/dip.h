@@ -667,6 +667,8 @@ int32_t dip_select_blocks(const dip_kv_cache* cache, int32_t layer, const dip_ba
  * Attention over what the blocks leave: arguments, softmax, rounding and what is not finite as in dip_window_attention (parents
  * NULL) or dip_tree_attention.  blocks: as dip_select_blocks writes them, or of the caller's own making: ascending, unused
  * entries, -1, at the end; an entry outside [front, tail) or not above the one before it is passed over.
+ * Every row reads its own blocks: meant for single tokens, trees and a few rows; the many rows of a prompt share what they
+ * read in dip_window_attention.
  */
 size_t dip_block_attention_workspace_bytes(const dip_kv_cache* cache, const dip_batch* batch, int32_t n_q_heads, int32_t block,
                                            int32_t n_select, int32_t sinks, int32_t recent);

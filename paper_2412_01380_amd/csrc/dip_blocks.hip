@@ -513,8 +513,9 @@ __global__ void __launch_bounds__(kThreads) block_choice_kernel(const ChoicePara
     uint32_t prefix = 0;
     int left = p.n_select;
     if (!known) {
-        // all of them in fp64; the key that the last chosen one has, and how many of those that have it
-        for (int i = tid >> 6; i < m.n; i += kThreads / 64) {
+        // all of them in fp64, unless no product was anything but zero (queries of zeros: every score is, to the letter); the
+        // key that the last chosen one has, and how many of those that have it
+        for (int i = error == 0.f ? m.n : tid >> 6; i < m.n; i += kThreads / 64) {
             const float x = exact_score<E>(p, table, q, head, m.first + i);
             if (lane == 0) scores[i] = x;
         }

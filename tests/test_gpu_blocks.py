@@ -303,3 +303,34 @@ def test_the_same_bits_every_time_and_in_graphs(dtype):
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(out, want) and torch.equal(blocks, want_blocks)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_closer_than_fp32_tells(dtype):
+    # blocks whose scores differ by less than fp32 sums do: the order of the 64-bit sums decides
+    s = Long(dtype, [3200], [3], 4, 2, 128, 16, 16, wide=1.0)
+    base = s.cache.k[s.layer, int(s.table[s.seqs[0], 0])].clone()
+    g = torch.Generator().manual_seed(1)
+    for j in range(200):
+        page = base.clone()
+        at = torch.randint(0, 128, (4,), generator=g).cuda()
+        page[..., at] *= 1 + (0.0078125 if dtype == "bf16" else 2.0 ** -20) * (j % 7)
+        s.cache.k[s.layer, int(s.table[s.seqs[0], j])] = page
+        s.k[0][j * 16:(j + 1) * 16] = page.transpose(0, 1).double().cpu().numpy()
+    s.q[1] *= 1e-3
+    s.q64 = s.q.double().numpy()
+    s.update()
+    for n_select in (1, 13, 50, 128, 199):
+        assert (s.select(n_select, 0, 0).cpu().numpy() == s.want_choice(n_select, 0, 0)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_blocks(dtype):
+    # more than a workgroup holds at a time, and rows of very different sizes beside each other
+    s = Long(dtype, [80000], [2], 2, 1, 64, 16, 16, seed=4)
+    s.q[0] *= 1e4
+    s.q64 = s.q.double().numpy()
+    s.update()
+    for n_select in (1, 700, 4096):
+        blocks = s.select(n_select, 5, 1000)
+        assert (blocks.cpu().numpy() == s.want_choice(n_select, 5, 1000)).all()
