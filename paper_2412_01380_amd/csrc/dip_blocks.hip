@@ -305,24 +305,27 @@ __global__ void __launch_bounds__(kThreads, sizeof(E) == 2 ? 4 : 3) block_scores
 // error is chosen, what lies below it by as much is not, and the few between are scored again in fp64 (unless all of them
 // are wanted) and ranked, equal ones by number.  Where that leaves more than kNear, or no error bound is known (queries that are
 // not finite, scores beyond fp32), all are scored in fp64 and selected by the digits of their keys.
+constexpr int kChoiceThreads = 512;
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);
     return u ^ ((int32_t)u < 0 ? 0xffffffffu : 0x80000000u);
 }
 __device__ __forceinline__ int block_before(int x, int* waves, int* total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane >> 4;
+    // in data-parallel moves within rows of 16 lanes, then the rows' sums by scalar
     int upto = x;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int y = __shfl_up(upto, off);
-        if (lane >= off) upto += y;
-    }
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x111, 0xf, 0xf, true);      // row_shr 1, 2, 4, 8
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x112, 0xf, 0xf, true);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x114, 0xf, 0xf, true);
+    upto += __builtin_amdgcn_update_dpp(0, upto, 0x118, 0xf, 0xf, true);
+    const int a = __builtin_amdgcn_readlane(upto, 15), b = __builtin_amdgcn_readlane(upto, 31), c = __builtin_amdgcn_readlane(upto, 47);
+    upto += (row > 0 ? a : 0) + (row > 1 ? b : 0) + (row > 2 ? c : 0);
     __syncthreads();
     if (lane == 63) waves[wave] = upto;
     __syncthreads();
     int before = upto - x, all = 0;
 #pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) {
+    for (int w = 0; w < kChoiceThreads / 64; ++w) {
         if (w < wave) before += waves[w];
         all += waves[w];
     }
@@ -366,7 +369,7 @@ __device__ __forceinline__ float exact_score(const ChoiceParams& p, const int32_
 }
 
 constexpr int kDigits = 1024;
-constexpr int kItems = 16;                // neighbouring scores of a thread
+constexpr int kItems = 4;                 // neighbouring scores of a thread
 constexpr int kNear = 128;
 // kItems scores from i0 on, of n (a row of scores is whole 16 bytes)
 __device__ __forceinline__ void load_scores(const float* scores, int i0, int n, float (&x)[kItems]) {
@@ -379,8 +382,8 @@ __device__ __forceinline__ void load_scores(const float* scores, int i0, int n, 
 }
 struct ChoiceShared {
     int hist[kDigits];
-    int waves[kThreads / 64];
-    float stat[3][kThreads / 64];
+    int waves[kChoiceThreads / 64];
+    float stat[3][kChoiceThreads / 64];
     int digit, before;
     int n_near, n_sure;
     int near[kNear];
@@ -389,14 +392,14 @@ struct ChoiceShared {
 };
 // the first place in hist, from `n` of them, at which their running sum comes to `need`: s.digit, and the sum in front of it s.before
 __device__ __forceinline__ void first_to(ChoiceShared& s, int n, int need) {
-    const int per = n / kThreads, tid = threadIdx.x;
-    int mine = 0, total, each[kDigits / kThreads];
+    const int per = n >= kChoiceThreads ? n / kChoiceThreads : (int)threadIdx.x < n, tid = threadIdx.x;
+    int mine = 0, total, each[kDigits / kChoiceThreads];
 #pragma unroll
-    for (int i = 0; i < kDigits / kThreads; ++i) mine += each[i] = i < per ? s.hist[tid * per + i] : 0;
+    for (int i = 0; i < kDigits / kChoiceThreads; ++i) mine += each[i] = i < per ? s.hist[tid * per + i] : 0;
     int before = block_before(mine, s.waves, &total);
     if (before < need && before + mine >= need)
 #pragma unroll
-        for (int i = 0; i < kDigits / kThreads; ++i) {
+        for (int i = 0; i < kDigits / kChoiceThreads; ++i) {
             const int x = each[i];
             if (before < need && before + x >= need) {
                 s.digit = tid * per + i;
@@ -407,7 +410,7 @@ __device__ __forceinline__ void first_to(ChoiceShared& s, int n, int need) {
     __syncthreads();
 }
 template <typename E>
-__global__ void __launch_bounds__(kThreads) block_choice_kernel(const ChoiceParams p) {
+__global__ void __launch_bounds__(kChoiceThreads) block_choice_kernel(const ChoiceParams p) {
     __shared__ ChoiceShared s;
     const int e = blockIdx.z, head = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
     const EntryRows er = entry_rows(p.b, e);
@@ -417,20 +420,24 @@ __global__ void __launch_bounds__(kThreads) block_choice_kernel(const ChoicePara
     const int seq = entry_seq(p.b, p.c, e);
     const Middle m = seq >= 0 ? middle_of(p, entry_len(p.c, seq)) : Middle{0, 0};
     if (m.n <= p.n_select) {
-        for (int i = tid; i < p.n_select; i += kThreads) out[i] = i < m.n ? m.first + i : -1;
+        for (int i = tid; i < p.n_select; i += kChoiceThreads) out[i] = i < m.n ? m.first + i : -1;
         return;
     }
     float* scores = p.scores + row * p.most;
     const int32_t* table = p.c.table + (size_t)seq * p.c.max_pages;
     const char* q = p.q + (int64_t)(er.first + blockIdx.x) * p.q_stride + (int64_t)head * p.group * p.c.pieces * 16;
 
+    // up to kChoiceThreads * kItems scores stay in registers
+    const bool one = m.n <= kChoiceThreads * kItems;
+    float x[kItems];
+    if (one) load_scores(scores, tid * kItems, m.n, x);
     float least = INFINITY, most = -INFINITY, error = 0.f;
     const float4* stats = p.stats + ((size_t)e * p.c.n_heads + head) * p.parts;
-    for (int c = tid; c < p.parts && (int64_t)c * kChunk < m.n; c += kThreads) {
-        const float4 x = stats[c];
-        least = fminf(least, x.x);
-        most = fmaxf(most, x.y);
-        error = fmaxf(error, x.z);
+    for (int c = tid; c < p.parts && (int64_t)c * kChunk < m.n; c += kChoiceThreads) {
+        const float4 y = stats[c];
+        least = fminf(least, y.x);
+        most = fmaxf(most, y.y);
+        error = fmaxf(error, y.z);
     }
 #pragma unroll
     for (int off = 32; off; off >>= 1) {
@@ -443,10 +450,10 @@ __global__ void __launch_bounds__(kThreads) block_choice_kernel(const ChoicePara
         s.stat[1][tid >> 6] = most;
         s.stat[2][tid >> 6] = error;
     }
-    for (int i = tid; i < kDigits; i += kThreads) s.hist[i] = 0;
+    for (int i = tid; i < kDigits; i += kChoiceThreads) s.hist[i] = 0;
     if (tid == 0) s.n_near = s.n_sure = 0;
     __syncthreads();
-    for (int w = 0; w < kThreads / 64; ++w) {
+    for (int w = 0; w < kChoiceThreads / 64; ++w) {
         least = fminf(least, s.stat[0][w]);
         most = fmaxf(most, s.stat[1][w]);
         error = fmaxf(error, s.stat[2][w]);
@@ -459,9 +466,8 @@ __global__ void __launch_bounds__(kThreads) block_choice_kernel(const ChoicePara
         // ranges from the largest score down
         const float per = span > 0.f ? (kDigits - 1) / span : 0.f, width = span / (kDigits - 1);
         known = per <= FLT_MAX;
-        for (int i0 = tid * kItems; i0 < m.n; i0 += kThreads * kItems) {
-            float x[kItems];
-            load_scores(scores, i0, m.n, x);
+        for (int i0 = tid * kItems; i0 < m.n; i0 += kChoiceThreads * kItems) {
+            if (!one) load_scores(scores, i0, m.n, x);
 #pragma unroll
             for (int i = 0; i < kItems; ++i)
                 if (i0 + i < m.n) atomicAdd(&s.hist[min(kDigits - 1, (int)((most - x[i]) * per))], 1);
@@ -473,9 +479,8 @@ __global__ void __launch_bounds__(kThreads) block_choice_kernel(const ChoicePara
         above = most - (float)s.digit * width + slack;
         under = most - (float)(s.digit + 1) * width - slack;
         int sure = 0;
-        for (int i0 = tid * kItems; i0 < m.n; i0 += kThreads * kItems) {
-            float x[kItems];
-            load_scores(scores, i0, m.n, x);
+        for (int i0 = tid * kItems; i0 < m.n; i0 += kChoiceThreads * kItems) {
+            if (!one) load_scores(scores, i0, m.n, x);
 #pragma unroll
             for (int i = 0; i < kItems; ++i) {
                 if (i0 + i >= m.n) continue;
@@ -494,9 +499,9 @@ __global__ void __launch_bounds__(kThreads) block_choice_kernel(const ChoicePara
     }
     const int near = s.n_near;
     if (known && near != need) {
-        for (int i = tid >> 6; i < near; i += kThreads / 64) {
-            const float x = exact_score<E>(p, table, q, head, m.first + s.near[i]);
-            if (lane == 0) s.near_score[i] = x;
+        for (int i = tid >> 6; i < near; i += kChoiceThreads / 64) {
+            const float y = exact_score<E>(p, table, q, head, m.first + s.near[i]);
+            if (lane == 0) s.near_score[i] = y;
         }
         __syncthreads();
         if (tid < near) {
@@ -515,16 +520,16 @@ __global__ void __launch_bounds__(kThreads) block_choice_kernel(const ChoicePara
     if (!known) {
         // all of them in fp64, unless no product was anything but zero (queries of zeros: every score is, to the letter); the
         // key that the last chosen one has, and how many of those that have it
-        for (int i = error == 0.f ? m.n : tid >> 6; i < m.n; i += kThreads / 64) {
-            const float x = exact_score<E>(p, table, q, head, m.first + i);
-            if (lane == 0) scores[i] = x;
+        for (int i = error == 0.f ? m.n : tid >> 6; i < m.n; i += kChoiceThreads / 64) {
+            const float y = exact_score<E>(p, table, q, head, m.first + i);
+            if (lane == 0) scores[i] = y;
         }
         for (int shift = 24; shift >= 0; shift -= 8) {
             constexpr int bits = 8, digits = 1 << bits;
             __syncthreads();
-            for (int i = tid; i < digits; i += kThreads) s.hist[i] = 0;
+            for (int i = tid; i < digits; i += kChoiceThreads) s.hist[i] = 0;
             __syncthreads();
-            for (int i = tid; i < m.n; i += kThreads) {
+            for (int i = tid; i < m.n; i += kChoiceThreads) {
                 const uint32_t k = key_of(scores[i]);
                 if ((uint64_t)(k ^ prefix) >> (shift + bits) == 0) atomicAdd(&s.hist[digits - 1 - (k >> shift & (digits - 1))], 1);
             }
@@ -536,10 +541,9 @@ __global__ void __launch_bounds__(kThreads) block_choice_kernel(const ChoicePara
     }
     // the chosen ones, in order
     int given = 0, ties = 0;
-    for (int i0 = 0; i0 < m.n; i0 += kThreads * kItems) {
+    for (int i0 = 0; i0 < m.n; i0 += kChoiceThreads * kItems) {
         uint32_t take = 0, tie = 0;
-        float x[kItems];
-        load_scores(scores, i0 + tid * kItems, m.n, x);
+        if (!one || !known) load_scores(scores, i0 + tid * kItems, m.n, x);
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
             const int at = i0 + tid * kItems + i;
@@ -876,7 +880,7 @@ hipError_t launch_choice(const ChoiceParams& p, int head_dim, int n_batch, hipSt
                                                                                                  : scores(std::integral_constant<int, 128>());
         if (err != hipSuccess) return err;
     }
-    return launch_timed(block_choice_kernel<E>, dim3(p.b.max_rows, p.c.n_heads, n_batch), dim3(kThreads), stream, DIP_KERNEL_BLOCKS, p);
+    return launch_timed(block_choice_kernel<E>, dim3(p.b.max_rows, p.c.n_heads, n_batch), dim3(kChoiceThreads), stream, DIP_KERNEL_BLOCKS, p);
 }
 // Workgroups of block_scores_kernel that share an entry and head: about kScoreGrid in all
 constexpr int kScoreGrid = 1280;
@@ -993,7 +997,7 @@ int32_t dip_select_blocks(const dip_kv_cache* cache, int32_t layer, const dip_ba
     if (st) return st;
     if (!bounds || !blocks) return fail(DIP_ERR_INVALID_ARG, "select_blocks: null pointer");
     if (!aligned16(bounds)) return fail(DIP_ERR_UNSUPPORTED, "select_blocks: bounds must be 16-byte aligned");
-    if (rows_bound(batch) >= 1 << 24) return fail(DIP_ERR_UNSUPPORTED, "select_blocks: too many rows for one call");
+    if (rows_bound(batch) >= 1 << 23) return fail(DIP_ERR_UNSUPPORTED, "select_blocks: too many rows for one call");
     st = validate_ws(ws, ws_bytes, dip_select_blocks_workspace_bytes(cache, batch, n_q_heads, block));
     if (st) return st;
     ChoiceParams p;
