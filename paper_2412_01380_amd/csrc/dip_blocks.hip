@@ -311,15 +311,7 @@ __device__ __forceinline__ uint32_t key_of(float x) {
     return u ^ ((int32_t)u < 0 ? 0xffffffffu : 0x80000000u);
 }
 __device__ __forceinline__ int block_before(int x, int* waves, int* total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane >> 4;
-    // in data-parallel moves within rows of 16 lanes, then the rows' sums by scalar
-    int upto = x;
-    upto += __builtin_amdgcn_update_dpp(0, upto, 0x111, 0xf, 0xf, true);      // row_shr 1, 2, 4, 8
-    upto += __builtin_amdgcn_update_dpp(0, upto, 0x112, 0xf, 0xf, true);
-    upto += __builtin_amdgcn_update_dpp(0, upto, 0x114, 0xf, 0xf, true);
-    upto += __builtin_amdgcn_update_dpp(0, upto, 0x118, 0xf, 0xf, true);
-    const int a = __builtin_amdgcn_readlane(upto, 15), b = __builtin_amdgcn_readlane(upto, 31), c = __builtin_amdgcn_readlane(upto, 47);
-    upto += (row > 0 ? a : 0) + (row > 1 ? b : 0) + (row > 2 ? c : 0);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, upto = running(x);
     __syncthreads();
     if (lane == 63) waves[wave] = upto;
     __syncthreads();

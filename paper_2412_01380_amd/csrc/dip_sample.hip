@@ -18,6 +18,7 @@
 
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 
 #include "dip_vocab_device.h"
 
@@ -172,10 +173,14 @@ template <int THREADS, typename T>
 __device__ __forceinline__ T block_before(T x, T* waves, T* total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     T upto = x;
+    if constexpr (std::is_same<T, uint64_t>::value) {
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const T y = __shfl_up(upto, off);
-        if (lane >= off) upto += y;
+        for (int off = 1; off < 64; off <<= 1) {
+            const T y = __shfl_up(upto, off);
+            if (lane >= off) upto += y;
+        }
+    } else {
+        upto = running(x);
     }
     __syncthreads();
     if (lane == 63) waves[wave] = upto;

@@ -43,7 +43,7 @@ __device__ __forceinline__ void load_entries(const char* row, int x, int end, fl
     }
 }
 
-// inclusive running sum over a wavefront: data-parallel moves within rows of 16 lanes, then the rows' sums by scalar
+// inclusive running sums over a wavefront: data-parallel moves within rows of 16 lanes, then the rows' sums by scalar
 template <int CTRL>
 __device__ __forceinline__ double moved(double x) {
     const uint64_t b = __double_as_longlong(x);
@@ -68,6 +68,16 @@ __device__ __forceinline__ double running(double x) {
     const int row = (threadIdx.x & 63) >> 4;
     return x + (row == 0 ? 0.0 : row == 1 ? a : row == 2 ? a + b : a + b + c);
 }
+__device__ __forceinline__ int running(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    const int a = __builtin_amdgcn_readlane(x, 15), b = __builtin_amdgcn_readlane(x, 31), c = __builtin_amdgcn_readlane(x, 47);
+    const int row = (threadIdx.x & 63) >> 4;
+    return x + (row > 0 ? a : 0) + (row > 1 ? b : 0) + (row > 2 ? c : 0);
+}
+__device__ __forceinline__ uint32_t running(uint32_t x) { return (uint32_t)running((int)x); }
 __device__ __forceinline__ double wave_sum(double x) {
     x = in_rows(x);
     return of_lane(x, 15) + of_lane(x, 31) + of_lane(x, 47) + of_lane(x, 63);
