@@ -47,7 +47,8 @@ __device__ __forceinline__ void widen(u32x4 x, float (&f)[16 / sizeof(E)]) {
 }
 
 // ---- bounds: grid (pages of a sequence, sequences, layers) ------------------------------------------------------------
-// A thread takes 16 bytes of a head's channels through a block's slots, kFlight of them on their way at a time.
+// A thread takes 16 bytes of a head's channels through a block's slots, kFlight of them on their way at a time.  Bound by bytes: 98304
+// positions of 10 heads of 128 dims, bf16, two layers, 535 MB read and written in 80 us, which a plain read takes too.
 constexpr int kFlight = 8;
 struct BoundsParams {
     KvView c;                 // k at the first layer
@@ -118,6 +119,7 @@ __global__ void __launch_bounds__(kThreads) block_bounds_kernel(const BoundsPara
 // 32: 92 MB).  In fp64 without the matrix cores it took 44 us, and 24 for trees.
 // The same sums with |hi| + |lo| and |q|, T, bound what rounding does to a score: half of its products are zero, the others are D
 // roundings of 2^-23 T at most, in whatever order they are added up.  The choice settles in fp64 what lies nearer to its border than that.
+// 25 us at 3.7 TB/s; a workgroup per 64 blocks, which has to look up entry, length, pages and queries for 32 KB of bounds, took 36.
 struct ChoiceParams {
     KvView c;
     BatchView b;
@@ -305,6 +307,8 @@ __global__ void __launch_bounds__(kThreads, sizeof(E) == 2 ? 4 : 3) block_scores
 // error is chosen, what lies below it by as much is not, and the few between are scored again in fp64 (unless all of them
 // are wanted) and ranked, equal ones by number.  Where that leaves more than kNear, or no error bound is known (queries that are
 // not finite, scores beyond fp32), all are scored in fp64 and selected by the digits of their keys.
+// Bound by latency, a chain of loads, barriers and LDS: 16 tokens of 10 heads, up to 2030 blocks, 11.6 us, two tokens 8.3 (256 threads
+// 17.4 and 10.6, 1024 threads 13.3 and 9.1, and 17.2 instead of 11.4 for three trees of 32 heads).
 constexpr int kChoiceThreads = 512;
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);
@@ -569,7 +573,9 @@ __global__ void __launch_bounds__(kChoiceThreads) block_choice_kernel(const Choi
 // A unit is a row, a key/value head, up to 16 query heads of its group and a share of what the row reads, which comes
 // in cells of 16 positions: those in front, those of the chosen blocks, those behind.  A cell lies within a page, so that it
 // has one address; a tile of a product is two cells (bf16) or one (fp32), wherever they lie.  Each wavefront streams tiles of
-// its own through LDS, as in attn_rows_kernel.
+// its own through LDS, as in attn_rows_kernel.  Bound by reading what was chosen: 16 tokens of 40 heads on 10, bf16, 64 blocks of 32
+// and 512 recent positions of up to 64k, 213 MB in 43 us (33 at the rate of a large read, 6.42 TB/s); three trees of up to 7 nodes, 32
+// heads, 96 dims, fp32, 24 blocks of 32, 343 MB in 81 us (53); two tokens 10 us, latency.
 struct BlockAttnParams {
     attn::AttnParams a;       // window, sinks 0
     const int32_t* blocks;    // [row][head][n_select]
@@ -901,7 +907,8 @@ AttnPlan plan_attention(const dip_kv_cache* c, const dip_batch* b, int n_q_heads
     read += std::min((int64_t)recent + c->page_size + block + rows_bound(b), all);
     const int64_t tiles = std::max<int64_t>(1, (std::min(read, all) + keys - 1) / keys + 2);
     const int64_t slots = 256 * ((160 * 1024 - 1024) / (pl.waves * 256 * c->head_dim + 6144));
-    // one round of workgroups; a share has two tiles for each wavefront at least
+    // one round of workgroups; a share has two tiles for each wavefront at least (two rounds: 49.7 instead of 43.9 us for 16
+    // tokens over up to 64k positions, 95 instead of 80 for three trees in fp32)
     const int64_t shares = std::max<int64_t>(1, std::min(slots / pl.units, tiles / (2 * pl.waves)));
     pl.share_tiles = (int)((tiles + shares - 1) / shares);
     pl.shares = (int)((tiles + pl.share_tiles - 1) / pl.share_tiles);

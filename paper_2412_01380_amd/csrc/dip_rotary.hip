@@ -4,6 +4,11 @@
 // is worked out in fp64, in turns, and reduced to the nearest half turn there: an fp32 product is off by 2^-24 of the
 // angle, 0.06 at a million radians.  What is left fits fp32, and so do sine, cosine and the turned pair, which is
 // rounded once.  Sines and cosines are worked out once for a row and pair, into LDS, whatever the number of heads.
+//
+// Bound by bytes, every element read and written once: 8192 rows of 40 heads of 128 dims, half of them turned, 168 MB in 39.9 us
+// (34.7 at the rate of a large copy, 4.83 TB/s); 7095 rows of two prompts, 40 query heads and 10 for keys and values, 218 MB in 50.6
+// us (45).  Few rows by latency: 7 rows 7.1 us, three trees of 7 nodes into the cache 9.4, of which a launch takes 4.4; hence
+// fewer rows to a workgroup then.
 
 #include <cmath>
 

@@ -25,10 +25,14 @@
 namespace dip {
 namespace {
 
+// Where the time goes: 512 rows of 128256, fp32, with probabilities, 277 us: chunks 70 (263 MB; the integer places and the histogram
+// take longer than the read, 41), rows 15, list 50, cut 28, probabilities 120 (525 MB).  64 rows in bf16 49 us, a row of 32064 35 us: five
+// launches in a chain, the cut the longest of them (14 to 21 us of loads, barriers and sums that wait for one another).
+//
 constexpr int kThreads = 256;             // of the kernels over chunks
 constexpr int kRowThreads = 512;          // of the kernels that have a workgroup per row
 constexpr int kTile = kThreads * kPer;
-constexpr int kMaxTiles = 2;              // of a chunk, in registers
+constexpr int kMaxTiles = 2;              // of a chunk, in registers (four: chunks 76 us, cut 35 of 512 rows of 128256)
 constexpr int kMaxChunks = (1 << 24) / (kMaxTiles * kTile);
 constexpr int kBins = 512;                // the last one: all that lies 64 nats and more below the maximum
 constexpr int kRest = kBins - 1;
