@@ -390,7 +390,7 @@ __device__ __forceinline__ uint32_t least_key(double rate, double top, int bins)
     for (int shift = 26;; shift -= 6) {   // ... and less than from + 64 << shift
         shift = max(shift, 0);
         const uint64_t key = (uint64_t)from + ((uint64_t)lane << shift);
-        const bool in = key > 0xff7fffffull || below(of_key((uint32_t)key), rate, top) >> kPlaceBits < (uint32_t)bins;
+        const bool in = key > 0xff7fffffull || top - place(of_key((uint32_t)key), rate) < bins * 0x1p23;
         const uint64_t mask = __ballot(in);
         const int first = mask ? __ffsll((unsigned long long)mask) - 1 : 64;
         if (shift == 0) return first ? from + first : from;
@@ -942,7 +942,7 @@ __global__ void __launch_bounds__(kThreads) sample_probs_kernel(const SamplePara
     }
     if (state == kEmpty) kept = 0;
     if (__any(kept != 0)) {
-        const Place first = place_of(rp->best, rate, top);
+        const Place first = greedy ? Place{0, 1u << 30} : place_of(rp->best, rate, top);
         const float each = (float)(greedy ? 1.0 : (double)first.weight * (first.bin ? 0.88249690258459540286 : 1.0) * 0x1p-30 / rp->total);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {

@@ -214,3 +214,31 @@ def test_draws_follow_the_probabilities():
     token, probs = run(x.expand(n, 300).contiguous(), u, torch.float32, dict(top_p=floats([0.95] * n)))
     counts = torch.bincount(token.long(), minlength=300).double() / n
     assert (counts - probs[0].double()).abs().max() <= 1.0 / n + 1e-6
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_rows_of_any_settings(dtype):
+    g = torch.Generator().manual_seed(14)
+    n, v = 1500, 257
+    x = torch.randn(n, v, generator=g) * torch.exp(3 * torch.rand(n, 1, generator=g))
+    x[::3] = (2 * x[::3]).round() / 2                          # a third of the rows full of ties
+    x[torch.rand(n, v, generator=g) < 0.3 * torch.rand(n, 1, generator=g)] = -math.inf
+    x[7::50, 3] = math.inf
+    x = x.to(DT[dtype]).cuda()
+    some = lambda lo, hi: lo + (hi - lo) * torch.rand(n, generator=g)
+    how = dict(temperature=some(-0.1, 2.0), top_k=(some(0, 1) ** 2 * 300).int() - 20, top_p=some(0.0, 1.2), min_p=some(-0.1, 0.3) ** 3)
+    how = {k: t.cuda() for k, t in how.items()}
+    u = torch.rand(n, generator=g).cuda()
+    token, probs = run(x, u, torch.float32, how)
+    check(x, u, token, probs, how)
+    for left in ("top_k", "top_p", "min_p"):
+        part = {k: t for k, t in how.items() if k != left}
+        token, probs = run(x, u, torch.float32, part)
+        check(x, u, token, probs, part)
+
+
+def test_rows_as_many_as_there_may_be():
+    x, u = logits(65535, 40, "bf16", 15)
+    token, probs = run(x, u, torch.bfloat16, dict(top_k=ints([3] * 65535)))
+    some = list(range(0, 65535, 997)) + [65534]
+    check(x[some], u[some], token[some], probs[some], dict(top_k=ints([3] * len(some))))
