@@ -25,14 +25,14 @@
 namespace dip {
 namespace {
 
-// Where the time goes: 512 rows of 128256, fp32, with probabilities, 277 us: chunks 70 (263 MB; the integer places and the histogram
-// take longer than the read, 41), rows 15, list 50, cut 28, probabilities 120 (525 MB).  64 rows in bf16 49 us, a row of 32064 35 us: five
+// Where the time goes: 512 rows of 128256, fp32, with probabilities, 223 us: chunks 57 (263 MB; the integer places and the histogram
+// take longer than the read, 41), rows 14, list 43, cut 27, probabilities 81 (525 MB).  64 rows in bf16 49 us, a row of 32064 35 us: five
 // launches in a chain, the cut the longest of them (14 to 21 us of loads, barriers and sums that wait for one another).
 //
 constexpr int kThreads = 256;             // of the kernels over chunks
 constexpr int kRowThreads = 512;          // of the kernels that have a workgroup per row
 constexpr int kTile = kThreads * kPer;
-constexpr int kMaxTiles = 2;              // of a chunk, in registers (four: chunks 76 us, cut 35 of 512 rows of 128256)
+constexpr int kMaxTiles = 2;              // of a chunk, in registers (four: chunks 76 instead of 70 us, cut 35 instead of 29 of 512 rows of 128256)
 constexpr int kMaxChunks = (1 << 24) / (kMaxTiles * kTile);
 constexpr int kBins = 512;                // the last one: all that lies 64 nats and more below the maximum
 constexpr int kRest = kBins - 1;
@@ -161,6 +161,8 @@ __device__ __forceinline__ How how_of(const SampleParams& p, int row) {
     return h;
 }
 
+__device__ __forceinline__ float widened(float x) { return x; }
+__device__ __forceinline__ float widened(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 // kPer words from x on, -inf from `end` on and in place of NaN
 template <typename E>
 __device__ __forceinline__ void load_logits(const char* row, int x, int end, float (&f)[kPer]) {
@@ -921,59 +923,75 @@ __global__ void __launch_bounds__(kRowThreads) sample_cut_kernel(const SamplePar
 }
 
 // ---- probabilities: grid (tiles, rows) ----------------------------------------------------------------------------
+// Four neighbouring words of a thread at a time, so that a wavefront writes one run of whole lines, past the caches: what they hold of
+// the logits is worth more.  (Sixteen of a thread, through the caches: 120 instead of 81 us for 512 rows of 128256 in fp32, and the next
+// call's chunks and list 70 and 50 instead of 57 and 43.  Read four at a time, these two take 62 and 47.)
 template <typename E, typename O>
 __global__ void __launch_bounds__(kThreads) sample_probs_kernel(const SampleParams p) {
-    const int row = blockIdx.y;
+    constexpr int N = 4, GROUPS = kTile / (N * kThreads);
+    typedef E In __attribute__((ext_vector_type(N), aligned(sizeof(E))));
+    typedef O Out __attribute__((ext_vector_type(N), aligned(sizeof(O))));
+    const int row = blockIdx.y, x0 = blockIdx.x * kTile + threadIdx.x * N;
+    const char* logits = p.logits + row * p.stride;
+    float f[GROUPS][N];
+#pragma unroll
+    for (int j = 0; j < GROUPS; ++j) {
+        const int x = x0 + j * (N * kThreads);
+        if (x + N <= p.n_vocab) {
+            const In v = *(const In*)(logits + (size_t)x * sizeof(E));
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[j][i] = widened(v[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) f[j][i] = x + i < p.n_vocab ? entry_at<E>(logits, x + i) : -INFINITY;
+        }
+    }
     const Row* rp = p.rows + row;
     const int state = rp->state, at = rp->at;
     const bool greedy = rp->greedy;
-    const uint32_t key = rp->key;
+    const float cut = of_key(rp->key);
     // weights relative to the largest logit's: differences of logits are exact, of 8 l / T they are not where T is next to nothing
     const double top = rp->top, rate = rp->rate, best = (double)rp->best, step = rate * (0x1p-26 * 1.44269504088896340736);
-    const int x = (blockIdx.x * kThreads + threadIdx.x) * kPer;
-    if (x >= p.n_vocab) return;
-    float f[kPer];
-    load_logits<E>(p.logits + row * p.stride, x, p.n_vocab, f);
-    uint32_t kept = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const uint32_t k = key_of(f[i]);
-        kept |= f[i] > -INFINITY && (k > key || (k == key && x + i <= at)) ? 1u << i : 0u;
+    float each = 0.f;
+    if (state != kEmpty && !greedy) {
+        const Place first = place_of(rp->best, rate, top);
+        each = (float)((double)first.weight * (first.bin ? 0.88249690258459540286 : 1.0) * 0x1p-30 / rp->total);
     }
-    if (state == kEmpty) kept = 0;
-    if (__any(kept != 0)) {
-        const Place first = greedy ? Place{0, 1u << 30} : place_of(rp->best, rate, top);
-        const float each = (float)(greedy ? 1.0 : (double)first.weight * (first.bin ? 0.88249690258459540286 : 1.0) * 0x1p-30 / rp->total);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            float y;
-            if (greedy) y = 1.f;
-            else if (top == (double)INFINITY) y = f[i] == INFINITY ? each : 0.f;
-            else {                        // 2^(whole + part)
-                const double z = ((double)f[i] - best) * step, whole = floor(fmax(z, -400.0));
-                y = ldexpf(__builtin_amdgcn_exp2f((float)(z - whole)) * each, (int)whole);
+    for (int j = 0; j < GROUPS; ++j) {
+        const int x = x0 + j * (N * kThreads);
+        if (x >= p.n_vocab) break;
+        bool kept[N], any = false;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {                     // (a NaN is neither above the cut nor at it)
+            kept[i] = state != kEmpty && f[j][i] > -INFINITY && (f[j][i] > cut || (f[j][i] == cut && x + i <= at));
+            any |= kept[i];
+        }
+        float y[N] = {0.f, 0.f, 0.f, 0.f};
+        if (__any(any)) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                float w;
+                if (greedy) w = 1.f;
+                else if (top == (double)INFINITY) w = f[j][i] == INFINITY ? each : 0.f;
+                else {                                    // 2^(whole + part)
+                    const double z = ((double)f[j][i] - best) * step, whole = floor(fmax(z, -400.0));
+                    w = ldexpf(__builtin_amdgcn_exp2f((float)(z - whole)) * each, (int)whole);
+                }
+                y[i] = kept[i] ? w : 0.f;
             }
-            f[i] = kept >> i & 1 ? y : 0.f;
         }
-    } else {
+        O* out = (O*)(p.probs + row * p.probs_stride) + x;
+        if (x + N <= p.n_vocab) {
+            Out a;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) f[i] = 0.f;
-    }
-    struct __attribute__((packed, aligned(sizeof(O)))) Any { O w[16 / sizeof(O)]; };
-    O* out = (O*)(p.probs + row * p.probs_stride) + x;
-    constexpr int N = 16 / sizeof(O);
-    if (x + kPer <= p.n_vocab) {
+            for (int i = 0; i < N; ++i) a[i] = (O)y[i];
+            __builtin_nontemporal_store(a, (Out*)out);
+        } else {
 #pragma unroll
-        for (int y = 0; y < kPer / N; ++y) {
-            Any a;
-#pragma unroll
-            for (int i = 0; i < N; ++i) a.w[i] = (O)f[y * N + i];
-            *(Any*)(out + y * N) = a;
+            for (int i = 0; i < N; ++i)
+                if (x + i < p.n_vocab) out[i] = (O)y[i];
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (x + i < p.n_vocab) out[i] = (O)f[i];
     }
 }
 
