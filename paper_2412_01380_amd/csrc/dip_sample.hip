@@ -678,6 +678,15 @@ __device__ __forceinline__ void each_word(const SampleParams& p, const Listed& l
         }
     }
 }
+// add(n) by the active lanes: those that agree with the first of them in `at` and `key` leave it to that one, n of them together.
+// (A wavefront's atomics on one LDS word take their turns: rows of 128256 equal logits 935 us one by one, 494 so.)
+template <typename F>
+__device__ __forceinline__ void add_alike(uint32_t at, uint32_t key, F add) {
+    const bool alike = at == (uint32_t)__builtin_amdgcn_readfirstlane((int)at) && key == (uint32_t)__builtin_amdgcn_readfirstlane((int)key);
+    const uint64_t mask = __ballot(alike);
+    if (!alike) add(1u);
+    else if ((int)(threadIdx.x & 63) == __ffsll((unsigned long long)mask) - 1) add((uint32_t)__popcll(mask));
+}
 // A listed word's weight as an integer, in units of exp(-lo / 8) 2^-38: 2^24 of them fit 64 bits.
 __device__ __forceinline__ uint64_t fixed_weight(const Listed& l, const Cut& s, uint32_t key) {
     const Place pl = place_of(of_key(key), l.rate, l.top);
@@ -698,7 +707,7 @@ __device__ __forceinline__ int nth(const SampleParams& p, const Listed& l, uint3
         each_word<E>(p, l, [&](uint32_t k, int number) {
             const uint32_t at = ((uint32_t)number - lo) >> shift;
             if (k < least || k > most || (uint32_t)number < lo || at >= kRanges) return;
-            atomicAdd(&s.range.count[at], 1u);
+            add_alike(at, 0, [&](uint32_t n) { atomicAdd(&s.range.count[at], n); });
             s.key = k;
         });
         __syncthreads();
@@ -748,8 +757,11 @@ __device__ __forceinline__ void find(const SampleParams& p, const Listed& l, uin
         each_word<E>(p, l, [&](uint32_t k, int number) {
             if (k < least || k > most || ends(k, number)) return;
             const uint32_t at = (most - k) >> shift;
-            atomicAdd(&s.range.count[at], 1u);
-            atomicAdd(&s.range.weight[at], (unsigned long long)fixed_weight(l, s, k));
+            const uint64_t w = fixed_weight(l, s, k);
+            add_alike(at, k, [&](uint32_t n) {
+                atomicAdd(&s.range.count[at], n);
+                atomicAdd(&s.range.weight[at], (unsigned long long)(w * n));
+            });
         });
         __syncthreads();
         uint32_t c_mine = 0, c_all;
@@ -909,7 +921,10 @@ __global__ void __launch_bounds__(kRowThreads) sample_cut_kernel(const SamplePar
     for (int c = tid; c < p.chunks; c += kRowThreads) s.fixed[c] = 0;
     __syncthreads();
     each_word<E>(p, l, [&](uint32_t k, int number) {
-        if (k > key || (k == key && number <= at)) atomicAdd(&s.fixed[number / p.chunk], (unsigned long long)fixed_weight(l, s, k));
+        if (k < key || (k == key && number > at)) return;
+        const uint32_t c = (uint32_t)number / (uint32_t)p.chunk;
+        const uint64_t w = fixed_weight(l, s, k);
+        add_alike(c, k, [&](uint32_t n) { atomicAdd(&s.fixed[c], (unsigned long long)(w * n)); });
     });
     __syncthreads();
     for (int c = tid; c < p.chunks; c += kRowThreads) s.d.chunk[c] += (double)s.fixed[c] * unit;
