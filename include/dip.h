@@ -666,7 +666,8 @@ int32_t dip_select_blocks(const dip_kv_cache* cache, int32_t layer, const dip_ba
 /*
  * Attention over what the blocks leave: arguments, softmax, rounding and what is not finite as in dip_window_attention (parents
  * NULL) or dip_tree_attention.  blocks: as dip_select_blocks writes them, or of the caller's own making: ascending, unused
- * entries, -1, at the end; an entry outside [front, tail) or not above the one before it is passed over.
+ * entries, -1, at the end; an entry outside [front, tail) or not above the one before it is passed over, and all others are read.
+ * (So a list that is not ascending may read a block more than once: 5, 3, 5 reads block 5 twice.)
  * Every row reads its own blocks: meant for single tokens, trees and a few rows; the many rows of a prompt share what they
  * read in dip_window_attention.
  */
