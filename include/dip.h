@@ -716,7 +716,8 @@ int32_t dip_verify_tree(const dip_batch* batch, const int32_t* tokens, const int
  * the first word alone.  A logit of -inf is never kept, NaN counts as -inf; +inf outweighs all that is finite, and several
  * share alike.  A row of nothing but -inf gives -1 and zeros.
  * Weights are accurate to 2^-26 + 2^-50 |l / temperature| and summed in integers or fp64, so that results do not hang on the
- * order of sums (bit-repeatable).
+ * order of sums (bit-repeatable).  A word whose l / temperature is 63.75 or more below the first's, its weight 2^-91 and less, may
+ * count for nothing in the sums; it is not drawn then, whatever u, but keeps its probability.
  *   logits   n_rows (at most 65535) rows of n_vocab (at most 2^24), DIP_F32 or DIP_BF16, `stride` elements apart
  *   how      host; per-row settings, device arrays of n_rows entries; a NULL array, or NULL for all: none of it (temperature 1)
  *   u        n_rows numbers in [0, 1); may be NULL if token is

@@ -450,7 +450,9 @@ __global__ void __launch_bounds__(kRowThreads) sample_row_kernel(const SamplePar
     for (int c = tid; c < p.chunks; c += kRowThreads) {
         const int off = bins_below(sums[c].top, top);
         s_below[c] = off;
-        s.chunk[c] = off == kRest || how.cuts ? 0.0 : sums[c].weight * (s.scale[off] * 0x1p30);
+        // (a chunk whose largest word is in the last bin of the row has nothing to draw, whatever it weighs beside that word)
+        const bool some = off < kRest && place_of(sums[c].best, how.rate, top).bin < kRest;
+        s.chunk[c] = !some || how.cuts ? 0.0 : sums[c].weight * (s.scale[off] * 0x1p30);
     }
     __syncthreads();
     if (!how.cuts) {
