@@ -8,12 +8,14 @@
 //   sample_row_kernel      a workgroup per row adds the histograms up and says which bins, and so which logits, the cut lies
 //                          in -- or, where no rule applies, draws
 //   sample_collect_kernel  the words with these logits (a few in a hundred) go into a list
-//   sample_cut_kernel      a workgroup per row narrows the cut down over the list, to a word, and draws
+//   sample_cut_kernel      a workgroup per row narrows the cut down over the list, to a word, and draws; one rule after the other, each
+//                          within the one bin that the running sums of the bins say
 //   sample_probs_kernel    the probabilities
 // A word's place is an integer: D = top - rint(8 2^23 l / T), in fp64, is how far below a grid line above the maximum it
 // lies, in units of 2^-23 of a bin.  Its bin is D >> 23, and its weight exp(-bin / 8) times a factor in (0.88, 1] that follows
 // from the other bits and is held in units of 2^-30.  So sums over a bin are integer sums, the same in any order, and 2^-26
-// accurate relative to the weight itself however small it is, and two chunks agree on every word's bin.  (Of an fp32 l / T 2^-24 is
+// accurate relative to the weight itself however small it is (but for the last bin's, 63.75 nats and more down, which counts for
+// nothing), and two chunks agree on every word's bin.  (Of an fp32 l / T 2^-24 is
 // lost, which at 30 nats is a weight off by 2 in 10^6.)
 
 #include <cfloat>
@@ -111,10 +113,13 @@ struct alignas(128) Row {
     int32_t at;
     int32_t state;
     int32_t greedy;
-    int32_t lo;               // the first bin that the cut may lie in, and the keys of these bins
+    int32_t lo;               // the first bin that the cut may lie in, and the keys of the bins that it may
     uint32_t least, most;
-    int32_t k;                // words up to top_k's cut, 0: no such rule
+    int32_t k;                // words up to top_k's cut, 0: no such rule; its bin, and words and weight in front of that
+    int32_t k_bin;
+    uint32_t k_count;
     int32_t by_part;          // top_p cuts
+    double k_weight;
     uint32_t min_key;         // min_p's cut, 0: no such rule
     int32_t listed;           // words with these keys: in the list, or too many for it
     uint32_t n;               // words in the list so far
@@ -136,6 +141,7 @@ struct SampleParams {
     Chunk* sums;              // [row][chunk]
     uint64_t* hist;           // [row][chunk][kBins]
     Row* rows;
+    double* bins;             // [row][kBins], of rows that top_p cuts: running weights of the bins
     uint64_t* list;           // [row][kList]: key, number
 };
 
@@ -557,6 +563,8 @@ __global__ void __launch_bounds__(kRowThreads) sample_row_kernel(const SamplePar
             } else if (lo == kRest) {
                 most = 0xff7fffffu;
             }
+            if (by_part)
+                for (int b = tid; b < kBins; b += 64) p.bins[(size_t)row * kBins + b] = s_weight[b];
             if (tid == 0) {
                 r->state = kCut;
                 r->part = (double)how.part;
@@ -564,6 +572,9 @@ __global__ void __launch_bounds__(kRowThreads) sample_row_kernel(const SamplePar
                 r->least = least;
                 r->most = most;
                 r->k = by_k ? how.k : 0;
+                r->k_bin = bin_k;
+                r->k_count = count_to(bin_k - 1);
+                r->k_weight = weight_to(bin_k - 1);
                 r->by_part = by_part;
                 r->min_key = min_key;
                 r->listed = (int)(count_to(hi) - count_to(lo - 1));
@@ -649,8 +660,19 @@ struct Listed {
     int row, n;
     bool listed;
     double rate, top;
-    int lo;
-    uint32_t least, most;
+    uint32_t least, most;     // keys of the list
+    int bin;                  // the one that is looked at, and keys that it lies between
+    uint32_t bin_least, bin_most;
+    __device__ __forceinline__ void look_at(int b) {
+        bin = b;
+        bin_least = least;
+        bin_most = most;
+        if (top == (double)INFINITY || rate == 0.0) return;
+        // its words' places, a unit and two keys to either side for what rounding may do
+        const double high = (top - (double)b * 0x1p23 + 1.0) / rate, low = (top - (double)(b + 1) * 0x1p23 - 1.0) / rate;
+        bin_most = max(least, min(most, key_of((float)high) + 2));
+        if (b < kRest) bin_least = min(most, max(least, key_of((float)low) - 2));
+    }
 };
 // f(key, number) of every word whose key lies among those that the cut may have, by the threads of a workgroup
 template <typename E, typename F>
@@ -689,10 +711,12 @@ __device__ __forceinline__ void add_alike(uint32_t at, uint32_t key, F add) {
     if (!alike) add(1u);
     else if ((int)(threadIdx.x & 63) == __ffsll((unsigned long long)mask) - 1) add((uint32_t)__popcll(mask));
 }
-// A listed word's weight as an integer, in units of exp(-lo / 8) 2^-38: 2^24 of them fit 64 bits.
-__device__ __forceinline__ uint64_t fixed_weight(const Listed& l, const Cut& s, uint32_t key) {
+// Whether a listed word lies in the bin that is looked at; its weight there, in units of the bin's: 2^24 of them fit 64 bits, and nothing is
+// lost.  (Weights of several bins in units of the first one's are a few units each where the others lie 20 nats below it.)
+__device__ __forceinline__ bool in_bin(const Listed& l, uint32_t key, uint32_t& weight) {
     const Place pl = place_of(of_key(key), l.rate, l.top);
-    return pl.bin == kRest ? 0 : (uint64_t)((double)pl.weight * (s.d.scale[max(pl.bin - l.lo, 0)] * 0x1p38) + 0.5);
+    weight = pl.bin == kRest ? 0 : pl.weight;
+    return pl.bin == l.bin;
 }
 
 // The number of the m-th word (from 1) of those with a key in [least, most], in order of their numbers; their key in s.key.
@@ -737,13 +761,13 @@ __device__ __forceinline__ int nth(const SampleParams& p, const Listed& l, uint3
     }
 }
 
-// The word at which the listed ones, in order, first come to `need` words or to `need` in weight: its key in s.key, its
+// The word at which the listed ones of the bin, in order, first come to `need` words or to `need` in weight: its key in s.key, its
 // number in s.at, and what all up to it weigh in s.weight.  Words behind (end_key, end_at) are not looked at.
 template <typename E, bool WEIGHT>
 __device__ __forceinline__ void find(const SampleParams& p, const Listed& l, uint32_t end_key, int end_at, double need, Cut& s) {
     const int tid = threadIdx.x, lane = tid & 63;
     constexpr int PER = kRanges / kRowThreads;
-    uint32_t least = end_key > l.least ? end_key : l.least, most = l.most, count = 0;
+    uint32_t least = max(end_key, l.bin_least), most = max(least, l.bin_most), count = 0;
     double weight = 0.0;
     auto ends = [&](uint32_t k, int number) { return k == end_key && number > end_at; };
     for (;;) {
@@ -759,10 +783,11 @@ __device__ __forceinline__ void find(const SampleParams& p, const Listed& l, uin
         each_word<E>(p, l, [&](uint32_t k, int number) {
             if (k < least || k > most || ends(k, number)) return;
             const uint32_t at = (most - k) >> shift;
-            const uint64_t w = fixed_weight(l, s, k);
+            uint32_t w;
+            if (!in_bin(l, k, w)) return;
             add_alike(at, k, [&](uint32_t n) {
                 atomicAdd(&s.range.count[at], n);
-                atomicAdd(&s.range.weight[at], (unsigned long long)(w * n));
+                atomicAdd(&s.range.weight[at], (unsigned long long)w * n);
             });
         });
         __syncthreads();
@@ -816,18 +841,19 @@ __device__ __forceinline__ void find(const SampleParams& p, const Listed& l, uin
         }
         if (here <= (uint32_t)kFew) {
             each_word<E>(p, l, [&](uint32_t k, int number) {
-                if (k < least || k > most || ends(k, number)) return;
+                uint32_t w;
+                if (k < least || k > most || ends(k, number) || !in_bin(l, k, w)) return;
                 s.few[atomicAdd(&s.n_few, 1u)] = ((uint64_t)k << 32) | (uint32_t)~number;
             });
             __syncthreads();
             if (tid < 64) {                               // every lane a word: what lies in front of it
                 const uint64_t mine = lane < (int)here ? s.few[lane] : 0;
-                const uint64_t w = lane < (int)here ? fixed_weight(l, s, (uint32_t)(mine >> 32)) : 0;
-                uint32_t c = 1;
+                uint32_t w = 0, c = 1;
+                if (lane < (int)here) in_bin(l, (uint32_t)(mine >> 32), w);
                 uint64_t upto = w;
                 for (int j = 0; j < (int)here; ++j) {
                     const uint64_t other = s.few[j];
-                    const uint64_t ow = __shfl((unsigned long long)w, j);
+                    const uint32_t ow = __shfl(w, j);
                     if (other > mine) {
                         ++c;
                         upto += ow;
@@ -874,43 +900,35 @@ __global__ void __launch_bounds__(kRowThreads) sample_cut_kernel(const SamplePar
     Row* rp = p.rows + row;
     if (rp->state != kCut) return;
     const Row r = *rp;
-    const Listed l = {row, min((int)r.n, kList), r.listed <= kList, r.rate, r.top, r.lo, r.least, r.most};
+    Listed l = {row, min((int)r.n, kList), r.listed <= kList, r.rate, r.top, r.least, r.most};
     bin_scales(s.d.scale);
+    const double upto = r.by_part ? p.bins[(size_t)row * kBins + tid] : 0.0, before = r.by_part && tid > 0 ? p.bins[(size_t)row * kBins + tid - 1] : 0.0;
+    static_assert(kRowThreads == kBins, "a bin of each thread");
     __syncthreads();
-    // the chunks' words above the bins that the cut lies in, a wavefront per chunk
-    const Chunk* sums = p.sums + (size_t)row * p.chunks;
-    const uint64_t* hist = p.hist + (size_t)row * p.chunks * kBins;
-    double above = 0.0, above_all;
-    uint32_t above_n = 0, above_count;
-    for (int c = tid >> 6; c < p.chunks; c += kRowThreads / 64) {
-        const int off = bins_below(sums[c].top, r.top);
-        double w = 0.0;
-        for (int b = tid & 63; b < r.lo - off; b += 64) {
-            const uint64_t h = hist[(size_t)c * kBins + b];
-            w += (double)(h & kWeightMask) * s.d.scale[b + off];
-            above_n += (uint32_t)(h >> kCountShift);
-        }
-        w = wave_sum(w);
-        if ((tid & 63) == 0) {
-            s.d.chunk[c] = w;
-            above += w;
-        }
-    }
-    block_before<kRowThreads>(above, s.d.waves, &above_all);
-    block_before<kRowThreads>(above_n, s.waves_i, &above_count);
-    // weights of listed words are counted in units
-    const double unit = s.d.scale[min(r.lo, kRest - 1)] * 0x1p-8;     // (exp(-lo / 8) 2^-38)
+    // the weight that a bin's are units of (behind the last but one nothing weighs anything)
+    const auto unit = [&](int bin) { return s.d.scale[min(bin, kRest - 1)]; };
     double total = r.total;
     uint32_t key = kNothing;
     int at = 0x7fffffff;
     if (r.k) {
-        find<E, false>(p, l, key, at, (double)((uint32_t)r.k - above_count), s);
+        l.look_at(r.k_bin);
+        find<E, false>(p, l, key, at, (double)((uint32_t)r.k - r.k_count), s);
         key = s.key;
         at = s.at;
-        total = above_all + s.weight * unit;
+        total = r.k_weight + s.weight * unit(l.bin);
     }
     if (r.by_part) {
-        find<E, true>(p, l, key, at, (r.part * total - above_all) / unit, s);
+        // the first bin that the running weights pass the need in, up to top_k's
+        const double need = r.part * total;
+        __syncthreads();
+        if (tid == 0) s.at = r.k ? r.k_bin : kRest;
+        __syncthreads();
+        to_least(&s.at, tid >= r.lo && upto >= need, tid);
+        __syncthreads();
+        l.look_at(s.at);
+        if (tid == l.bin) s.d.target = need - before;
+        __syncthreads();
+        find<E, true>(p, l, key, at, s.d.target / unit(l.bin), s);
         key = s.key;
         at = s.at;
     }
@@ -918,18 +936,29 @@ __global__ void __launch_bounds__(kRowThreads) sample_cut_kernel(const SamplePar
         key = r.min_key;
         at = 0x7fffffff;
     }
-    // the kept ones among the listed
+    // the chunks' words above the bin that the cut lies in, a wavefront per chunk
+    l.look_at(place_of(of_key(key), r.rate, r.top).bin);
+    const Chunk* sums = p.sums + (size_t)row * p.chunks;
+    const uint64_t* hist = p.hist + (size_t)row * p.chunks * kBins;
+    for (int c = tid >> 6; c < p.chunks; c += kRowThreads / 64) {
+        const int off = bins_below(sums[c].top, r.top);
+        double w = 0.0;
+        for (int b = tid & 63; b < l.bin - off; b += 64) w += (double)(hist[(size_t)c * kBins + b] & kWeightMask) * s.d.scale[b + off];
+        w = wave_sum(w);
+        if ((tid & 63) == 0) s.d.chunk[c] = w;
+    }
+    // the kept ones of the bin itself
     __syncthreads();
     for (int c = tid; c < p.chunks; c += kRowThreads) s.fixed[c] = 0;
     __syncthreads();
     each_word<E>(p, l, [&](uint32_t k, int number) {
-        if (k < key || (k == key && number > at)) return;
+        uint32_t w;
+        if (k < key || (k == key && number > at) || !in_bin(l, k, w)) return;
         const uint32_t c = (uint32_t)number / (uint32_t)p.chunk;
-        const uint64_t w = fixed_weight(l, s, k);
-        add_alike(c, k, [&](uint32_t n) { atomicAdd(&s.fixed[c], (unsigned long long)(w * n)); });
+        add_alike(c, k, [&](uint32_t n) { atomicAdd(&s.fixed[c], (unsigned long long)w * n); });
     });
     __syncthreads();
-    for (int c = tid; c < p.chunks; c += kRowThreads) s.d.chunk[c] += (double)s.fixed[c] * unit;
+    for (int c = tid; c < p.chunks; c += kRowThreads) s.d.chunk[c] += (double)s.fixed[c] * unit(l.bin);
     total = draw<E>(p, row, r.top, r.rate, key, at, s.d);
     if (tid == 0) {
         rp->total = total;
@@ -1014,7 +1043,7 @@ __global__ void __launch_bounds__(kThreads) sample_probs_kernel(const SamplePara
 
 struct SamplePlan {
     int tiles, chunks;
-    size_t off_hist, off_rows, off_list, total;
+    size_t off_hist, off_rows, off_bins, off_list, total;
 };
 SamplePlan plan_sample(int n_rows, int n_vocab) {
     SamplePlan pl;
@@ -1028,6 +1057,7 @@ SamplePlan plan_sample(int n_rows, int n_vocab) {
     take(sizeof(Chunk) * parts);
     pl.off_hist = take(sizeof(uint64_t) * kBins * parts);
     pl.off_rows = take(sizeof(Row) * n_rows);
+    pl.off_bins = take(sizeof(double) * kBins * n_rows);
     pl.off_list = take(sizeof(uint64_t) * kList * n_rows);
     pl.total = o;
     return pl;
@@ -1104,6 +1134,7 @@ int32_t dip_sample(const void* logits, int64_t stride, int32_t dtype, int32_t n_
     p.sums = (Chunk*)base;
     p.hist = (uint64_t*)(base + pl.off_hist);
     p.rows = (Row*)(base + pl.off_rows);
+    p.bins = (double*)(base + pl.off_bins);
     p.list = (uint64_t*)(base + pl.off_list);
     const bool cuts = p.top_k || p.top_p || p.min_p;
     return dtype == DIP_F32 ? launch_sample<float>(p, pl, cuts, probs_dtype, (hipStream_t)stream)
