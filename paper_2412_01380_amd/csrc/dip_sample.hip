@@ -39,7 +39,7 @@ constexpr int kMaxChunks = (1 << 24) / (kMaxTiles * kTile);
 constexpr int kBins = 512;                // the last one: all that lies 64 nats and more below the maximum
 constexpr int kRest = kBins - 1;
 constexpr int kPlaceBits = 23;            // of a place within a bin
-constexpr int kList = 8192;               // words of a row's list; where more qualify the row itself is gone through again
+constexpr int kList = 8192;               // most words of a row's list; where more qualify the row itself is gone through again
 constexpr int kRanges = 1024;             // key ranges of a step of narrowing down
 constexpr int kFew = 64;                  // words that a wavefront puts in order
 constexpr float kOne = 0x1p30f;           // weight 1 within a bin
@@ -142,7 +142,8 @@ struct SampleParams {
     uint64_t* hist;           // [row][chunk][kBins]
     Row* rows;
     double* bins;             // [row][kBins], of rows that top_p cuts: running weights of the bins
-    uint64_t* list;           // [row][kList]: key, number
+    uint64_t* list;           // [row][most_listed]: key, number
+    int most_listed;          // kList, or a whole row
 };
 
 // a row's settings
@@ -605,7 +606,7 @@ __global__ void __launch_bounds__(kThreads) sample_collect_kernel(const SamplePa
     __shared__ uint32_t s_at;
     const int row = blockIdx.y, tid = threadIdx.x;
     Row* r = p.rows + row;
-    if (r->state != kCut || r->listed > kList) return;
+    if (r->state != kCut || r->listed > p.most_listed) return;
     const float least = of_key(r->least), most = of_key(r->most);
     const int begin = blockIdx.x * (TILES * kTile), end = min(p.n_vocab, begin + TILES * kTile);
     const float best = p.sums[(size_t)row * p.chunks + blockIdx.x].best;
@@ -627,13 +628,13 @@ __global__ void __launch_bounds__(kThreads) sample_collect_kernel(const SamplePa
     if (tid == 0) s_at = atomicAdd(&r->n, all);
     __syncthreads();
     uint32_t at = s_at + before;
-    uint64_t* list = p.list + (size_t)row * kList;
+    uint64_t* list = p.list + (size_t)row * p.most_listed;
 #pragma unroll
     for (int t = 0; t < TILES; ++t)
 #pragma unroll
         for (int i = 0; i < kPer; ++i)
             if (hits >> (t * kPer + i) & 1) {
-                if (at < (uint32_t)kList) list[at] = ((uint64_t)key_of(f[t][i]) << 32) | (uint32_t)(begin + t * kTile + tid * kPer + i);
+                if (at < (uint32_t)p.most_listed) list[at] = ((uint64_t)key_of(f[t][i]) << 32) | (uint32_t)(begin + t * kTile + tid * kPer + i);
                 ++at;
             }
 }
@@ -679,7 +680,7 @@ template <typename E, typename F>
 __device__ __forceinline__ void each_word(const SampleParams& p, const Listed& l, F f) {
     constexpr int FLIGHT = 8;
     if (l.listed) {
-        const uint64_t* list = p.list + (size_t)l.row * kList;
+        const uint64_t* list = p.list + (size_t)l.row * p.most_listed;
         for (int i0 = threadIdx.x; i0 < l.n; i0 += FLIGHT * kRowThreads) {
             uint64_t e[FLIGHT];
 #pragma unroll
@@ -900,7 +901,7 @@ __global__ void __launch_bounds__(kRowThreads) sample_cut_kernel(const SamplePar
     Row* rp = p.rows + row;
     if (rp->state != kCut) return;
     const Row r = *rp;
-    Listed l = {row, min((int)r.n, kList), r.listed <= kList, r.rate, r.top, r.least, r.most};
+    Listed l = {row, min((int)r.n, p.most_listed), r.listed <= p.most_listed, r.rate, r.top, r.least, r.most};
     bin_scales(s.d.scale);
     const double upto = r.by_part ? p.bins[(size_t)row * kBins + tid] : 0.0, before = r.by_part && tid > 0 ? p.bins[(size_t)row * kBins + tid - 1] : 0.0;
     static_assert(kRowThreads == kBins, "a bin of each thread");
@@ -1042,7 +1043,7 @@ __global__ void __launch_bounds__(kThreads) sample_probs_kernel(const SamplePara
 }
 
 struct SamplePlan {
-    int tiles, chunks;
+    int tiles, chunks, most_listed;
     size_t off_hist, off_rows, off_bins, off_list, total;
 };
 SamplePlan plan_sample(int n_rows, int n_vocab) {
@@ -1058,7 +1059,8 @@ SamplePlan plan_sample(int n_rows, int n_vocab) {
     pl.off_hist = take(sizeof(uint64_t) * kBins * parts);
     pl.off_rows = take(sizeof(Row) * n_rows);
     pl.off_bins = take(sizeof(double) * kBins * n_rows);
-    pl.off_list = take(sizeof(uint64_t) * kList * n_rows);
+    pl.most_listed = n_vocab < kList ? n_vocab : kList;
+    pl.off_list = take(sizeof(uint64_t) * pl.most_listed * n_rows);
     pl.total = o;
     return pl;
 }
@@ -1136,6 +1138,7 @@ int32_t dip_sample(const void* logits, int64_t stride, int32_t dtype, int32_t n_
     p.rows = (Row*)(base + pl.off_rows);
     p.bins = (double*)(base + pl.off_bins);
     p.list = (uint64_t*)(base + pl.off_list);
+    p.most_listed = pl.most_listed;
     const bool cuts = p.top_k || p.top_p || p.min_p;
     return dtype == DIP_F32 ? launch_sample<float>(p, pl, cuts, probs_dtype, (hipStream_t)stream)
                             : launch_sample<uint16_t>(p, pl, cuts, probs_dtype, (hipStream_t)stream);
