@@ -550,7 +550,8 @@ typedef struct dip_rotary_scaling {
     const double* factors;  /* host; dims / 2 entries > 0: LIST                             */
 } dip_rotary_scaling;
 
-/* freq: host, dims / 2 entries.  scaling: host, NULL for none.  Host only; nothing is enqueued. */
+/* freq: host, dims / 2 entries.  scaling: host, NULL for none.  Angles (or a scaled base) beyond the finite numbers are refused.
+ * Host only; nothing is enqueued. */
 int32_t dip_rotary_frequencies(int32_t dims, double base, const dip_rotary_scaling* scaling /* host */,
                                double* freq /* host */);
 

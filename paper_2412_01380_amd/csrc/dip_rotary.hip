@@ -275,7 +275,7 @@ int32_t dip_rotary_frequencies(int32_t dims, double base, const dip_rotary_scali
                 return fail(DIP_ERR_INVALID_ARG, "rotary_frequencies: factor %d must be finite and > 0", i);
     }
     if (kind == DIP_SCALING_BASE) base *= std::pow(scaling->factor, (double)dims / (dims - 2));
-    for (int i = 0; i < dims / 2; ++i) {
+    const auto angle = [&](int i) {
         double f = std::pow(base, -2.0 * i / dims);
         if (kind == DIP_SCALING_LINEAR) f /= scaling->factor;
         if (kind == DIP_SCALING_LIST) f /= scaling->factors[i];
@@ -285,8 +285,12 @@ int32_t dip_rotary_frequencies(int32_t dims, double base, const dip_rotary_scali
             m = m < 0.0 ? 0.0 : m > 1.0 ? 1.0 : m;
             f = f * m + f / scaling->factor * (1.0 - m);
         }
-        freq[i] = f;
-    }
+        return f;
+    };
+    bool fits = std::isfinite(base) && base > 0.0;
+    for (int i = 0; i < dims / 2; ++i) fits &= std::isfinite(angle(i));
+    if (!fits) return fail(DIP_ERR_INVALID_ARG, "rotary_frequencies: base and scaling lead beyond the finite numbers");
+    for (int i = 0; i < dims / 2; ++i) freq[i] = angle(i);
     return DIP_OK;
 }
 
