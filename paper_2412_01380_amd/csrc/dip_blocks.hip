@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(kThreads) block_bounds_kernel(const BoundsPara
 // 32: 92 MB).  In fp64 without the matrix cores it took 44 us, and 24 for trees.
 // The same sums with |hi| + |lo| and |q|, T, bound what rounding does to a score: half of its products are zero, the others are D
 // roundings of 2^-23 T at most, in whatever order they are added up.  The choice settles in fp64 what lies nearer to its border than that.
-// 25 us at 3.7 TB/s; a workgroup per 64 blocks, which has to look up entry, length, pages and queries for 32 KB of bounds, took 36.
+// 28 us at 3.3 TB/s (25 where the last-level cache has them); a workgroup per 64 blocks, which has to look up entry, length, pages and queries for 32 KB of bounds, took 36.
 struct ChoiceParams {
     KvView c;
     BatchView b;
@@ -307,7 +307,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(E) == 2 ? 4 : 3) block_scores
 // One histogram of the fp32 scores finds the range that the border lies in.  What lies above it by more than three times the
 // error is chosen, what lies below it by as much is not, and the few between are scored again in fp64 (unless all of them
 // are wanted) and ranked, equal ones by number.  Where that leaves more than kNear, or no error bound is known (queries that are
-// not finite, scores beyond fp32), all are scored in fp64 and selected by the digits of their keys.
+// not finite, scores beyond fp32), all are scored in fp64 and selected by the digits of their keys.  Ranges and error are those of all
+// rows of the entry and head together, so a few scores far from the others widen them: 16 tokens over up to 64k positions take 36 us for
+// scores and choice, 67 with one block of each sequence three times as large as the others and 475 with one ten times, and three
+// trees of seven nodes 23, or 460 where one node's queries are a hundred times the others'.
 // Bound by latency, a chain of loads, barriers and LDS: 16 tokens of 10 heads, up to 2030 blocks, 11.6 us, two tokens 8.3 (256 threads
 // 17.4 and 10.6, 1024 threads 13.3 and 9.1, and 17.2 instead of 11.4 for three trees of 32 heads).
 constexpr int kChoiceThreads = 512;

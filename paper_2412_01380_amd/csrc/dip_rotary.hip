@@ -6,8 +6,9 @@
 // rounded once.  Sines and cosines are worked out once for a row and pair, into LDS, whatever the number of heads.
 //
 // Bound by bytes, every element read and written once: 8192 rows of 40 heads of 128 dims, half of them turned, 168 MB in 39.9 us
-// (34.7 at the rate of a large copy, 4.83 TB/s); 7095 rows of two prompts, 40 query heads and 10 for keys and values, 218 MB in 50.6
-// us (45).  Few rows by latency: 7 rows 7.1 us, three trees of 7 nodes into the cache 9.4, of which a launch takes 4.4; hence
+// (34.7 at the rate of a large copy, 4.83 TB/s); 7095 rows of two prompts, 40 query heads and 10 for keys and values, 218 MB in 50.7
+// us (45); both with inputs that change from call to call, and 28 and 35 us where the call before left them in the last-level
+// cache.  Few rows by latency: 7 rows 7.1 us, three trees of 7 nodes into the cache 9.4, of which a launch takes 4.4; hence
 // fewer rows to a workgroup then.
 
 #include <cmath>

@@ -15,8 +15,8 @@
 // lies, in units of 2^-23 of a bin.  Its bin is D >> 23, and its weight exp(-bin / 8) times a factor in (0.88, 1] that follows
 // from the other bits and is held in units of 2^-30.  So sums over a bin are integer sums, the same in any order, and 2^-26
 // accurate relative to the weight itself however small it is (but for the last bin's, 63.75 nats and more down, which counts for
-// nothing), and two chunks agree on every word's bin.  (Of an fp32 l / T 2^-24 is
-// lost, which at 30 nats is a weight off by 2 in 10^6.)
+// nothing), and two chunks agree on every word's bin.  (Of an fp32 l / T 2^-24 is lost, which at 30 nats is a weight off by 2 in
+// 10^6.)
 
 #include <cfloat>
 #include <cmath>
@@ -27,9 +27,12 @@
 namespace dip {
 namespace {
 
-// Where the time goes: 512 rows of 128256, fp32, with probabilities, 223 us: chunks 57 (263 MB; the integer places and the histogram
-// take longer than the read, 41), rows 14, list 43, cut 27, probabilities 81 (525 MB).  64 rows in bf16 49 us, a row of 32064 35 us: five
-// launches in a chain, the cut the longest of them (14 to 21 us of loads, barriers and sums that wait for one another).
+// Where the time goes: 512 rows of 128256, fp32, with probabilities, 228 us; under the profiler, logits that change from call to call:
+// chunks 65 (263 MB; the integer places and the histogram take longer than the read, 41), rows 16, list 52, cut 31, probabilities 77
+// (525 MB).  64 rows in bf16 without probabilities 49 us, four launches in a chain, a row of 32064 with them 34 us, five: the cut is the
+// longest of them (14 to 23 us of loads, barriers and sums that wait for one another).  Without a rule 19 us for the 64 rows and 154
+// for the 512, greedy 10 and 113.  Words that meet in one bin queue for its LDS word: where 95 % of them are -1e4 64 rows without a rule take
+// 40 us and 512 303, and 18 and 138 where these are -inf, which no bin counts.
 //
 constexpr int kThreads = 256;             // of the kernels over chunks
 constexpr int kRowThreads = 512;          // of the kernels that have a workgroup per row
@@ -39,7 +42,9 @@ constexpr int kMaxChunks = (1 << 24) / (kMaxTiles * kTile);
 constexpr int kBins = 512;                // the last one: all that lies 64 nats and more below the maximum
 constexpr int kRest = kBins - 1;
 constexpr int kPlaceBits = 23;            // of a place within a bin
-constexpr int kList = 8192;               // most words of a row's list; where more qualify the row itself is gone through again
+// Most words of a row's list.  Where more qualify, a workgroup goes through the row itself again: top_p 0.9 of 64 rows takes 49 us where
+// logits deviate by 2.5, 60 by 1, 246 by 0.5, 408 where all are equal, and behind a top_k of 20000 307.
+constexpr int kList = 8192;
 constexpr int kRanges = 1024;             // key ranges of a step of narrowing down
 constexpr int kFew = 64;                  // words that a wavefront puts in order
 constexpr float kOne = 0x1p30f;           // weight 1 within a bin
@@ -704,7 +709,8 @@ __device__ __forceinline__ void each_word(const SampleParams& p, const Listed& l
     }
 }
 // add(n) by the active lanes: those that agree with the first of them in `at` and `key` leave it to that one, n of them together.
-// (A wavefront's atomics on one LDS word take their turns: rows of 128256 equal logits 935 us one by one, 494 so.)
+// (A wavefront's atomics on one LDS word take their turns: rows of 128256 equal logits 935 us one by one, 494 so, all rules; 408 since
+// each rule looks at one bin.)
 template <typename F>
 __device__ __forceinline__ void add_alike(uint32_t at, uint32_t key, F add) {
     const bool alike = at == (uint32_t)__builtin_amdgcn_readfirstlane((int)at) && key == (uint32_t)__builtin_amdgcn_readfirstlane((int)key);
